@@ -1,0 +1,105 @@
+/*
+ * kt operators -- the parts of a transformer block's training pass that make
+ * the gradients which kt.h packs, reduces and applies: layer norm with its
+ * backward pass, and activation checkpoints in 8 bits.
+ *
+ * The conventions of kt.h hold: status codes, kt_last_error(), device pointers
+ * owned by the caller, asynchronous calls on `stream`.  Beyond them:
+ *  - The calls need no plan and keep nothing between calls: no allocation, no
+ *    upload, no wait, no memory that has to start at zero.  Every one of them
+ *    may be recorded into a HIP graph, without an eager call before it.
+ *  - Scratch memory is the caller's: kt_*_workspace() says how many bytes a
+ *    call needs (0: none, `ws` may be NULL), aligned to 16.  Its contents mean
+ *    nothing before or after the call; calls on different streams need one each.
+ *  - Weight gradients may be written where a bucket keeps them: any address
+ *    that is a multiple of the element size will do.
+ *  - Sums, softmax statistics and products are held in binary32; a result is
+ *    rounded to bf16 once, to nearest-even.  Results depend on the arguments
+ *    alone: no atomics, every sum has a fixed order.
+ *  - A matrix [rows, cols] has adjacent columns and rows `ld` elements apart
+ *    (ld >= cols).  Rows may be 0: then weight gradients are written as 0.
+ *  - Outputs must not overlap inputs or each other, except where a call says so.
+ */
+#ifndef KT_OPS_H
+#define KT_OPS_H
+
+#include "kt.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- layer norm ---------------------------------------------------------------- */
+
+#define KT_LAYERNORM_MAX_COLS 16384
+
+/*
+ * y = (x - mean) * rstd * gamma + beta for every row, with mean the row's mean
+ * and rstd = 1 / sqrt(mean((x - mean)^2) + eps), both from the row itself in
+ * two steps (no E[x^2] - mean^2).
+ *
+ *   dt          type of x and y;  pdt: type of gamma and beta.
+ *   beta        may be NULL (no bias).
+ *   mean, rstd  rows floats each, for the backward pass; both NULL: not wanted.
+ *   y8, e8      both NULL, or the 8-bit checkpoint of y (as stored), written in
+ *               the same pass: bit-identical to kt_act8_save(y).
+ * y may be x itself (same ld).
+ * Errors: KT_EINVAL (NULL, sizes, eps negative or not finite, overlap),
+ * KT_EALIGN, KT_EUNSUPPORTED (cols > KT_LAYERNORM_MAX_COLS).
+ */
+KT_API kt_status kt_layernorm_fwd(kt_dtype dt, kt_dtype pdt, int64_t rows,
+                                  int64_t cols, const void *x, int64_t ldx,
+                                  const void *gamma, const void *beta, float eps,
+                                  void *y, int64_t ldy, float *mean, float *rstd,
+                                  int8_t *y8, uint8_t *e8, void *stream);
+
+/*
+ * The gradients of kt_layernorm_fwd from dy: with xh = (x - mean) * rstd and
+ * t = gamma * dy,
+ *   dx     = rstd * (t - mean(t) - xh * mean(t * xh))     (means over the row)
+ *   dgamma = sum over rows of dy * xh,   dbeta = sum over rows of dy.
+ * The input is x, or (x == NULL) its 8-bit checkpoint x8, e8; mean and rstd are
+ * those that the forward pass left.
+ *   dt          type of dy, x and dx;  pdt: type of gamma, dgamma and dbeta.
+ *   dx          may be dy or x itself (same ld).
+ *   dbeta       may be NULL.
+ *   ws          kt_layernorm_bwd_workspace(rows, cols) bytes.
+ * Errors as above; KT_EINVAL also for both or neither of x and x8, and for a
+ * workspace that is too small.
+ */
+KT_API int64_t kt_layernorm_bwd_workspace(int64_t rows, int64_t cols);
+KT_API kt_status kt_layernorm_bwd(kt_dtype dt, kt_dtype pdt, int64_t rows,
+                                  int64_t cols, const void *dy, int64_t lddy,
+                                  const void *x, int64_t ldx, const int8_t *x8,
+                                  const uint8_t *e8, const void *gamma,
+                                  const float *mean, const float *rstd, void *dx,
+                                  int64_t lddx, void *dgamma, void *dbeta,
+                                  void *ws, int64_t ws_bytes, void *stream);
+
+/* ---- activation checkpoints in 8 bits ------------------------------------------- */
+
+/*
+ * A checkpoint of a matrix x [rows, cols] is
+ *   q  rows x (32 * G) int8, G = ceil(cols / 32); columns past cols hold 0,
+ *   e  rows x G bytes,
+ * and stands for q * 2^(e - 127), one e for 32 neighbouring columns.  With a the
+ * largest magnitude of the 32 and 2^E <= a < 2^(E+1):
+ *   e = max(E - 6 + 127, 1),  q = rint(x * 2^(127 - e)) clamped to [-127, 127]
+ * (ties to even).  The scale being a power of two, the one rounding is that of q:
+ * at most half a step of 2^(e - 127) <= a / 64, one step for a member that is
+ * clamped (a >= 127.5 steps); every value that q stands for is exact in bf16.
+ * A group with a member that is not finite has e = 255 and q = 0 and stands for
+ * NaN throughout, so that an overflow is not hidden.
+ * A checkpoint takes 1.03 bytes an element.
+ */
+KT_API kt_status kt_act8_save(kt_dtype dt, int64_t rows, int64_t cols,
+                              const void *x, int64_t ldx, int8_t *q, uint8_t *e,
+                              void *stream);
+KT_API kt_status kt_act8_restore(kt_dtype dt, int64_t rows, int64_t cols,
+                                 const int8_t *q, const uint8_t *e, void *y,
+                                 int64_t ldy, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* KT_OPS_H */

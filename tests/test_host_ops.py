@@ -1,0 +1,136 @@
+"""What the operators refuse, before any GPU is touched: the C calls get addresses that nothing reads, the binding gets tensors
+that are not on a GPU."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2505_10183_amd as kt
+from paper_2505_10183_amd import ops
+
+EINVAL, EALIGN, EUNSUPPORTED = 1, 2, 5
+F32, BF16 = 0, 1
+M = 1 << 20                        # each argument has a MiB of addresses of its own
+
+
+def at(i):
+    return (i + 1) * M
+
+
+def call(name, args, status, word, **changes):
+    """The call with some arguments changed is refused with this status and a message that says why."""
+    L = ops._library()
+    a = dict(args, **changes)
+    got = getattr(L, name)(*a.values())
+    text = L.kt_last_error().decode()
+    assert got == status, (name, changes, got, text)
+    assert name in text and word in text, (changes, text)
+
+
+LN_FWD = dict(dt=F32, pdt=F32, rows=8, cols=64, x=at(0), ldx=64, gamma=at(1), beta=at(2), eps=1e-5, y=at(3), ldy=64, mean=at(4),
+              rstd=at(5), y8=at(6), e8=at(7), stream=0)
+LN_BWD = dict(dt=F32, pdt=F32, rows=8, cols=64, dy=at(0), lddy=64, x=at(1), ldx=64, x8=0, e8=0, gamma=at(2), mean=at(3), rstd=at(4),
+              dx=at(5), lddx=64, dgamma=at(6), dbeta=at(7), ws=at(8), ws_bytes=M, stream=0)
+SAVE = dict(dt=F32, rows=8, cols=64, x=at(0), ldx=64, q=at(1), e=at(2), stream=0)
+RESTORE = dict(dt=F32, rows=8, cols=64, q=at(1), e=at(2), y=at(0), ldy=64, stream=0)
+
+
+@pytest.mark.parametrize("changes,status,word", [
+    (dict(dt=2), EINVAL, "type"), (dict(pdt=-1), EINVAL, "type"),
+    (dict(rows=-1), EINVAL, "rows"), (dict(cols=0), EINVAL, "cols"), (dict(ldx=63), EINVAL, "ld"), (dict(ldy=63), EINVAL, "ld"),
+    (dict(rows=1 << 60), EINVAL, "rows"), (dict(ldx=1 << 62), EINVAL, "ld"),
+    (dict(cols=16385, ldx=16385, ldy=16385), EUNSUPPORTED, "columns"),
+    (dict(eps=-1.0), EINVAL, "eps"), (dict(eps=math.nan), EINVAL, "eps"), (dict(eps=math.inf), EINVAL, "eps"),
+    (dict(x=0), EINVAL, "NULL"), (dict(gamma=0), EINVAL, "NULL"), (dict(y=0), EINVAL, "NULL"),
+    (dict(mean=0), EINVAL, "together"), (dict(rstd=0), EINVAL, "together"), (dict(y8=0), EINVAL, "together"), (dict(e8=0), EINVAL, "together"),
+    (dict(x=at(0) + 2), EALIGN, "x"), (dict(y=at(3) + 1), EALIGN, "y"), (dict(gamma=at(1) + 2), EALIGN, "gamma"),
+    (dict(beta=at(2) + 1), EALIGN, "beta"), (dict(mean=at(4) + 2), EALIGN, "mean"), (dict(rstd=at(5) + 1), EALIGN, "rstd"),
+    (dict(y8=at(6) + 8), EALIGN, "y8"),
+    (dict(y=at(0) + 4), EINVAL, "overlaps"), (dict(y=at(0), ldy=65), EINVAL, "overlaps"), (dict(mean=at(5)), EINVAL, "overlaps"),
+    (dict(rstd=at(0) + 4 * 511), EINVAL, "overlaps"), (dict(y8=at(3)), EINVAL, "overlaps"), (dict(e8=at(1)), EINVAL, "overlaps"),
+    (dict(y=at(2) - 4 * 511), EINVAL, "overlaps"),
+])
+def test_layernorm_fwd_refuses(changes, status, word):
+    call("kt_layernorm_fwd", LN_FWD, status, word, **changes)
+
+
+@pytest.mark.parametrize("changes,status,word", [
+    (dict(dt=2), EINVAL, "type"), (dict(pdt=2), EINVAL, "type"),
+    (dict(rows=-1), EINVAL, "rows"), (dict(cols=0), EINVAL, "cols"), (dict(lddy=63), EINVAL, "ld"), (dict(ldx=63), EINVAL, "ld"),
+    (dict(lddx=63), EINVAL, "ld"), (dict(cols=16385, lddy=16385, ldx=16385, lddx=16385), EUNSUPPORTED, "columns"),
+    (dict(dy=0), EINVAL, "NULL"), (dict(gamma=0), EINVAL, "NULL"), (dict(mean=0), EINVAL, "NULL"), (dict(rstd=0), EINVAL, "NULL"),
+    (dict(dx=0), EINVAL, "NULL"), (dict(dgamma=0), EINVAL, "NULL"), (dict(dgamma=0, rows=0), EINVAL, "NULL"),
+    (dict(x=0), EINVAL, "either"), (dict(x8=at(9), e8=at(10)), EINVAL, "either"), (dict(x=0, x8=at(9)), EINVAL, "either"),
+    (dict(x=0, e8=at(9)), EINVAL, "either"),
+    (dict(ws=0), EINVAL, "workspace"), (dict(ws_bytes=511), EINVAL, "workspace"),
+    (dict(ws=at(8) + 4), EALIGN, "ws"), (dict(dy=at(0) + 2), EALIGN, "dy"), (dict(x=at(1) + 2), EALIGN, "x"), (dict(dx=at(5) + 2), EALIGN, "dx"),
+    (dict(dgamma=at(6) + 2), EALIGN, "dgamma"), (dict(dbeta=at(7) + 2), EALIGN, "dbeta"), (dict(gamma=at(2) + 2), EALIGN, "gamma"),
+    (dict(mean=at(3) + 2), EALIGN, "mean"), (dict(rstd=at(4) + 2), EALIGN, "rstd"), (dict(x=0, x8=at(9) + 8, e8=at(10)), EALIGN, "x8"),
+    (dict(dx=at(0) + 4), EINVAL, "overlaps"), (dict(dx=at(1) + 4), EINVAL, "overlaps"), (dict(dgamma=at(2)), EINVAL, "overlaps"),
+    (dict(dbeta=at(6) + 4 * 63), EINVAL, "overlaps"), (dict(ws=at(5)), EINVAL, "overlaps"), (dict(dgamma=at(0)), EINVAL, "overlaps"),
+    (dict(dx=at(3)), EINVAL, "overlaps"), (dict(x=0, x8=at(5), e8=at(10)), EINVAL, "overlaps"), (dict(x=0, x8=at(9), e8=at(5)), EINVAL, "overlaps"),
+])
+def test_layernorm_bwd_refuses(changes, status, word):
+    call("kt_layernorm_bwd", LN_BWD, status, word, **changes)
+
+
+@pytest.mark.parametrize("name,args,wide", [("kt_act8_save", SAVE, "x"), ("kt_act8_restore", RESTORE, "y")])
+def test_act8_refuses(name, args, wide):
+    ld = "ld" + wide
+    for changes, status, word in [
+            (dict(dt=3), EINVAL, "type"), (dict(rows=-1), EINVAL, "rows"), (dict(cols=0), EINVAL, "cols"), ({ld: 63}, EINVAL, "ld"),
+            ({"cols": (1 << 30) + 1, ld: 1 << 31}, EUNSUPPORTED, "columns"),
+            ({wide: 0}, EINVAL, "NULL"), (dict(q=0), EINVAL, "NULL"), (dict(e=0), EINVAL, "NULL"),
+            ({wide: at(0) + 2}, EALIGN, wide), (dict(q=at(1) + 8), EALIGN, "q"),
+            (dict(q=at(0)), EINVAL, "overlaps"), (dict(e=at(0) + 3), EINVAL, "overlaps")]:
+        call(name, args, status, word, **changes)
+    if name == "kt_act8_save":
+        call(name, args, EINVAL, "overlaps", e=at(1) + 511)
+
+
+def test_columns_of_one_buffer_may_lie_side_by_side():
+    """Equal distances between rows: x in columns 0..63, dx in 64..127 of a buffer 128 wide.  One column too far is refused (the
+    others are refused for their NULL dgamma only, so nothing is launched)."""
+    wide = dict(LN_FWD, ldx=128, ldy=128, y8=0, e8=0)
+    call("kt_layernorm_fwd", wide, EINVAL, "y overlaps x", y=at(0) + 4 * 63)
+    call("kt_layernorm_fwd", wide, EINVAL, "y overlaps x", y=at(0) + 4 * (128 - 63))
+    call("kt_layernorm_fwd", wide, EINVAL, "rstd overlaps mean", y=at(0) + 4 * 64, mean=at(5))       # y passed its check
+    call("kt_layernorm_fwd", wide, EINVAL, "rstd overlaps mean", y=at(0) - 4 * 64, mean=at(5))
+
+
+def test_nothing_to_do_touches_no_gpu():
+    L = ops._library()
+    assert L.kt_layernorm_fwd(*dict(LN_FWD, rows=0).values()) == 0
+    assert L.kt_act8_save(*dict(SAVE, rows=0, x=0, q=0, e=0).values()) == 0
+    assert L.kt_act8_restore(*dict(RESTORE, rows=0, y=0, q=0, e=0).values()) == 0
+
+
+def test_layernorm_workspace():
+    for rows, cols in [(-1, 64), (8, 0), (8, 16385), (0, 64)]:
+        assert kt.kt_layernorm_bwd_workspace(rows, cols) == 0
+    for rows in (1, 15, 16, 17, 8191, 8192, 1 << 40):
+        for cols in (1, 63, 64, 65, 16384):
+            n = kt.kt_layernorm_bwd_workspace(rows, cols)
+            assert n % (2 * 64 * 4) == 0 and 2 * 4 * cols <= n <= 2 * 4 * 512 * (cols + 63)
+
+
+def test_act8_shapes():
+    assert kt.kt_act8_shapes(5, 1) == ((5, 32), (5, 1))
+    assert kt.kt_act8_shapes(5, 32) == ((5, 32), (5, 1))
+    assert kt.kt_act8_shapes(0, 33) == ((0, 64), (0, 2))
+
+
+def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
+    x, g, v = torch.zeros(4, 64), torch.zeros(64), torch.zeros(4)
+    q, e = torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4, 2, dtype=torch.uint8)
+    for f in (lambda: kt.kt_layernorm_fwd(x, g, g, 1e-5, x, v, v),
+              lambda: kt.kt_layernorm_bwd(x, x, g, v, v, x, g, g),
+              lambda: kt.kt_act8_save(x, q, e),
+              lambda: kt.kt_act8_restore(q, e, x)):
+        if torch.cuda.is_available():
+            with pytest.raises(ValueError, match="current GPU"):
+                f()
+        else:
+            with pytest.raises((ValueError, RuntimeError, AssertionError)):
+                f()
