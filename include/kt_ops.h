@@ -1,7 +1,8 @@
 /*
  * kt operators -- the parts of a transformer block's training pass that make
  * the gradients which kt.h packs, reduces and applies: layer norm with its
- * backward pass, and activation checkpoints in 8 bits.
+ * backward pass, and activation checkpoints in 8 bits with the weight gradient
+ * of a linear layer from them.
  *
  * The conventions of kt.h hold: status codes, kt_last_error(), device pointers
  * owned by the caller, asynchronous calls on `stream`.  Beyond them:
@@ -98,6 +99,24 @@ KT_API kt_status kt_act8_save(kt_dtype dt, int64_t rows, int64_t cols,
 KT_API kt_status kt_act8_restore(kt_dtype dt, int64_t rows, int64_t cols,
                                  const int8_t *q, const uint8_t *e, void *y,
                                  int64_t ldy, void *stream);
+
+/*
+ * The weight gradient of a linear layer y = x W^T from the checkpoint of its
+ * input: dw[o, i] = sum over t of dy[t, o] * x8[t, i].
+ *   dt   type of dy [tokens, out];  gdt: type of dw [out, in].
+ *   q, e the checkpoint of x [tokens, in].
+ *   ws   kt_act8_weight_grad_workspace(...) bytes.
+ * bf16 dy: products of bf16 pairs, exact, summed in binary32.  f32 dy: binary32
+ * products and sums.  lddw >= in: dw may be a window of a larger matrix.  out
+ * and in are at most 2^30.
+ */
+KT_API int64_t kt_act8_weight_grad_workspace(kt_dtype dt, int64_t tokens,
+                                             int64_t out, int64_t in);
+KT_API kt_status kt_act8_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t tokens,
+                                     int64_t out, int64_t in, const void *dy,
+                                     int64_t lddy, const int8_t *q,
+                                     const uint8_t *e, void *dw, int64_t lddw,
+                                     void *ws, int64_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -19,4 +19,5 @@ def __getattr__(name):
     raise AttributeError("module %r has no attribute %r" % (__name__, name))
 
 
-_OPERATORS = ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_layernorm_bwd_workspace", "kt_act8_shapes", "kt_act8_save", "kt_act8_restore")
+_OPERATORS = ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_layernorm_bwd_workspace", "kt_act8_shapes", "kt_act8_save", "kt_act8_restore",
+              "kt_act8_weight_grad", "kt_act8_weight_grad_workspace")

@@ -162,7 +162,7 @@ extern "C" kt_status kt_layernorm_bwd(kt_dtype dt, kt_dtype pdt, int64_t rows, i
                                                  dgamma, dbeta, (float *)ws, stream));
 }
 
-// A chunk's column and the number of chunks of a piece of rows are 31-bit numbers in the kernels.
+// Columns are 31-bit numbers in the kernels.
 static const int64_t MOST_ACT8_COLS = 1 << 30;
 
 extern "C" kt_status kt_act8_save(kt_dtype dt, int64_t rows, int64_t cols, const void *x, int64_t ldx, int8_t *q, uint8_t *e,
@@ -200,4 +200,38 @@ extern "C" kt_status kt_act8_restore(kt_dtype dt, int64_t rows, int64_t cols, co
     KT_TRY(apart(who, out, flat("q", q, rows * G * KT_ACT8_GROUP)));
     KT_TRY(apart(who, out, flat("e", e, rows * G)));
     return launched(who, kt_launch_act8_restore(dt, rows, cols, q, e, y, ldy, stream));
+}
+
+static bool weight_grad_sizes(int64_t tokens, int64_t out, int64_t in)
+{
+    return tokens >= 0 && tokens <= (1ll << 40) && out >= 1 && in >= 1 && out <= MOST_ACT8_COLS && in <= MOST_ACT8_COLS && out * in <= (1ll << 46);
+}
+
+extern "C" int64_t kt_act8_weight_grad_workspace(kt_dtype dt, int64_t tokens, int64_t out, int64_t in)
+{
+    return is_type(dt) && weight_grad_sizes(tokens, out, in) ? kt_weight_grad_ws(dt, tokens, out, in) : 0;
+}
+
+extern "C" kt_status kt_act8_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t tokens, int64_t out, int64_t in, const void *dy,
+                                         int64_t lddy, const int8_t *q, const uint8_t *e, void *dw, int64_t lddw, void *ws,
+                                         int64_t ws_bytes, void *stream)
+{
+    const char *who = "kt_act8_weight_grad";
+    if (!is_type(dt) || !is_type(gdt)) return bad(who, "unknown element type");
+    if (!sizes(tokens, out, lddy) || !sizes(out, in, lddw)) return bad(who, "tokens >= 0, out and in >= 1 and ld >= columns are needed");
+    if (!weight_grad_sizes(tokens, out, in)) return unsupported(who, "more than 2^40 tokens, 2^30 rows or columns, or 2^46 weights");
+    if (!dw || (tokens && (!dy || !q || !e))) return bad(who, "NULL dy, q, e or dw");
+    const int64_t need = kt_weight_grad_ws(dt, tokens, out, in);
+    if (need && (!ws || ws_bytes < need)) return bad(who, "the workspace is smaller than kt_act8_weight_grad_workspace says");
+    KT_TRY(aligned(who, "dy", dy, size_of(dt)));
+    KT_TRY(aligned(who, "q", q, 16));
+    KT_TRY(aligned(who, "dw", dw, size_of(gdt)));
+    KT_TRY(aligned(who, "ws", ws, 16));
+    const int64_t G = kt_act8_groups(in);
+    const Block outs[] = {matrix("dw", dw, gdt, out, in, lddw), flat("ws", ws, need)};
+    const Block ins[] = {matrix("dy", dy, dt, tokens, out, lddy), flat("q", q, tokens * G * KT_ACT8_GROUP), flat("e", e, tokens * G)};
+    for (const Block &o : outs)
+        for (const Block &i : ins) KT_TRY(apart(who, o, i));
+    KT_TRY(apart(who, outs[1], outs[0]));
+    return launched(who, kt_launch_weight_grad(dt, gdt, tokens, (int)out, (int)in, dy, lddy, q, e, dw, lddw, (float *)ws, stream));
 }

@@ -24,5 +24,8 @@ int kt_launch_act8_save(kt_dtype dt, int64_t rows, int64_t cols, const void *x, 
                         void *stream);
 int kt_launch_act8_restore(kt_dtype dt, int64_t rows, int64_t cols, const int8_t *q, const uint8_t *e, void *y,
                            int64_t ldy, void *stream);
+int64_t kt_weight_grad_ws(kt_dtype dt, int64_t tokens, int64_t out, int64_t in);
+int kt_launch_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t tokens, int out, int in, const void *dy, int64_t lddy,
+                          const int8_t *q, const uint8_t *e, void *dw, int64_t lddw, float *ws, void *stream);
 
 #endif

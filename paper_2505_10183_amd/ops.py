@@ -31,7 +31,10 @@ def _library() -> ctypes.CDLL:
         L.kt_layernorm_bwd.argtypes = [i32, i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
         L.kt_act8_save.argtypes = [i32, i64, i64, vp, i64, vp, vp, vp]
         L.kt_act8_restore.argtypes = [i32, i64, i64, vp, vp, vp, i64, vp]
-        for n in ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore"):
+        L.kt_act8_weight_grad_workspace.argtypes = [i32, i64, i64, i64]
+        L.kt_act8_weight_grad_workspace.restype = i64
+        L.kt_act8_weight_grad.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+        for n in ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore", "kt_act8_weight_grad"):
             getattr(L, n).restype = i32
         _lib = L
     return L
@@ -169,5 +172,25 @@ def kt_act8_restore(q, e, y, stream=None):
     p, rows, cols, ld = _matrix(y, "y")
     pq, pe = _act8(q, e, rows, cols, "checkpoint")
     status = L.kt_act8_restore(_type(y, "y"), rows, cols, pq, pe, p, ld, _stream(stream))
+    if status:
+        _check(status, L)
+
+
+def kt_act8_weight_grad_workspace(dtype, tokens: int, out: int, inn: int) -> int:
+    return _library().kt_act8_weight_grad_workspace(_TYPES[dtype], tokens, out, inn)
+
+
+def kt_act8_weight_grad(dy, q, e, dw, workspace=None, stream=None):
+    """dw [out, in] = dy^T x8: the weight gradient of a linear layer from dy [tokens, out] and the 8-bit checkpoint of its
+    input [tokens, in].  dw may be float32 or bfloat16 whatever dy is, and may lie in a bucket."""
+    L = _library()
+    p, tokens, out, ld = _matrix(dy, "dy")
+    pw, rows, inn, ldw = _matrix(dw, "dw")
+    if rows != out:
+        raise ValueError("dw: %d rows are needed, got %d" % (out, rows))
+    t = _type(dy, "dy")
+    pq, pe = _act8(q, e, tokens, inn, "checkpoint")
+    ws, size, held = _workspace(workspace, L.kt_act8_weight_grad_workspace(t, tokens, out, inn), stream, dy.device)
+    status = L.kt_act8_weight_grad(t, _type(dw, "dw"), tokens, out, inn, p, ld, pq, pe, pw, ldw, ws, size, _stream(stream))
     if status:
         _check(status, L)

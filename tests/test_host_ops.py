@@ -89,6 +89,32 @@ def test_act8_refuses(name, args, wide):
         call(name, args, EINVAL, "overlaps", e=at(1) + 511)
 
 
+WEIGHT_GRAD = dict(dt=BF16, gdt=BF16, tokens=4096, out=64, inn=64, dy=at(0), lddy=64, q=at(1), e=at(2), dw=at(3), lddw=64, ws=at(4),
+                   ws_bytes=M, stream=0)
+
+
+@pytest.mark.parametrize("changes,status,word", [
+    (dict(dt=2), EINVAL, "type"), (dict(gdt=2), EINVAL, "type"), (dict(tokens=-1), EINVAL, "tokens"), (dict(out=0), EINVAL, "out"),
+    (dict(inn=0), EINVAL, "in"), (dict(lddy=63), EINVAL, "ld"), (dict(lddw=63), EINVAL, "ld"),
+    (dict(tokens=(1 << 40) + 1), EUNSUPPORTED, "tokens"), (dict(out=(1 << 30) + 1, lddy=1 << 31), EUNSUPPORTED, "2^30"),
+    (dict(inn=(1 << 30) + 1, lddw=1 << 31), EUNSUPPORTED, "2^30"), (dict(out=1 << 24, inn=1 << 23, lddy=1 << 24, lddw=1 << 23), EUNSUPPORTED, "2^46"),
+    (dict(dy=0), EINVAL, "NULL"), (dict(q=0), EINVAL, "NULL"), (dict(e=0), EINVAL, "NULL"), (dict(dw=0), EINVAL, "NULL"),
+    (dict(dw=0, tokens=0), EINVAL, "NULL"), (dict(ws=0), EINVAL, "workspace"), (dict(ws_bytes=1), EINVAL, "workspace"),
+    (dict(dy=at(0) + 1), EALIGN, "dy"), (dict(q=at(1) + 8), EALIGN, "q"), (dict(dw=at(3) + 1), EALIGN, "dw"), (dict(ws=at(4) + 8), EALIGN, "ws"),
+    (dict(dw=at(0) + 2 * 64 * 100), EINVAL, "overlaps"), (dict(dw=at(1)), EINVAL, "overlaps"), (dict(dw=at(2)), EINVAL, "overlaps"),
+    (dict(ws=at(3)), EINVAL, "overlaps"), (dict(ws=at(1)), EINVAL, "overlaps"),
+])
+def test_weight_grad_refuses(changes, status, word):
+    call("kt_act8_weight_grad", WEIGHT_GRAD, status, word, **changes)
+
+
+def test_weight_grad_workspace():
+    for args in [(torch.float32, -1, 4, 4), (torch.float32, 4, 0, 4), (torch.bfloat16, 4, 4, 0), (torch.float32, 1, 64, 64)]:
+        assert kt.kt_act8_weight_grad_workspace(*args) == 0
+    n = kt.kt_act8_weight_grad_workspace(torch.bfloat16, 4096, 64, 65)
+    assert n % (64 * 68 * 4) == 0 and n > 0
+
+
 def test_columns_of_one_buffer_may_lie_side_by_side():
     """Equal distances between rows: x in columns 0..63, dx in 64..127 of a buffer 128 wide.  One column too far is refused (the
     others are refused for their NULL dgamma only, so nothing is launched)."""
@@ -127,7 +153,8 @@ def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
     for f in (lambda: kt.kt_layernorm_fwd(x, g, g, 1e-5, x, v, v),
               lambda: kt.kt_layernorm_bwd(x, x, g, v, v, x, g, g),
               lambda: kt.kt_act8_save(x, q, e),
-              lambda: kt.kt_act8_restore(q, e, x)):
+              lambda: kt.kt_act8_restore(q, e, x),
+              lambda: kt.kt_act8_weight_grad(x, q, e, x)):
         if torch.cuda.is_available():
             with pytest.raises(ValueError, match="current GPU"):
                 f()
