@@ -1,8 +1,8 @@
 /*
  * kt operators -- the parts of a transformer block's training pass that make
  * the gradients which kt.h packs, reduces and applies: layer norm with its
- * backward pass, and activation checkpoints in 8 bits with the weight gradient
- * of a linear layer from them.
+ * backward pass, activation checkpoints in 8 bits with the weight gradient of
+ * a linear layer from them, and attention with its backward pass.
  *
  * The conventions of kt.h hold: status codes, kt_last_error(), device pointers
  * owned by the caller, asynchronous calls on `stream`.  Beyond them:
@@ -117,6 +117,58 @@ KT_API kt_status kt_act8_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t tokens,
                                      int64_t lddy, const int8_t *q,
                                      const uint8_t *e, void *dw, int64_t lddw,
                                      void *ws, int64_t ws_bytes, void *stream);
+
+/* ---- attention ------------------------------------------------------------------ */
+
+#define KT_ATTENTION_MAX_DIM 128
+
+/* A tensor [batch, tokens, heads, dim] with adjacent elements of a head; strides in elements, >= 0. */
+typedef struct {
+    void *data;
+    int64_t batch, token, head;
+} kt_heads;
+
+/* Sizes and mask shared by the forward and the backward pass. */
+typedef struct {
+    kt_dtype dt;                  /* type of all tensors but lse                         */
+    int64_t batch, nq, nk;        /* sequences, queries and keys of each                 */
+    int64_t heads, kv_heads;      /* kv_heads divides heads: query head h reads key head h / (heads / kv_heads) */
+    int64_t dim;                  /* 1 .. KT_ATTENTION_MAX_DIM                           */
+    float scale;                  /* of the scores; finite and > 0                       */
+    int causal;                   /* query i sees keys j <= i + nk - nq only             */
+    const int32_t *k_lens;        /* device, batch entries, or NULL: keys j >= k_lens[b] are not seen */
+} kt_attention;
+
+/*
+ * o = softmax(scale * q k^T) v over the keys that a query sees, and lse, the
+ * logarithm of the softmax's denominator [batch, heads, nq] in binary32.  A
+ * query that sees no key gets o = 0 and lse = -inf.  Keys at and past k_lens[b]
+ * are not read; a value k_lens[b] outside [0, nk] counts as the nearer end.
+ * The causal mask gives a key no weight, and does not stop a NaN or infinity
+ * in a v row from reaching earlier queries of the same tile (0 * inf).
+ * lse may be NULL (no backward pass).
+ */
+KT_API kt_status kt_attention_fwd(const kt_attention *a, const kt_heads *q,
+                                  const kt_heads *k, const kt_heads *v,
+                                  const kt_heads *o, float *lse, void *stream);
+
+/*
+ * The gradients of q, k and v from that of o.  The probabilities are computed
+ * again from q, k and lse: p = exp(scale * q k^T - lse); with
+ * delta = rowsum(d_o * o) and ds = p * (d_o v^T - delta),
+ *   dq = scale * ds k,  dk = scale * ds^T q,  dv = p^T d_o,
+ * dk and dv summed over the query heads that share a key head.  Every element
+ * of dq, dk and dv is written: 0 where a query sees no key, and for keys past
+ * k_lens.
+ *   ws  kt_attention_bwd_workspace(a) bytes.
+ */
+KT_API int64_t kt_attention_bwd_workspace(const kt_attention *a);
+KT_API kt_status kt_attention_bwd(const kt_attention *a, const kt_heads *d_o,
+                                  const kt_heads *q, const kt_heads *k,
+                                  const kt_heads *v, const kt_heads *o,
+                                  const float *lse, const kt_heads *dq,
+                                  const kt_heads *dk, const kt_heads *dv,
+                                  void *ws, int64_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

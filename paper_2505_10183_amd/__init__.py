@@ -20,4 +20,5 @@ def __getattr__(name):
 
 
 _OPERATORS = ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_layernorm_bwd_workspace", "kt_act8_shapes", "kt_act8_save", "kt_act8_restore",
-              "kt_act8_weight_grad", "kt_act8_weight_grad_workspace")
+              "kt_act8_weight_grad", "kt_act8_weight_grad_workspace",
+              "kt_attention_fwd", "kt_attention_bwd", "kt_attention_bwd_workspace")

@@ -235,3 +235,175 @@ extern "C" kt_status kt_act8_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t toke
     KT_TRY(apart(who, outs[1], outs[0]));
     return launched(who, kt_launch_weight_grad(dt, gdt, tokens, (int)out, (int)in, dy, lddy, q, e, dw, lddw, (float *)ws, stream));
 }
+
+// ---- attention -------------------------------------------------------------------
+
+namespace {
+
+const int64_t MOST_TOKENS = 1 << 30, MOST_HEADS = 1 << 16, MOST_STRIDE = 1ll << 40;
+
+// A tensor of heads in memory; strides in bytes.
+struct Spread {
+    const char *name;
+    const void *p;
+    int64_t n[3], stride[3], dim;       // batch, tokens, heads
+};
+Spread spread(const char *name, const kt_heads *h, const kt_attention *a, int64_t tokens, int64_t heads)
+{
+    const int64_t s = size_of(a->dt);
+    return Spread{name, h->data, {a->batch, tokens, heads}, {h->batch * s, h->token * s, h->head * s}, a->dim * s};
+}
+bool empty(const Spread &t) { return t.n[0] < 1 || t.n[1] < 1 || t.n[2] < 1; }
+uintptr_t begin(const Spread &t) { return reinterpret_cast<uintptr_t>(t.p); }
+// Bytes that the dimensions with strides below `ld` span; -1 where one of the others is no multiple of it.
+int64_t extent(const Spread &t, int64_t ld)
+{
+    int64_t e = t.dim;
+    for (int i = 0; i < 3; ++i) {
+        if (t.n[i] < 2) continue;
+        if (t.stride[i] < ld) e += (t.n[i] - 1) * t.stride[i];
+        else if (t.stride[i] % ld) return -1;
+    }
+    return e;
+}
+// Whether two tensors provably share no byte: one ends before the other begins, or both are windows of one buffer that lie side
+// by side within a token, a head or a sequence.
+bool apart(const Spread &a, const Spread &b)
+{
+    if (empty(a) || empty(b)) return true;
+    if (begin(a) + (uintptr_t)extent(a, INT64_MAX) <= begin(b) || begin(b) + (uintptr_t)extent(b, INT64_MAX) <= begin(a)) return true;
+    for (int i = 0; i < 3; ++i) {
+        const int64_t ld = a.stride[i];
+        if (ld < 1) continue;
+        const int64_t ea = extent(a, ld), eb = extent(b, ld);
+        if (ea < 0 || eb < 0 || ea > ld || eb > ld) continue;
+        const int64_t d = begin(b) >= begin(a) ? (int64_t)((begin(b) - begin(a)) % (uintptr_t)ld)
+                                               : (ld - (int64_t)((begin(a) - begin(b)) % (uintptr_t)ld)) % ld;
+        if (d >= ea && d + eb <= ld) return true;
+    }
+    return false;
+}
+// Whether no two elements of an output share an address: in order of their strides, each dimension steps over those below.
+bool distinct(const Spread &t)
+{
+    int order[3] = {0, 1, 2};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (t.stride[order[j]] < t.stride[order[i]]) { const int x = order[i]; order[i] = order[j]; order[j] = x; }
+    int64_t below = t.dim;
+    for (int i : order) {
+        if (t.n[i] < 2) continue;
+        if (t.stride[i] < below) return false;
+        below += (t.n[i] - 1) * t.stride[i];
+    }
+    return true;
+}
+
+kt_status attention_sizes(const char *who, const kt_attention *a)
+{
+    if (!a) return bad(who, "NULL sizes");
+    if (!is_type(a->dt)) return bad(who, "unknown element type");
+    if (a->batch < 0 || a->nq < 0 || a->nk < 0 || a->heads < 1 || a->kv_heads < 1 || a->dim < 1) return bad(who, "negative sizes, or no heads or dim");
+    if (a->heads % a->kv_heads) return bad(who, "kv_heads does not divide heads");
+    if (!(a->scale > 0.0f) || std::isinf(a->scale)) return bad(who, "scale must be finite and > 0");
+    if (a->dim > KT_ATTENTION_MAX_DIM) return unsupported(who, "dim over KT_ATTENTION_MAX_DIM");
+    if (a->nq > MOST_TOKENS || a->nk > MOST_TOKENS || a->heads > MOST_HEADS || a->batch > MOST_TOKENS)
+        return unsupported(who, "more than 2^30 queries, keys or sequences, or 2^16 heads");
+    const int64_t most = a->nq > a->nk ? a->nq : a->nk;
+    if (a->batch * a->heads > INT32_MAX / (most / 128 + 1)) return unsupported(who, "more than 2^31 workgroups");
+    return aligned(who, "k_lens", a->k_lens, 4);
+}
+
+kt_status heads_tensor(const char *who, const char *name, const kt_heads *h, const kt_attention *a, int64_t tokens, int64_t heads,
+                       bool out)
+{
+    const bool none = a->batch == 0 || tokens == 0;
+    if (!h || (!h->data && !none)) {
+        kt_set_error("%s: NULL %s", who, name);
+        return KT_EINVAL;
+    }
+    if (none) return KT_OK;
+    if (h->batch < 0 || h->token < 0 || h->head < 0 || h->batch > MOST_STRIDE || h->token > MOST_STRIDE || h->head > MOST_STRIDE) {
+        kt_set_error("%s: strides of %s are negative or over 2^40", who, name);
+        return KT_EINVAL;
+    }
+    const int64_t room = INT64_MAX / 8;         // of a span in bytes
+    if ((a->batch > 1 && h->batch > room / 4 / a->batch) || (tokens > 1 && h->token > room / 4 / tokens)) {
+        kt_set_error("%s: %s spans more than 2^60 bytes", who, name);
+        return KT_EINVAL;
+    }
+    const kt_status st = aligned(who, name, h->data, size_of(a->dt));
+    if (st != KT_OK) return st;
+    if (out && !distinct(spread(name, h, a, tokens, heads))) {
+        kt_set_error("%s: elements of %s share addresses", who, name);
+        return KT_EINVAL;
+    }
+    return KT_OK;
+}
+
+kt_status all_apart(const char *who, const Spread *outs, int no, const Spread *ins, int ni)
+{
+    for (int i = 0; i < no; ++i) {
+        for (int j = 0; j < ni; ++j)
+            if (!apart(outs[i], ins[j])) { kt_set_error("%s: %s overlaps %s", who, outs[i].name, ins[j].name); return KT_EINVAL; }
+        for (int j = 0; j < i; ++j)
+            if (!apart(outs[i], outs[j])) { kt_set_error("%s: %s overlaps %s", who, outs[i].name, outs[j].name); return KT_EINVAL; }
+    }
+    return KT_OK;
+}
+
+}  // namespace
+
+extern "C" kt_status kt_attention_fwd(const kt_attention *a, const kt_heads *q, const kt_heads *k, const kt_heads *v,
+                                      const kt_heads *o, float *lse, void *stream)
+{
+    const char *who = "kt_attention_fwd";
+    KT_TRY(attention_sizes(who, a));
+    KT_TRY(heads_tensor(who, "q", q, a, a->nq, a->heads, false));
+    KT_TRY(heads_tensor(who, "k", k, a, a->nk, a->kv_heads, false));
+    KT_TRY(heads_tensor(who, "v", v, a, a->nk, a->kv_heads, false));
+    KT_TRY(heads_tensor(who, "o", o, a, a->nq, a->heads, true));
+    KT_TRY(aligned(who, "lse", lse, 4));
+    if (a->batch == 0 || a->nq == 0) return KT_OK;
+    const int64_t stats = a->batch * a->heads * a->nq * 4;
+    const Spread outs[] = {spread("o", o, a, a->nq, a->heads), Spread{"lse", lse, {lse ? 1 : 0, 1, 1}, {0, 0, 0}, stats}};
+    const Spread ins[] = {spread("q", q, a, a->nq, a->heads), spread("k", k, a, a->nk, a->kv_heads), spread("v", v, a, a->nk, a->kv_heads),
+                          Spread{"k_lens", a->k_lens, {a->k_lens ? 1 : 0, 1, 1}, {0, 0, 0}, a->batch * 4}};
+    KT_TRY(all_apart(who, outs, 2, ins, 4));
+    return launched(who, kt_launch_attention_fwd(a, q, k, v, o, lse, stream));
+}
+
+extern "C" int64_t kt_attention_bwd_workspace(const kt_attention *a)
+{
+    return attention_sizes("kt_attention_bwd_workspace", a) == KT_OK ? kt_attention_bwd_ws(a) : 0;
+}
+
+extern "C" kt_status kt_attention_bwd(const kt_attention *a, const kt_heads *d_o, const kt_heads *q, const kt_heads *k,
+                                      const kt_heads *v, const kt_heads *o, const float *lse, const kt_heads *dq,
+                                      const kt_heads *dk, const kt_heads *dv, void *ws, int64_t ws_bytes, void *stream)
+{
+    const char *who = "kt_attention_bwd";
+    KT_TRY(attention_sizes(who, a));
+    KT_TRY(heads_tensor(who, "d_o", d_o, a, a->nq, a->heads, false));
+    KT_TRY(heads_tensor(who, "q", q, a, a->nq, a->heads, false));
+    KT_TRY(heads_tensor(who, "k", k, a, a->nk, a->kv_heads, false));
+    KT_TRY(heads_tensor(who, "v", v, a, a->nk, a->kv_heads, false));
+    KT_TRY(heads_tensor(who, "o", o, a, a->nq, a->heads, false));
+    KT_TRY(heads_tensor(who, "dq", dq, a, a->nq, a->heads, true));
+    KT_TRY(heads_tensor(who, "dk", dk, a, a->nk, a->kv_heads, true));
+    KT_TRY(heads_tensor(who, "dv", dv, a, a->nk, a->kv_heads, true));
+    if (a->batch == 0) return KT_OK;
+    const int64_t stats = a->batch * a->heads * a->nq * 4, need = kt_attention_bwd_ws(a);
+    if (!lse && stats) return bad(who, "NULL lse");
+    KT_TRY(aligned(who, "lse", lse, 4));
+    if (need && (!ws || ws_bytes < need)) return bad(who, "the workspace is smaller than kt_attention_bwd_workspace says");
+    KT_TRY(aligned(who, "ws", ws, 16));
+    const Spread outs[] = {spread("dq", dq, a, a->nq, a->heads), spread("dk", dk, a, a->nk, a->kv_heads), spread("dv", dv, a, a->nk, a->kv_heads),
+                           Spread{"ws", ws, {need ? 1 : 0, 1, 1}, {0, 0, 0}, need}};
+    const Spread ins[] = {spread("d_o", d_o, a, a->nq, a->heads), spread("q", q, a, a->nq, a->heads), spread("k", k, a, a->nk, a->kv_heads),
+                          spread("v", v, a, a->nk, a->kv_heads), spread("o", o, a, a->nq, a->heads),
+                          Spread{"lse", lse, {stats ? 1 : 0, 1, 1}, {0, 0, 0}, stats},
+                          Spread{"k_lens", a->k_lens, {a->k_lens ? 1 : 0, 1, 1}, {0, 0, 0}, a->batch * 4}};
+    KT_TRY(all_apart(who, outs, 4, ins, 7));
+    return launched(who, kt_launch_attention_bwd(a, d_o, q, k, v, o, lse, dq, dk, dv, (float *)ws, stream));
+}

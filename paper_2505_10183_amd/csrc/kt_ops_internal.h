@@ -28,4 +28,11 @@ int64_t kt_weight_grad_ws(kt_dtype dt, int64_t tokens, int64_t out, int64_t in);
 int kt_launch_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t tokens, int out, int in, const void *dy, int64_t lddy,
                           const int8_t *q, const uint8_t *e, void *dw, int64_t lddw, float *ws, void *stream);
 
+int64_t kt_attention_bwd_ws(const kt_attention *a);
+int kt_launch_attention_fwd(const kt_attention *a, const kt_heads *q, const kt_heads *k, const kt_heads *v, const kt_heads *o,
+                            float *lse, void *stream);
+int kt_launch_attention_bwd(const kt_attention *a, const kt_heads *d_o, const kt_heads *q, const kt_heads *k, const kt_heads *v,
+                            const kt_heads *o, const float *lse, const kt_heads *dq, const kt_heads *dk, const kt_heads *dv,
+                            float *ws, void *stream);
+
 #endif

@@ -20,6 +20,16 @@ _lib = None         # the library that the prototypes below were given to
 ACT8_GROUP = 32
 
 
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class _Attention(ctypes.Structure):
+    _fields_ = [("dt", ctypes.c_int), ("batch", ctypes.c_int64), ("nq", ctypes.c_int64), ("nk", ctypes.c_int64),
+                ("heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("dim", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("causal", ctypes.c_int), ("k_lens", ctypes.c_void_p)]
+
+
 def _library() -> ctypes.CDLL:
     global _lib
     L = binding.lib()
@@ -34,7 +44,13 @@ def _library() -> ctypes.CDLL:
         L.kt_act8_weight_grad_workspace.argtypes = [i32, i64, i64, i64]
         L.kt_act8_weight_grad_workspace.restype = i64
         L.kt_act8_weight_grad.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp]
-        for n in ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore", "kt_act8_weight_grad"):
+        hp, ap = ctypes.POINTER(_Heads), ctypes.POINTER(_Attention)
+        L.kt_attention_fwd.argtypes = [ap, hp, hp, hp, hp, vp, vp]
+        L.kt_attention_bwd_workspace.argtypes = [ap]
+        L.kt_attention_bwd_workspace.restype = i64
+        L.kt_attention_bwd.argtypes = [ap, hp, hp, hp, hp, hp, vp, hp, hp, hp, vp, i64, vp]
+        for n in ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore", "kt_act8_weight_grad",
+                  "kt_attention_fwd", "kt_attention_bwd"):
             getattr(L, n).restype = i32
         _lib = L
     return L
@@ -192,5 +208,59 @@ def kt_act8_weight_grad(dy, q, e, dw, workspace=None, stream=None):
     pq, pe = _act8(q, e, tokens, inn, "checkpoint")
     ws, size, held = _workspace(workspace, L.kt_act8_weight_grad_workspace(t, tokens, out, inn), stream, dy.device)
     status = L.kt_act8_weight_grad(t, _type(dw, "dw"), tokens, out, inn, p, ld, pq, pe, pw, ldw, ws, size, _stream(stream))
+    if status:
+        _check(status, L)
+
+
+def _heads(x, shape, dtype, what: str) -> _Heads:
+    _on_gpu(x, what)
+    if x.dtype != dtype or x.shape != shape:
+        raise ValueError("%s: %s of %s is needed, got %s of %s" % (what, list(shape), dtype, list(x.shape), x.dtype))
+    b, t, h, d = x.stride()
+    if d != 1 and shape[3] > 1:
+        raise ValueError("%s: adjacent elements of a head are needed, got stride %d" % (what, d))
+    return _Heads(x.data_ptr(), b, t, h)
+
+
+def _attention(q, k, causal, scale, k_lens) -> Tuple[_Attention, tuple, tuple]:
+    """The sizes, and the shapes of the query and the key side."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k: [batch, tokens, heads, dim] is needed")
+    batch, nq, heads, dim = q.shape
+    qs, ks = q.shape, torch.Size((batch, k.shape[1], k.shape[2], dim))
+    lens = _vector(k_lens, batch, torch.int32, "k_lens")
+    return _Attention(_type(q, "q"), batch, nq, k.shape[1], heads, k.shape[2], dim, dim ** -0.5 if scale is None else scale,
+                      1 if causal else 0, lens), qs, ks
+
+
+def kt_attention_fwd(q, k, v, o, lse=None, causal: bool = False, scale: Optional[float] = None, k_lens=None, stream=None):
+    """o = softmax(scale q k^T) v; all tensors [batch, tokens, heads, dim] with adjacent elements of a head and any strides else,
+    k and v with a divisor of q's heads.  lse [batch, heads, queries] (float32): what the backward pass needs.  scale: None =
+    1 / sqrt(dim).  causal: the last query sees the last key.  k_lens [batch] (int32): keys of each sequence, on the GPU."""
+    L = _library()
+    a, qs, ks = _attention(q, k, causal, scale, k_lens)
+    t = q.dtype
+    status = L.kt_attention_fwd(a, _heads(q, qs, t, "q"), _heads(k, ks, t, "k"), _heads(v, ks, t, "v"), _heads(o, qs, t, "o"),
+                                _vector(lse, qs[0] * qs[1] * qs[2], torch.float32, "lse"), _stream(stream))
+    if status:
+        _check(status, L)
+
+
+def kt_attention_bwd_workspace(q, k) -> int:
+    a, _, _ = _attention(q, k, False, None, None)
+    return _library().kt_attention_bwd_workspace(a)
+
+
+def kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal: bool = False, scale: Optional[float] = None, k_lens=None,
+                     workspace=None, stream=None):
+    """Gradients of q, k and v from that of o; o and lse are what kt_attention_fwd left for the same arguments.  dq, dk and dv may
+    be views of one buffer, as q, k and v may."""
+    L = _library()
+    a, qs, ks = _attention(q, k, causal, scale, k_lens)
+    t = q.dtype
+    ws, size, held = _workspace(workspace, L.kt_attention_bwd_workspace(a), stream, q.device)
+    status = L.kt_attention_bwd(a, _heads(do, qs, t, "do"), _heads(q, qs, t, "q"), _heads(k, ks, t, "k"), _heads(v, ks, t, "v"),
+                                _heads(o, qs, t, "o"), _vector(lse, qs[0] * qs[1] * qs[2], torch.float32, "lse"),
+                                _heads(dq, qs, t, "dq"), _heads(dk, ks, t, "dk"), _heads(dv, ks, t, "dv"), ws, size, _stream(stream))
     if status:
         _check(status, L)

@@ -108,6 +108,91 @@ def test_weight_grad_refuses(changes, status, word):
     call("kt_act8_weight_grad", WEIGHT_GRAD, status, word, **changes)
 
 
+def attention(name, status, word, tensors=(), **changes):
+    """kt_attention_fwd or _bwd refused; sizes changed by name, tensors by (name, data or None, batch, token, head)."""
+    L = ops._library()
+    a = dict(dt=BF16, batch=2, nq=16, nk=16, heads=4, kv_heads=2, dim=64, scale=0.125, causal=1, k_lens=at(20))
+    a.update({k: v for k, v in changes.items() if k in a})
+    names = ["q", "k", "v", "o"] if name == "kt_attention_fwd" else ["d_o", "q", "k", "v", "o", "dq", "dk", "dv"]
+    h = {n: ops._Heads(at(i), 16 * 4 * 64, 4 * 64, 64) for i, n in enumerate(names)}
+    for n, *f in tensors:
+        h[n] = None if f[0] is None else ops._Heads(*f)
+    more = dict(lse=at(10), ws=at(11), ws_bytes=M)
+    more.update({k: v for k, v in changes.items() if k in more})
+    sizes = ops._Attention(*a.values())
+    if name == "kt_attention_fwd":
+        got = L.kt_attention_fwd(sizes, *h.values(), more["lse"], 0)
+    else:
+        got = L.kt_attention_bwd(sizes, *(h[n] for n in names[:5]), more["lse"], *(h[n] for n in names[5:]), more["ws"], more["ws_bytes"], 0)
+    text = L.kt_last_error().decode()
+    assert got == status and name in text and word in text, (got, changes, tensors, text)
+
+
+@pytest.mark.parametrize("name", ["kt_attention_fwd", "kt_attention_bwd"])
+def test_attention_refuses(name):
+    I = EINVAL
+    s = (16 * 4 * 64, 4 * 64, 64)
+    for changes, status, word in [
+            (dict(dt=2), I, "type"), (dict(batch=-1), I, "negative"), (dict(nq=-1), I, "negative"), (dict(nk=-1), I, "negative"),
+            (dict(heads=0), I, "heads"), (dict(kv_heads=0), I, "heads"), (dict(dim=0), I, "dim"), (dict(kv_heads=3), I, "divide"),
+            (dict(scale=0.0), I, "scale"), (dict(scale=-1.0), I, "scale"), (dict(scale=math.nan), I, "scale"), (dict(scale=math.inf), I, "scale"),
+            (dict(dim=129), EUNSUPPORTED, "dim"), (dict(nk=(1 << 30) + 1), EUNSUPPORTED, "2^30"), (dict(nq=(1 << 30) + 1), EUNSUPPORTED, "2^30"),
+            (dict(heads=1 << 17, kv_heads=1), EUNSUPPORTED, "heads"), (dict(batch=1 << 30), EUNSUPPORTED, "workgroups"),
+            (dict(k_lens=at(20) + 2), EALIGN, "k_lens"), (dict(lse=at(10) + 2), EALIGN, "lse")]:
+        attention(name, status, word, **changes)
+    for n in ["q", "k", "v", "o"] + ([] if name == "kt_attention_fwd" else ["d_o", "dq", "dk", "dv"]):
+        attention(name, I, "NULL " + n, [(n, None)])
+        attention(name, I, "NULL " + n, [(n, 0, *s)])
+        attention(name, EALIGN, n, [(n, at(15) + 1, *s)])
+        attention(name, I, "strides of " + n, [(n, at(15), -1, s[1], s[2])])
+        attention(name, I, "strides of " + n, [(n, at(15), s[0], (1 << 40) + 1, s[2])])
+    for n in ["o"] if name == "kt_attention_fwd" else ["dq", "dk", "dv"]:
+        attention(name, I, "share", [(n, at(15), 0, s[1], s[2])])
+        attention(name, I, "share", [(n, at(15), s[0], s[1], 0)])
+        attention(name, I, "share", [(n, at(15), s[0], s[1], 63)])
+        attention(name, I, "share", [(n, at(15), s[0], 127, 64)])
+        attention(name, I, "overlaps", [(n, at(1), *s)])
+        attention(name, I, "overlaps", [(n, at(1) + 2 * (16 * 4 * 64 + 5), *s)])
+        attention(name, I, n + " overlaps k_lens", [(n, at(20), *s)])
+    if name == "kt_attention_fwd":
+        attention(name, I, "lse overlaps q", lse=at(0))
+    else:
+        attention(name, I, "NULL lse", lse=0)
+        attention(name, I, "workspace", ws=0)
+        attention(name, I, "workspace", ws_bytes=2 * 4 * 16 * 4 - 1)
+        attention(name, EALIGN, "ws", ws=at(11) + 4)
+        attention(name, I, "ws overlaps", ws=at(2))
+        attention(name, I, "dq overlaps lse", [("dq", at(10), *s)])
+
+
+def test_attention_windows_of_one_buffer():
+    """dq, dk and dv side by side in a token, in [batch, 3, heads, tokens, dim] or in one allocation after another pass; a window that
+    reaches into its neighbour is refused.  (Those that pass are refused for their workspace only.)"""
+    name, row = "kt_attention_bwd", (4 + 2 + 2) * 64
+    def token(n, start, by=0):
+        return (n, at(30) + 2 * (64 * start + by), 16 * row, row, 64)
+    three = [token("dq", 0), token("dk", 4), token("dv", 6)]
+    attention(name, EINVAL, "workspace", three, ws=0)
+    attention(name, EINVAL, "overlaps", [token("dq", 0, 1)] + three[1:])
+    attention(name, EINVAL, "overlaps", three[:2] + [token("dv", 5)])
+    attention(name, EINVAL, "overlaps", three[:2] + [token("dv", 6, 1)])
+    size = 16 * 64
+    def plane(n, start, by=0):
+        return (n, at(30) + 2 * (size * start + by), 8 * size, 64, size)
+    three = [plane("dq", 0), plane("dk", 4), plane("dv", 6)]
+    attention(name, EINVAL, "workspace", three, ws=0)
+    attention(name, EINVAL, "overlaps", three[:1] + [plane("dk", 4, -1)] + three[2:])
+
+
+def test_attention_does_nothing_for_no_sequences():
+    L = ops._library()
+    none = ops._Heads(0, 0, 0, 0)
+    a = ops._Attention(BF16, 0, 16, 16, 4, 2, 64, 0.125, 0, 0)
+    assert L.kt_attention_fwd(a, none, none, none, none, 0, 0) == 0
+    assert L.kt_attention_bwd(a, none, none, none, none, none, 0, none, none, none, 0, 0, 0) == 0
+    assert L.kt_attention_bwd_workspace(a) == 0
+
+
 def test_weight_grad_workspace():
     for args in [(torch.float32, -1, 4, 4), (torch.float32, 4, 0, 4), (torch.bfloat16, 4, 4, 0), (torch.float32, 1, 64, 64)]:
         assert kt.kt_act8_weight_grad_workspace(*args) == 0
@@ -150,11 +235,14 @@ def test_act8_shapes():
 def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
     x, g, v = torch.zeros(4, 64), torch.zeros(64), torch.zeros(4)
     q, e = torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4, 2, dtype=torch.uint8)
+    h = torch.zeros(1, 4, 1, 64)
     for f in (lambda: kt.kt_layernorm_fwd(x, g, g, 1e-5, x, v, v),
               lambda: kt.kt_layernorm_bwd(x, x, g, v, v, x, g, g),
               lambda: kt.kt_act8_save(x, q, e),
               lambda: kt.kt_act8_restore(q, e, x),
-              lambda: kt.kt_act8_weight_grad(x, q, e, x)):
+              lambda: kt.kt_act8_weight_grad(x, q, e, x),
+              lambda: kt.kt_attention_fwd(h, h, h, h),
+              lambda: kt.kt_attention_bwd(h, h, h, h, h, v, h, h, h)):
         if torch.cuda.is_available():
             with pytest.raises(ValueError, match="current GPU"):
                 f()
