@@ -39,40 +39,133 @@ template <typename T> struct Args {
     __device__ __forceinline__ int keys(int b) const { return k_lens ? max(0, min(nk, k_lens[b])) : nk; }
 };
 
-// Fragment c of a row in memory: elements 16 c + 8 h .. + 7, zeros at and past dim and for rows that are not there.
-template <typename T> __device__ __forceinline__ typename Frag<T>::type row_frag(const T *row, bool there, int c, int dim)
+// A wavefront's 32 rows from row0 on, one per lane and half, as fragments along them: fragment c is elements 16 c + 8 h .. + 7;
+// zeros at and past dim and for rows at and past `end`, which are not read.  DMA (see Feed): through a buffer that ends there, without
+// a branch, so that all loads of a workgroup's start are on their way together.
+template <typename T, int D, bool DMA>
+__device__ __forceinline__ void row_frags(typename Frag<T>::type (&f)[D / 16], const T *p, int64_t stride, int row0, int end, int dim)
 {
-    const int d = 16 * c + 8 * ((threadIdx.x & 63) >> 5);
-    if constexpr (sizeof(T) == 2) {
-        return __builtin_bit_cast(bf16x8, there ? ld_chunk(row, d, dim) : u32x4{0, 0, 0, 0});
-    } else {
-        const u32x4 lo = there ? ld_chunk(row, d, dim) : u32x4{0, 0, 0, 0};
-        const u32x4 hi = there ? ld_chunk(row, d + 4, dim) : u32x4{0, 0, 0, 0};
-        return __builtin_shufflevector(__builtin_bit_cast(f32x4, lo), __builtin_bit_cast(f32x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+    const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
+    constexpr int PARTS = 8 / VE<T>;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        u32x4 v[PARTS];
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+            const int d = 16 * c + 8 * h + k * VE<T>;
+            if constexpr (DMA) {
+#ifdef __HIP_DEVICE_COMPILE__           // the host pass knows neither the type nor the builtins
+                const int rows = min(32, end - row0);
+                const int bytes = rows > 0 ? ((rows - 1) * (int)stride + dim) * (int)sizeof(T) : 0;
+                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(p + row0 * stride), 0, bytes, 0x00020000);
+                v[k] = __builtin_amdgcn_raw_buffer_load_b128(rs, d < dim ? (row * (int)stride + d) * (int)sizeof(T) : INT32_MIN, 0, 0);
+#endif
+            } else {
+                v[k] = row0 + row < end ? ld_chunk(p + (row0 + row) * stride, d, dim) : u32x4{0, 0, 0, 0};
+            }
+        }
+        if constexpr (PARTS == 1) {
+            f[c] = __builtin_bit_cast(typename Frag<T>::type, v[0]);
+        } else {
+            f[c] = __builtin_shufflevector(__builtin_bit_cast(f32x4, v[0]), __builtin_bit_cast(f32x4, v[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
     }
 }
 
-// A tile of ROWS rows on its way from memory to LDS; rows at and past `end` are zeros and are not read.
-template <typename T, int D> struct Stage {
-    static constexpr int V = VE<T>, N = ROWS<T> * D / V / BLOCK;
-    u32x4 r[N];
-    __device__ __forceinline__ void load(const T *p, int64_t stride, int row0, int end, int dim)
+// The wavefront's number, known to be the same in all of its lanes: what follows from it are scalars and scalar branches.
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+
+// Tiles of R rows on their way from memory to LDS; rows at and past `end` are zeros and are not read.
+// DMA: the loads write LDS themselves, 16 bytes a lane, without a register: lane l of an instruction writes the l-th 16 bytes of
+// a KiB, so the exchange of chunks (Tile) is made on the side of the addresses.  The buffer's size ends at the last row, which
+// makes zeros of what lies past it; columns past dim are sent there too.  It needs rows at multiples of 16 bytes and offsets
+// within a tile of 31 bits; other tensors pass through registers.
+template <typename T, int D, int R, bool DMA> struct Feed {
+    static constexpr int V = VE<T>, N = R * D / V / BLOCK;
+    static_assert(N >= 1, "a tile has a chunk for every lane");
+    const T *p;
+    int64_t stride;
+    int end, dim;
+    u32x4 r[DMA ? 1 : N];
+    int at[DMA ? N : 1];
+
+    __device__ __forceinline__ Feed(const T *p_, int64_t stride_, int end_, int dim_) : p(p_), stride(stride_), end(end_), dim(dim_)
     {
+        if constexpr (DMA) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int n = threadIdx.x + u * BLOCK, row = row0 + n / (D / V);
-            r[u] = row < end ? ld_chunk(p + row * stride, n % (D / V) * V, dim) : u32x4{0, 0, 0, 0};
+            for (int u = 0; u < N; ++u) {
+                const int n = threadIdx.x + u * BLOCK, row = n / (D / V), c = (n % (D / V) ^ Tile<T, D>::swizzle(row)) * V;
+                at[u] = c < dim ? row * (int)stride * (int)sizeof(T) + c * (int)sizeof(T) : INT32_MIN;
+            }
         }
     }
-    __device__ __forceinline__ void store(char *tile) const
+    // In assembly: of the builtin the compiler only knows that it writes LDS some time, and waits for it before the next read of
+    // any tile.  The instruction has no output register and reads its operands when it is issued; arrived() waits for it.  s_nop: m0
+    // and a descriptor that the vector unit has just written need up to 5 cycles before a memory instruction reads them.  m0 cannot
+    // be named as overwritten (it is reserved); nothing else in these kernels uses it.
+    __device__ __forceinline__ void bring(const T *from, int bytes, char *tile) const
     {
+        const uint64_t base = (uint64_t)from;
+        const u32x4 rs{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+        const uint32_t to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int n = threadIdx.x + u * BLOCK;
-            *(u32x4 *)(tile + Tile<T, D>::at(n / (D / V), n % (D / V))) = r[u];
+        for (int u = 0; u < N; ++u)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :: "s"(to + u * BLOCK * 16), "v"(at[u]), "s"(rs) : "memory");
+    }
+    // Starts bringing the rows from row0 on into `tile`; they are there after finish() and a barrier.
+    __device__ __forceinline__ void start(char *tile, int row0)
+    {
+        if constexpr (DMA) {
+            const int rows = min(R, end - row0);
+            const int bytes = rows > 0 ? ((rows - 1) * (int)stride + dim) * (int)sizeof(T) : 0;
+            bring(p + row0 * stride, bytes, tile);
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int n = threadIdx.x + u * BLOCK, row = row0 + n / (D / V);
+                r[u] = row < end ? ld_chunk(p + row * stride, n % (D / V) * V, dim) : u32x4{0, 0, 0, 0};
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(char *tile) const
+    {
+        if constexpr (!DMA) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int n = threadIdx.x + u * BLOCK;
+                *(u32x4 *)(tile + Tile<T, D>::at(n / (D / V), n % (D / V))) = r[u];
+            }
         }
     }
 };
+// Before the barrier behind which a tile is read: what this wavefront brings has arrived.
+__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }       // vmcnt(0)
+
+// N products one after another.  Product i takes the fragment that load(i) reads from LDS; reads run AHEAD products before
+// their use, and what use(i, fragment) computes beside its product stays beside it: nothing moves across a step.  Left to itself the
+// compiler reads each fragment right before its product, and puts all vector work between the products.
+template <typename T, int AHEAD, typename L, typename U, int... I>
+__device__ __forceinline__ void stream(L load, U use, std::integer_sequence<int, I...>)
+{
+    constexpr int N = sizeof...(I);
+    typename Frag<T>::type f[AHEAD];
+    auto first = [&](auto i) {
+        if constexpr (i < AHEAD) f[i] = load(i);
+    };
+    auto step = [&](auto i) {
+        use(i, f[i % AHEAD]);
+        if constexpr (i + AHEAD < N) f[i % AHEAD] = load(std::integral_constant<int, i + AHEAD>());
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    (first(std::integral_constant<int, I>()), ...);
+    __builtin_amdgcn_sched_barrier(0);
+    (step(std::integral_constant<int, I>()), ...);
+}
+template <typename T, int AHEAD, int N, typename L, typename U> __device__ __forceinline__ void stream(L load, U use)
+{
+    stream<T, AHEAD>(load, use, std::make_integer_sequence<int, N>());
+}
 
 __device__ __forceinline__ float other_half(float x)
 {
@@ -109,103 +202,131 @@ template <typename T, int D> __device__ __forceinline__ void store_row(T *row, c
         }
 }
 
-// Rows of OWN and head of a workgroup.  The last rows come first: under a causal mask they have the most keys, and the short ones
-// fill the end of the launch.
+// Rows of OWN and head of a workgroup.  The last rows of all heads come first: under a causal mask they have the most keys, and the
+// short ones fill the end of the launch.  (Head by head on each XCD, so that its L2 holds a head's keys: the long blocks of the last
+// heads end late; 8 x 2048 causal, 16 heads of 128: dk and dv 370 -> 427 us.)
 struct Place {
     int row0, b, h;
 };
 __device__ __forceinline__ Place place(int blocks, int heads)
 {
-    const int bh = blockIdx.x % (gridDim.x / blocks), n = blockIdx.x / (gridDim.x / blocks);
+    const int per = gridDim.x / blocks, bh = blockIdx.x % per, n = blockIdx.x / per;
     return Place{(blocks - 1 - n) * OWN, bh / heads, bh % heads};
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(BLOCK, 2) void kt_attention_fwd_kernel(Args<T> a, int blocks)
+template <typename T, int D, bool DMA>
+__global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_attention_fwd_kernel(Args<T> a, int blocks)
 {
-    constexpr int R = ROWS<T>, KB = R / 32;
+    constexpr int R = ROWS<T>, KB = R / 32, BYTES = Tile<T, D>::bytes(R);
     typedef typename Frag<T>::type F;
-    __shared__ __align__(16) char kt[Tile<T, D>::bytes(R)], vt[Tile<T, D>::bytes(R)];
+    __shared__ __align__(16) char kt0[BYTES], vt0[BYTES], kt1[BYTES], vt1[BYTES];
     const Place at = place(blocks, a.heads);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, hk = at.h / (a.heads / a.kv_heads);
+    const int lane = threadIdx.x & 63, wave = wave_id(), hk = at.h / (a.heads / a.kv_heads);
     const int q = at.row0 + wave * 32 + (lane & 31), off = a.nk - a.nq, len = a.keys(at.b);
     const bool there = q < a.nq;
     // keys [0, mine) are seen by this lane's query, [0, all) by some query of the workgroup
     const int mine = there ? (a.causal ? min(len, max(0, q + off + 1)) : len) : 0;
     const int all = a.causal ? min(len, max(0, min(a.nq, at.row0 + OWN) + off)) : len;
-    const T *kp = a.k.at(at.b, hk), *vp = a.v.at(at.b, hk), *qp = a.q.at(at.b, at.h) + q * a.q.token;
+    const T *kp = a.k.at(at.b, hk), *vp = a.v.at(at.b, hk);
     F qf[D / 16];
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) qf[c] = row_frag(qp, there, c, a.dim);
+    row_frags<T, D, DMA>(qf, a.q.at(at.b, at.h), a.q.token, at.row0 + wave * 32, a.nq, a.dim);
     f32x16 o[D / 32];
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[db] = f32x16{0};
     const float c2 = a.scale * LOG2E;
     float m = NEVER, mc = 0.0f, l = 0.0f;         // maximum that the sums refer to, m * c2, and the sum of this half's keys
-    // the fewest and the most keys that a query of this wavefront sees: tiles below the first need no mask
-    const int first = at.row0 + wave * 32, least = a.causal ? min(len, max(0, first + off + 1)) : len;
+    // tiles below seen_by_all need no mask; a wavefront's queries see nothing from `most` on
+    const int first = at.row0 + wave * 32, seen_by_all = a.causal ? min(len, max(0, at.row0 + off + 1)) : len;
     const int most = first >= a.nq ? 0 : a.causal ? min(len, max(0, min(a.nq, first + 32) + off)) : len;
 
-    Stage<T, D> ks, vs;
-    ks.load(kp, a.k.token, 0, all, a.dim);
-    vs.load(vp, a.v.token, 0, all, a.dim);
-    for (int k0 = 0; k0 < all; k0 += R) {
-        ks.store(kt);
-        vs.store(vt);
-        __syncthreads();
-        if (k0 + R < all) {
-            ks.load(kp, a.k.token, k0 + R, all, a.dim);
-            vs.load(vp, a.v.token, k0 + R, all, a.dim);
+    Feed<T, D, R, DMA> ks(kp, a.k.token, all, a.dim), vs(vp, a.v.token, all, a.dim);
+    auto step = [&](auto edge, int k0, const char *kt, const char *vt, char *ktn, char *vtn) {
+        const bool more = k0 + R < all;
+        if (more) {
+            ks.start(ktn, k0 + R);
+            vs.start(vtn, k0 + R);
         }
-        if (k0 < most) {
+        if (!edge || k0 < most) {
+            constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;
+            constexpr int NS = KB * D / 16, NO = D / 16;            // products of the scores; of a block of 32 keys with v
             f32x16 s[KB];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                s[kb] = f32x16{0};
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) mma(s[kb], load_r<T, D>(kt, 32 * kb, c), qf[c]);
-            }
-            if (k0 + R > least) {
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[kb][r] = k0 + 32 * kb + row_of(r) < mine ? s[kb][r] : NEVER;
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
-            top = fmaxf(top, other_half(top));
-            // the reference moves only when a query's maximum has outgrown it by 2^8: probabilities up to 256 lose nothing
-            // in floating point, and the sums are seldom multiplied
-            if (__any((top - m) * c2 > 8.0f)) {
-                const float next = fmaxf(m, top), by = m == NEVER ? 0.0f : __builtin_amdgcn_exp2f((m - next) * c2);
-                m = next;
-                mc = m == NEVER ? 0.0f : m * c2;
-                l *= by;
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db) o[db] *= by;
-            }
             F pf[KB][2];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
+            for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{0};
+            auto weigh = [&](int kb, int r) {           // a score becomes a probability
+                s[kb][r] = __builtin_amdgcn_exp2f(__fmaf_rn(s[kb][r], c2, -mc));
+                l += s[kb][r];
+                if (r % 8 == 7) pf[kb][r / 8] = frag_of<T>(s[kb], r / 8);
+            };
+            auto load = [&](auto n0) -> F {
+                constexpr int n = n0;
+                if constexpr (n < NS) return load_r<T, D>(kt, 32 * (n % KB), n / KB);
+                constexpr int i = n - NS;
+                return load_t<T, D>(vt, 2 * (i / NO) + i % NO / (D / 32), 32 * (i % (D / 32)));
+            };
+            stream<T, AHEAD, NS + KB * NO>(load, [&](auto n0, const F &f) {
+                constexpr int n = n0;
+                if constexpr (n == NS) {
+                    if constexpr (edge) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[kb][r] = __builtin_amdgcn_exp2f(__fmaf_rn(s[kb][r], c2, -mc));
-                    l += s[kb][r];
+                        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) s[kb][r] = k0 + 32 * kb + row_of(r) < mine ? s[kb][r] : NEVER;
+                    }
+                    float top = s[0][0];
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
+                    top = fmaxf(top, other_half(top));
+                    // the reference moves only when a query's maximum has outgrown it by 2^8: probabilities up to 256 lose
+                    // nothing in floating point, and the sums are seldom multiplied
+                    if (__any((top - m) * c2 > 8.0f)) {
+                        const float next = fmaxf(m, top), by = m == NEVER ? 0.0f : __builtin_amdgcn_exp2f((m - next) * c2);
+                        m = next;
+                        mc = m == NEVER ? 0.0f : m * c2;
+                        l *= by;
+#pragma unroll
+                        for (int db = 0; db < D / 32; ++db) o[db] *= by;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) weigh(0, r);
                 }
-                pf[kb][0] = frag_of<T>(s[kb], 0);
-                pf[kb][1] = frag_of<T>(s[kb], 1);
-            }
+                if constexpr (n < NS) {
+                    mma(s[n % KB], f, qf[n / KB]);
+                } else {
+                    constexpr int i = n - NS;
+                    mma(o[i % (D / 32)], f, pf[i / NO][i % NO / (D / 32)]);
+                    if constexpr (KB > 1 && i < NO) {       // the second block's beside the first block's products
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int db = 0; db < D / 32; ++db) mma(o[db], load_t<T, D>(vt, 2 * kb + c, 32 * db), pf[kb][c]);
+                        for (int k = 0; k < 16 / NO; ++k) weigh(1, i * (16 / NO) + k);
+                    }
+                }
+            });
         }
+        if (more) {
+            ks.finish(ktn);
+            vs.finish(vtn);
+        }
+        arrived();
         __syncthreads();
+    };
+    if (all > 0) {
+        ks.start(kt0, 0);
+        vs.start(vt0, 0);
+        ks.finish(kt0);
+        vs.finish(vt0);
+    }
+    arrived();
+    __syncthreads();
+    int k0 = 0;
+    for (; k0 + 2 * R <= seen_by_all; k0 += 2 * R) {
+        step(std::false_type(), k0, kt0, vt0, kt1, vt1);
+        step(std::false_type(), k0 + R, kt1, vt1, kt0, vt0);
+    }
+    for (; k0 < all; k0 += 2 * R) {
+        step(std::true_type(), k0, kt0, vt0, kt1, vt1);
+        if (k0 + R < all) step(std::true_type(), k0 + R, kt1, vt1, kt0, vt0);
     }
     if (!there) return;
     l += other_half(l);
@@ -216,38 +337,38 @@ __global__ __launch_bounds__(BLOCK, 2) void kt_attention_fwd_kernel(Args<T> a, i
 // What exp2 subtracts from the scaled score of a query, from its log-sum-exp; a query without keys gets probability 0 for all.
 __device__ __forceinline__ float reference(float lse) { return lse == NEVER ? -NEVER : lse * LOG2E; }
 
-template <typename T, int D>
+template <typename T, int D, bool DMA>
 __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_attention_dq_kernel(Args<T> a, int blocks)
 {
-    constexpr int R = ROWS<T>, KB = R / 32;
+    constexpr int R = ROWS<T>, KB = R / 32, BYTES = Tile<T, D>::bytes(R);
     typedef typename Frag<T>::type F;
-    __shared__ __align__(16) char kt[Tile<T, D>::bytes(R)], vt[Tile<T, D>::bytes(R)];
+    __shared__ __align__(16) char kt0[BYTES], vt0[BYTES], kt1[BYTES], vt1[BYTES];
     const Place at = place(blocks, a.heads);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, hk = at.h / (a.heads / a.kv_heads);
+    const int lane = threadIdx.x & 63, wave = wave_id(), hk = at.h / (a.heads / a.kv_heads);
     const int q = at.row0 + wave * 32 + (lane & 31), off = a.nk - a.nq, len = a.keys(at.b);
     const bool there = q < a.nq;
     const int mine = there ? (a.causal ? min(len, max(0, q + off + 1)) : len) : 0;
     const int all = a.causal ? min(len, max(0, min(a.nq, at.row0 + OWN) + off)) : len;
-    const int first = at.row0 + wave * 32, least = a.causal ? min(len, max(0, first + off + 1)) : len;
+    const int first = at.row0 + wave * 32, seen_by_all = a.causal ? min(len, max(0, at.row0 + off + 1)) : len;
     const int most = first >= a.nq ? 0 : a.causal ? min(len, max(0, min(a.nq, first + 32) + off)) : len;
     const T *kp = a.k.at(at.b, hk), *vp = a.v.at(at.b, hk);
-    Stage<T, D> ks, vs;
-    ks.load(kp, a.k.token, 0, all, a.dim);
-    vs.load(vp, a.v.token, 0, all, a.dim);
+    Feed<T, D, R, DMA> ks(kp, a.k.token, all, a.dim), vs(vp, a.v.token, all, a.dim);
+    if (all > 0) {
+        ks.start(kt0, 0);
+        vs.start(vt0, 0);
+    }
 
     F qf[D / 16], df[D / 16];
     float delta = 0.0f;
     {
-        const T *qp = a.q.at(at.b, at.h) + q * a.q.token, *dp = a.d_o.at(at.b, at.h) + q * a.d_o.token;
-        const T *op = a.o.at(at.b, at.h) + q * a.o.token;
+        F of[D / 16];
+        row_frags<T, D, DMA>(qf, a.q.at(at.b, at.h), a.q.token, first, a.nq, a.dim);
+        row_frags<T, D, DMA>(df, a.d_o.at(at.b, at.h), a.d_o.token, first, a.nq, a.dim);
+        row_frags<T, D, DMA>(of, a.o.at(at.b, at.h), a.o.token, first, a.nq, a.dim);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            qf[c] = row_frag(qp, there, c, a.dim);
-            df[c] = row_frag(dp, there, c, a.dim);
-            const F of = row_frag(op, there, c, a.dim);
+        for (int c = 0; c < D / 16; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) delta = __fmaf_rn((float)df[c][j], (float)of[j], delta);
-        }
+            for (int j = 0; j < 8; ++j) delta = __fmaf_rn((float)df[c][j], (float)of[c][j], delta);
         delta += other_half(delta);
     }
     const int64_t stat = ((int64_t)at.b * a.heads + at.h) * a.nq + q;
@@ -257,137 +378,202 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) dq[db] = f32x16{0};
 
-    for (int k0 = 0; k0 < all; k0 += R) {
-        ks.store(kt);
-        vs.store(vt);
-        __syncthreads();
-        if (k0 + R < all) {
-            ks.load(kp, a.k.token, k0 + R, all, a.dim);
-            vs.load(vp, a.v.token, k0 + R, all, a.dim);
+    auto step = [&](auto edge, int k0, const char *kt, const char *vt, char *ktn, char *vtn) {
+        const bool more = k0 + R < all;
+        if (more) {
+            ks.start(ktn, k0 + R);
+            vs.start(vtn, k0 + R);
         }
-        if (k0 < most) {
-            const bool edge = k0 + R > least;
+        if (!edge || k0 < most) {
+            constexpr int AHEAD = sizeof(T) == 2 ? 6 : 2;
+            constexpr int NS = 2 * D / 16, NO = D / 16;             // products of a block of 32 keys: s and dp; dq
+            f32x16 s, dp;
+            F sf[2];
+            auto load = [&](auto n0) -> F {
+                constexpr int n = n0, kb = n / (NS + NO), i = n % (NS + NO);
+                if constexpr (i < NS) return load_r<T, D>(i % 2 ? vt : kt, 32 * kb, i / 2);
+                else return load_t<T, D>(kt, 2 * kb + (i - NS) / (D / 32), 32 * ((i - NS) % (D / 32)));
+            };
+            stream<T, AHEAD, KB * (NS + NO)>(load, [&](auto n0, const F &f) {
+                constexpr int n = n0, kb = n / (NS + NO), i = n % (NS + NO);
+                if constexpr (i == 0) s = dp = f32x16{0};
+                if constexpr (i == NS) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                f32x16 s{0}, dp{0};
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    mma(s, load_r<T, D>(kt, 32 * kb, c), qf[c]);
-                    mma(dp, load_r<T, D>(vt, 32 * kb, c), df[c]);
+                    for (int r = 0; r < 16; ++r) {
+                        const float p = __builtin_amdgcn_exp2f(__fmaf_rn(s[r], c2, -ref));
+                        s[r] = p * (dp[r] - delta);
+                        if constexpr (edge) s[r] = k0 + 32 * kb + row_of(r) < mine ? s[r] : 0.0f;
+                    }
+                    sf[0] = frag_of<T>(s, 0);
+                    sf[1] = frag_of<T>(s, 1);
                 }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(__fmaf_rn(s[r], c2, -ref));
-                    s[r] = p * (dp[r] - delta);
+                if constexpr (i < NS) {
+                    if constexpr (i % 2) mma(dp, f, df[i / 2]);
+                    else mma(s, f, qf[i / 2]);
+                } else {
+                    mma(dq[(i - NS) % (D / 32)], f, sf[(i - NS) / (D / 32)]);
                 }
-                if (edge) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = k0 + 32 * kb + row_of(r) < mine ? s[r] : 0.0f;
-                }
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const F f = frag_of<T>(s, c);
-#pragma unroll
-                    for (int db = 0; db < D / 32; ++db) mma(dq[db], load_t<T, D>(kt, 2 * kb + c, 32 * db), f);
-                }
-            }
+            });
         }
+        if (more) {
+            ks.finish(ktn);
+            vs.finish(vtn);
+        }
+        arrived();
         __syncthreads();
+    };
+    if (all > 0) {
+        ks.finish(kt0);
+        vs.finish(vt0);
+    }
+    arrived();
+    __syncthreads();
+    int k0 = 0;
+    for (; k0 + 2 * R <= seen_by_all; k0 += 2 * R) {
+        step(std::false_type(), k0, kt0, vt0, kt1, vt1);
+        step(std::false_type(), k0 + R, kt1, vt1, kt0, vt0);
+    }
+    for (; k0 < all; k0 += 2 * R) {
+        step(std::true_type(), k0, kt0, vt0, kt1, vt1);
+        if (k0 + R < all) step(std::true_type(), k0 + R, kt1, vt1, kt0, vt0);
     }
     if (there) store_row<T, D>(a.dq.at(at.b, at.h) + q * a.dq.token, dq, a.scale, a.dim);
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_attention_dkv_kernel(Args<T> a, int blocks)
+template <typename T, int D, bool DMA>
+__global__ __launch_bounds__(BLOCK, 1) void kt_attention_dkv_kernel(Args<T> a, int blocks)
 {
-    constexpr int R = ROWS<T>, QB = R / 32;
+    constexpr int R = ROWS<T>, QB = R / 32, BYTES = Tile<T, D>::bytes(R);
     typedef typename Frag<T>::type F;
-    __shared__ __align__(16) char qt[Tile<T, D>::bytes(R)], dt[Tile<T, D>::bytes(R)];
-    __shared__ __align__(16) float refs[R], deltas[R];
-    const int bh = blockIdx.x % (gridDim.x / blocks), k0 = blockIdx.x / (gridDim.x / blocks) * OWN;
+    __shared__ __align__(16) char qt0[BYTES], dt0[BYTES], qt1[BYTES], dt1[BYTES];
+    __shared__ __align__(16) float stat0[2 * R], stat1[2 * R];
+    const int per = gridDim.x / blocks, bh = blockIdx.x % per, k0 = blockIdx.x / per * OWN;     // the first keys have the most queries
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads, group = a.heads / a.kv_heads;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, off = a.nk - a.nq, len = a.keys(b);
+    const int lane = threadIdx.x & 63, wave = wave_id(), off = a.nk - a.nq, len = a.keys(b);
     const int first = k0 + wave * 32, key = first + (lane & 31);
     const bool there = key < len;                   // seen by some query; others get gradient 0 (key < nk)
     F kf[D / 16], vf[D / 16];
-    {
-        const T *kp = a.k.at(b, hk) + key * a.k.token, *vp = a.v.at(b, hk) + key * a.v.token;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            kf[c] = row_frag(kp, there, c, a.dim);
-            vf[c] = row_frag(vp, there, c, a.dim);
-        }
-    }
+    row_frags<T, D, DMA>(kf, a.k.at(b, hk), a.k.token, first, len, a.dim);
+    row_frags<T, D, DMA>(vf, a.v.at(b, hk), a.v.token, first, len, a.dim);
     f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{0};
     const float c2 = a.scale * LOG2E;
-    // queries [from, nq) see a key of the workgroup; of this wavefront, those from `mine0` on, all of its keys those from `full` on
+    // queries [from, nq) see a key of the workgroup, those from `mine0` on one of this wavefront; those from `full` on see all keys of
+    // the workgroup, and their tiles need no mask.  A head's tiles are taken in pairs: an odd one more is all zeros.
     const int from = k0 >= len ? a.nq : a.causal ? max(0, k0 - off) / R * R : 0;
     const int mine0 = first >= len ? a.nq : a.causal ? max(0, first - off) : 0;
-    const int full = first + 32 > len ? a.nq : a.causal ? max(0, first + 31 - off) : 0;
     const int mine = a.causal ? key - off : 0;      // first query that sees this lane's key
+    const int full = k0 + OWN > len ? a.nq : a.causal ? max(0, k0 + OWN - 1 - off) : 0;
+    const int upto = from + (a.nq - from + 2 * R - 1) / (2 * R) * (2 * R);
+    const int mid = from + (max(0, full - from) + 2 * R - 1) / (2 * R) * (2 * R);
 
-    Stage<T, D> qs, ds;
-    float sref, sdelta;
-    const int64_t stats = ((int64_t)b * a.heads + hk * group) * a.nq;
-    auto load = [&](int g, int q0) {
-        const int h = hk * group + g;
-        qs.load(a.q.at(b, h), a.q.token, q0, a.nq, a.dim);
-        ds.load(a.d_o.at(b, h), a.d_o.token, q0, a.nq, a.dim);
-        if (threadIdx.x < R) {
-            const bool ok = q0 + (int)threadIdx.x < a.nq;
-            const int64_t i = stats + (int64_t)g * a.nq + q0 + threadIdx.x;
-            sref = ok ? reference(a.lse[i]) : -NEVER;
-            sdelta = ok ? a.delta[i] : 0.0f;
+    Feed<T, D, R, DMA> qs(a.q.at(b, hk * group), a.q.token, a.nq, a.dim), ds(a.d_o.at(b, hk * group), a.d_o.token, a.nq, a.dim);
+    float stat;
+    const float *stats = threadIdx.x < R ? a.lse : a.delta;
+    stats += ((int64_t)b * a.heads + hk * group) * a.nq;
+    auto start = [&](int q0, char *qt, char *dt) {
+        qs.start(qt, q0);
+        ds.start(dt, q0);
+        if (threadIdx.x < 2 * R) {
+            const int q = q0 + threadIdx.x % R;
+            stat = q < a.nq ? stats[q] : threadIdx.x < R ? NEVER : 0.0f;
         }
     };
+    auto finish = [&](char *qt, char *dt, float *st) {
+        qs.finish(qt);
+        ds.finish(dt);
+        if (threadIdx.x < 2 * R) st[threadIdx.x] = threadIdx.x < R ? reference(stat) : stat;
+    };
     int g = 0, q0 = from;
-    if (q0 < a.nq) load(g, q0);
-    while (q0 < a.nq) {
-        qs.store(qt);
-        ds.store(dt);
-        if (threadIdx.x < R) { refs[threadIdx.x] = sref; deltas[threadIdx.x] = sdelta; }
-        __syncthreads();
-        int ng = g, nq0 = q0 + R;
-        if (nq0 >= a.nq && g + 1 < group) { ng = g + 1; nq0 = from; }
-        if (nq0 < a.nq) load(ng, nq0);
-        if (q0 + R > mine0) {
-            const bool edge = q0 < full;
+    auto step = [&](auto edge, const char *qt, const char *dt, const float *refs, char *qtn, char *dtn, float *refsn) {
+        const float *deltas = refs + R;
+        int nq0 = q0 + R;
+        if (nq0 >= upto && g + 1 < group) {         // the next head that shares these keys
+            ++g;
+            nq0 = from;
+            qs.p += a.q.head;
+            ds.p += a.d_o.head;
+            stats += a.nq;
+        }
+        const bool more = nq0 < upto;
+        if (more) start(nq0, qtn, dtn);
+        if (!edge || q0 + R > mine0) {
+            constexpr int AHEAD = sizeof(T) == 2 ? 6 : 2;
+            constexpr int NS = 2 * D / 16, NO = 4 * D / 32;         // products of a block of 32 queries: s and dp; dv and dk
+            f32x16 s[QB], dp[QB];
+            f32x4 ref[QB][4], delta[QB][4];
+            F pf[QB][2], sf[QB][2];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
-                f32x16 s{0}, dp{0};
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    mma(s, load_r<T, D>(qt, 32 * qb, c), kf[c]);
-                    mma(dp, load_r<T, D>(dt, 32 * qb, c), vf[c]);
-                }
-                f32x16 p;
+                s[qb] = dp[qb] = f32x16{0};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f32x4 ref = *(const f32x4 *)(refs + 32 * qb + row_of(4 * i)), delta = *(const f32x4 *)(deltas + 32 * qb + row_of(4 * i));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int r = 4 * i + j;
-                        p[r] = __builtin_amdgcn_exp2f(__fmaf_rn(s[r], c2, -ref[j]));
-                        if (edge) p[r] = there && q0 + 32 * qb + row_of(r) >= mine ? p[r] : 0.0f;
-                        s[r] = p[r] * (dp[r] - delta[j]);
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const F pf = frag_of<T>(p, c), sf = frag_of<T>(s, c);
-#pragma unroll
-                    for (int db = 0; db < D / 32; ++db) {
-                        mma(dv[db], load_t<T, D>(dt, 2 * qb + c, 32 * db), pf);
-                        mma(dk[db], load_t<T, D>(qt, 2 * qb + c, 32 * db), sf);
-                    }
+                    ref[qb][i] = *(const f32x4 *)(refs + 32 * qb + row_of(4 * i));
+                    delta[qb][i] = *(const f32x4 *)(deltas + 32 * qb + row_of(4 * i));
                 }
             }
+            auto weigh = [&](int qb, int r) {
+                float p = __builtin_amdgcn_exp2f(__fmaf_rn(s[qb][r], c2, -ref[qb][r / 4][r % 4]));
+                if constexpr (edge) p = there && q0 + 32 * qb + row_of(r) >= mine ? p : 0.0f;
+                dp[qb][r] = p * (dp[qb][r] - delta[qb][r / 4][r % 4]);
+                s[qb][r] = p;
+                if (r % 8 == 7) {
+                    pf[qb][r / 8] = frag_of<T>(s[qb], r / 8);
+                    sf[qb][r / 8] = frag_of<T>(dp[qb], r / 8);
+                }
+            };
+            auto load = [&](auto n0) -> F {
+                constexpr int n = n0;
+                if constexpr (n < QB * NS) return load_r<T, D>(n % 2 ? dt : qt, 32 * (n / NS), n % NS / 2);
+                constexpr int i = n - QB * NS;
+                return load_t<T, D>(i % 2 ? qt : dt, 2 * (i / NO) + i % NO / (NO / 2), 32 * (i / 2 % (D / 32)));
+            };
+            stream<T, AHEAD, QB * (NS + NO)>(load, [&](auto n0, const F &f) {
+                constexpr int n = n0;
+                if constexpr (QB == 1 && n == NS) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) weigh(0, r);
+                }
+                if constexpr (n < QB * NS) {
+                    constexpr int qb = n / NS;
+                    if constexpr (n % 2) mma(dp[qb], f, vf[n % NS / 2]);
+                    else mma(s[qb], f, kf[n % NS / 2]);
+                    if constexpr (qb == 1) {                // the first block's beside the second block's products
+#pragma unroll
+                        for (int k = 0; k < 16 / NS; ++k) weigh(0, n % NS * (16 / NS) + k);
+                    }
+                } else {
+                    constexpr int i = n - QB * NS, qb = i / NO, c = i % NO / (NO / 2), db = i / 2 % (D / 32);
+                    if constexpr (i % 2) mma(dk[db], f, sf[qb][c]);
+                    else mma(dv[db], f, pf[qb][c]);
+                    if constexpr (QB > 1 && i < NO) {
+#pragma unroll
+                        for (int k = 0; k < 16 / NO; ++k) weigh(1, i * (16 / NO) + k);
+                    }
+                }
+            });
         }
+        if (more) finish(qtn, dtn, refsn);
+        arrived();
         __syncthreads();
-        g = ng;
         q0 = nq0;
+    };
+    if (q0 < a.nq) {
+        start(q0, qt0, dt0);
+        finish(qt0, dt0, stat0);
+    }
+    arrived();
+    __syncthreads();
+    while (q0 < upto) {
+        while (q0 < mid && q0 < upto) {             // of the last head q0 ends at upto, of the others at from again
+            step(std::true_type(), qt0, dt0, stat0, qt1, dt1, stat1);
+            step(std::true_type(), qt1, dt1, stat1, qt0, dt0, stat0);
+        }
+        while (q0 >= mid && q0 < upto) {
+            step(std::false_type(), qt0, dt0, stat0, qt1, dt1, stat1);
+            step(std::false_type(), qt1, dt1, stat1, qt0, dt0, stat0);
+        }
     }
     if (key < a.nk) {
         store_row<T, D>(a.dk.at(b, hk) + key * a.dk.token, dk, a.scale, a.dim);
@@ -414,23 +600,31 @@ template <typename T> Args<T> args(const kt_attention *a)
     return r;
 }
 
-template <typename T, int D> int fwd(const kt_attention *a, const Args<T> &r, hipStream_t s)
+// Whether tiles of these rows can be brought by DMA (Feed).
+template <typename T> bool dma(const View<T> &v, int dim)
+{
+    const int64_t to = 16 / sizeof(T);
+    return reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.batch % to == 0 && v.token % to == 0 && v.head % to == 0 && dim % to == 0 &&
+           v.token * (int64_t)sizeof(T) < (1 << 24);
+}
+
+template <typename T, int D, bool DMA> int fwd(const kt_attention *a, const Args<T> &r, hipStream_t s)
 {
     const int blocks = (r.nq + OWN - 1) / OWN;
-    kt_attention_fwd_kernel<T, D><<<(unsigned)(a->batch * a->heads * blocks), BLOCK, 0, s>>>(r, blocks);
+    kt_attention_fwd_kernel<T, D, DMA><<<(unsigned)(a->batch * a->heads * blocks), BLOCK, 0, s>>>(r, blocks);
     return (int)hipGetLastError();
 }
 
-template <typename T, int D> int bwd(const kt_attention *a, const Args<T> &r, hipStream_t s)
+template <typename T, int D, bool DMA> int bwd(const kt_attention *a, const Args<T> &r, hipStream_t s)
 {
     const int qb = (r.nq + OWN - 1) / OWN, kb = (r.nk + OWN - 1) / OWN;
     if (qb) {
-        kt_attention_dq_kernel<T, D><<<(unsigned)(a->batch * a->heads * qb), BLOCK, 0, s>>>(r, qb);
+        kt_attention_dq_kernel<T, D, DMA><<<(unsigned)(a->batch * a->heads * qb), BLOCK, 0, s>>>(r, qb);
         const int e = (int)hipGetLastError();
         if (e) return e;
     }
     if (!kb) return 0;
-    kt_attention_dkv_kernel<T, D><<<(unsigned)(a->batch * a->kv_heads * kb), BLOCK, 0, s>>>(r, kb);
+    kt_attention_dkv_kernel<T, D, DMA><<<(unsigned)(a->batch * a->kv_heads * kb), BLOCK, 0, s>>>(r, kb);
     return (int)hipGetLastError();
 }
 
@@ -443,7 +637,8 @@ int forward(const kt_attention *a, const kt_heads *q, const kt_heads *k, const k
     r.v = view<T>(v);
     r.o = view<T>(o);
     r.lse = lse;
-    return r.dim <= 64 ? fwd<T, 64>(a, r, s) : fwd<T, 128>(a, r, s);
+    if (dma(r.q, r.dim) && dma(r.k, r.dim) && dma(r.v, r.dim)) return r.dim <= 64 ? fwd<T, 64, true>(a, r, s) : fwd<T, 128, true>(a, r, s);
+    return r.dim <= 64 ? fwd<T, 64, false>(a, r, s) : fwd<T, 128, false>(a, r, s);
 }
 
 template <typename T>
@@ -461,7 +656,9 @@ int backward(const kt_attention *a, const kt_heads *d_o, const kt_heads *q, cons
     r.dv = view<T>(dv);
     r.lse = const_cast<float *>(lse);
     r.delta = ws;
-    return r.dim <= 64 ? bwd<T, 64>(a, r, s) : bwd<T, 128>(a, r, s);
+    if (dma(r.q, r.dim) && dma(r.k, r.dim) && dma(r.v, r.dim) && dma(r.o, r.dim) && dma(r.d_o, r.dim))
+        return r.dim <= 64 ? bwd<T, 64, true>(a, r, s) : bwd<T, 128, true>(a, r, s);
+    return r.dim <= 64 ? bwd<T, 64, false>(a, r, s) : bwd<T, 128, false>(a, r, s);
 }
 
 }  // namespace
