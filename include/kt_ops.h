@@ -108,7 +108,7 @@ KT_API kt_status kt_act8_restore(kt_dtype dt, int64_t rows, int64_t cols,
  *   ws   kt_act8_weight_grad_workspace(...) bytes.
  * bf16 dy: products of bf16 pairs, exact, summed in binary32.  f32 dy: binary32
  * products and sums.  lddw >= in: dw may be a window of a larger matrix.  out
- * and in are at most 2^30.
+ * and in are at most 2^24, tokens at most 2^40.
  */
 KT_API int64_t kt_act8_weight_grad_workspace(kt_dtype dt, int64_t tokens,
                                              int64_t out, int64_t in);

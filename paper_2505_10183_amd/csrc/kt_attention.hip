@@ -54,12 +54,9 @@ __device__ __forceinline__ void row_frags(typename Frag<T>::type (&f)[D / 16], c
         for (int k = 0; k < PARTS; ++k) {
             const int d = 16 * c + 8 * h + k * VE<T>;
             if constexpr (DMA) {
-#ifdef __HIP_DEVICE_COMPILE__           // the host pass knows neither the type nor the builtins
                 const int rows = min(32, end - row0);
                 const int bytes = rows > 0 ? ((rows - 1) * (int)stride + dim) * (int)sizeof(T) : 0;
-                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(p + row0 * stride), 0, bytes, 0x00020000);
-                v[k] = __builtin_amdgcn_raw_buffer_load_b128(rs, d < dim ? (row * (int)stride + d) * (int)sizeof(T) : INT32_MIN, 0, 0);
-#endif
+                v[k] = buffer16(p + row0 * stride, bytes, d < dim ? (row * (int)stride + d) * (int)sizeof(T) : INT32_MIN);
             } else {
                 v[k] = row0 + row < end ? ld_chunk(p + (row0 + row) * stride, d, dim) : u32x4{0, 0, 0, 0};
             }
@@ -71,76 +68,6 @@ __device__ __forceinline__ void row_frags(typename Frag<T>::type (&f)[D / 16], c
         }
     }
 }
-
-// The wavefront's number, known to be the same in all of its lanes: what follows from it are scalars and scalar branches.
-__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
-
-// Tiles of R rows on their way from memory to LDS; rows at and past `end` are zeros and are not read.
-// DMA: the loads write LDS themselves, 16 bytes a lane, without a register: lane l of an instruction writes the l-th 16 bytes of
-// a KiB, so the exchange of chunks (Tile) is made on the side of the addresses.  The buffer's size ends at the last row, which
-// makes zeros of what lies past it; columns past dim are sent there too.  It needs rows at multiples of 16 bytes and offsets
-// within a tile of 31 bits; other tensors pass through registers.
-template <typename T, int D, int R, bool DMA> struct Feed {
-    static constexpr int V = VE<T>, N = R * D / V / BLOCK;
-    static_assert(N >= 1, "a tile has a chunk for every lane");
-    const T *p;
-    int64_t stride;
-    int end, dim;
-    u32x4 r[DMA ? 1 : N];
-    int at[DMA ? N : 1];
-
-    __device__ __forceinline__ Feed(const T *p_, int64_t stride_, int end_, int dim_) : p(p_), stride(stride_), end(end_), dim(dim_)
-    {
-        if constexpr (DMA) {
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int n = threadIdx.x + u * BLOCK, row = n / (D / V), c = (n % (D / V) ^ Tile<T, D>::swizzle(row)) * V;
-                at[u] = c < dim ? row * (int)stride * (int)sizeof(T) + c * (int)sizeof(T) : INT32_MIN;
-            }
-        }
-    }
-    // In assembly: of the builtin the compiler only knows that it writes LDS some time, and waits for it before the next read of
-    // any tile.  The instruction has no output register and reads its operands when it is issued; arrived() waits for it.  s_nop: m0
-    // and a descriptor that the vector unit has just written need up to 5 cycles before a memory instruction reads them.  m0 cannot
-    // be named as overwritten (it is reserved); nothing else in these kernels uses it.
-    __device__ __forceinline__ void bring(const T *from, int bytes, char *tile) const
-    {
-        const uint64_t base = (uint64_t)from;
-        const u32x4 rs{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
-        const uint32_t to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
-#pragma unroll
-        for (int u = 0; u < N; ++u)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                         :: "s"(to + u * BLOCK * 16), "v"(at[u]), "s"(rs) : "memory");
-    }
-    // Starts bringing the rows from row0 on into `tile`; they are there after finish() and a barrier.
-    __device__ __forceinline__ void start(char *tile, int row0)
-    {
-        if constexpr (DMA) {
-            const int rows = min(R, end - row0);
-            const int bytes = rows > 0 ? ((rows - 1) * (int)stride + dim) * (int)sizeof(T) : 0;
-            bring(p + row0 * stride, bytes, tile);
-        } else {
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int n = threadIdx.x + u * BLOCK, row = row0 + n / (D / V);
-                r[u] = row < end ? ld_chunk(p + row * stride, n % (D / V) * V, dim) : u32x4{0, 0, 0, 0};
-            }
-        }
-    }
-    __device__ __forceinline__ void finish(char *tile) const
-    {
-        if constexpr (!DMA) {
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int n = threadIdx.x + u * BLOCK;
-                *(u32x4 *)(tile + Tile<T, D>::at(n / (D / V), n % (D / V))) = r[u];
-            }
-        }
-    }
-};
-// Before the barrier behind which a tile is read: what this wavefront brings has arrived.
-__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }       // vmcnt(0)
 
 // N products one after another.  Product i takes the fragment that load(i) reads from LDS; reads run AHEAD products before
 // their use, and what use(i, fragment) computes beside its product stays beside it: nothing moves across a step.  Left to itself the
@@ -239,7 +166,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
     const int first = at.row0 + wave * 32, seen_by_all = a.causal ? min(len, max(0, at.row0 + off + 1)) : len;
     const int most = first >= a.nq ? 0 : a.causal ? min(len, max(0, min(a.nq, first + 32) + off)) : len;
 
-    Feed<T, D, R, DMA> ks(kp, a.k.token, all, a.dim), vs(vp, a.v.token, all, a.dim);
+    Feed<T, D, R, BLOCK, DMA> ks(kp, a.k.token, all, a.dim), vs(vp, a.v.token, all, a.dim);
     auto step = [&](auto edge, int k0, const char *kt, const char *vt, char *ktn, char *vtn) {
         const bool more = k0 + R < all;
         if (more) {
@@ -352,7 +279,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
     const int first = at.row0 + wave * 32, seen_by_all = a.causal ? min(len, max(0, at.row0 + off + 1)) : len;
     const int most = first >= a.nq ? 0 : a.causal ? min(len, max(0, min(a.nq, first + 32) + off)) : len;
     const T *kp = a.k.at(at.b, hk), *vp = a.v.at(at.b, hk);
-    Feed<T, D, R, DMA> ks(kp, a.k.token, all, a.dim), vs(vp, a.v.token, all, a.dim);
+    Feed<T, D, R, BLOCK, DMA> ks(kp, a.k.token, all, a.dim), vs(vp, a.v.token, all, a.dim);
     if (all > 0) {
         ks.start(kt0, 0);
         vs.start(vt0, 0);
@@ -468,7 +395,7 @@ __global__ __launch_bounds__(BLOCK, 1) void kt_attention_dkv_kernel(Args<T> a, i
     const int upto = from + (a.nq - from + 2 * R - 1) / (2 * R) * (2 * R);
     const int mid = from + (max(0, full - from) + 2 * R - 1) / (2 * R) * (2 * R);
 
-    Feed<T, D, R, DMA> qs(a.q.at(b, hk * group), a.q.token, a.nq, a.dim), ds(a.d_o.at(b, hk * group), a.d_o.token, a.nq, a.dim);
+    Feed<T, D, R, BLOCK, DMA> qs(a.q.at(b, hk * group), a.q.token, a.nq, a.dim), ds(a.d_o.at(b, hk * group), a.d_o.token, a.nq, a.dim);
     float stat;
     const float *stats = threadIdx.x < R ? a.lse : a.delta;
     stats += ((int64_t)b * a.heads + hk * group) * a.nq;

@@ -9,6 +9,9 @@
 #ifndef KT_MFMA_H
 #define KT_MFMA_H
 
+#include <type_traits>
+#include <utility>
+
 #include "kt_ops_device.h"
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -19,6 +22,16 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define KT_LDS __attribute__((address_space(3)))
 
 namespace {
+
+// f(A), f(A + 1), ... f(B - 1), the numbers known to the compiler.
+template <int A, typename F, int... I> __device__ __forceinline__ void span_of(F f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, A + I>()), ...);
+}
+template <int A, int B, typename F> __device__ __forceinline__ void span(F f)
+{
+    if constexpr (A < B) span_of<A>(f, std::make_integer_sequence<int, B - A>());
+}
 
 template <typename T> struct Frag;
 template <> struct Frag<bf16> { typedef bf16x8 type; };
@@ -109,6 +122,99 @@ __device__ __forceinline__ typename Frag<T>::type load_t(const char *tile, int c
         }
         return v;
     }
+}
+
+// The wavefront's number, known to be the same in all of its lanes: what follows from it are scalars and scalar branches.
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+
+// 16 bytes, or one byte, at `at` of a buffer of `bytes` bytes; zeros where it ends before.
+__device__ __forceinline__ u32x4 buffer16([[maybe_unused]] const void *p, [[maybe_unused]] int bytes, [[maybe_unused]] int at)
+{
+#ifdef __HIP_DEVICE_COMPILE__           // the host pass knows neither the type nor the builtins
+    return __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000), at, 0, 0);
+#else
+    return u32x4{0, 0, 0, 0};
+#endif
+}
+__device__ __forceinline__ uint32_t buffer1([[maybe_unused]] const void *p, [[maybe_unused]] int bytes, [[maybe_unused]] int at)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    return __builtin_amdgcn_raw_buffer_load_b8(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000), at, 0, 0);
+#else
+    return 0;
+#endif
+}
+
+// Tiles of R rows of D elements on their way from memory to LDS, brought by BLOCK lanes; rows at and past `end` are zeros and are not read.
+// DMA: the loads write LDS themselves, 16 bytes a lane, without a register: lane l of an instruction writes the l-th 16 bytes of
+// a KiB, so the exchange of chunks (Tile) is made on the side of the addresses.  The buffer's size ends at the last row, which
+// makes zeros of what lies past it; columns past dim are sent there too.  It needs rows at multiples of 16 bytes and offsets
+// within a tile of 31 bits; other tensors pass through registers.
+template <typename T, int D, int R, int BLOCK, bool DMA> struct Feed {
+    static constexpr int V = VE<T>, N = R * D / V / BLOCK;
+    static_assert(N >= 1, "a tile has a chunk for every lane");
+    const T *p;
+    int64_t stride;
+    int end, dim;
+    u32x4 r[DMA ? 1 : N];
+    int at[DMA ? N : 1];
+
+    __device__ __forceinline__ Feed(const T *p_, int64_t stride_, int end_, int dim_) : p(p_), stride(stride_), end(end_), dim(dim_)
+    {
+        if constexpr (DMA) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int n = threadIdx.x + u * BLOCK, row = n / (D / V), c = (n % (D / V) ^ Tile<T, D>::swizzle(row)) * V;
+                at[u] = c < dim ? row * (int)stride * (int)sizeof(T) + c * (int)sizeof(T) : INT32_MIN;
+            }
+        }
+    }
+    // In assembly: of the builtin the compiler only knows that it writes LDS some time, and waits for it before the next read of
+    // any tile.  The instruction has no output register and reads its operands when it is issued; arrived() waits for it.  s_nop: m0
+    // and a descriptor that the vector unit has just written need up to 5 cycles before a memory instruction reads them.  m0 cannot
+    // be named as overwritten (it is reserved); nothing else in these kernels uses it.
+    __device__ __forceinline__ void bring(const T *from, int bytes, char *tile) const
+    {
+        const uint64_t base = (uint64_t)from;
+        const u32x4 rs{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+        const uint32_t to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :: "s"(to + u * BLOCK * 16), "v"(at[u]), "s"(rs) : "memory");
+    }
+    // Starts bringing the rows from row0 on into `tile`; they are there after finish() and a barrier.
+    __device__ __forceinline__ void start(char *tile, int row0)
+    {
+        if constexpr (DMA) {
+            const int rows = min(R, end - row0);
+            const int bytes = rows > 0 ? ((rows - 1) * (int)stride + dim) * (int)sizeof(T) : 0;
+            bring(p + row0 * stride, bytes, tile);
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int n = threadIdx.x + u * BLOCK, row = row0 + n / (D / V);
+                r[u] = row < end ? ld_chunk(p + row * stride, n % (D / V) * V, dim) : u32x4{0, 0, 0, 0};
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(char *tile) const
+    {
+        if constexpr (!DMA) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int n = threadIdx.x + u * BLOCK;
+                *(u32x4 *)(tile + Tile<T, D>::at(n / (D / V), n % (D / V))) = r[u];
+            }
+        }
+    }
+};
+// Before the barrier behind which a tile is read: what this wavefront brings has arrived.
+// LATER: loads started after it that may still be on their way.
+template <int LATER = 0> __device__ __forceinline__ void arrived()
+{
+    static_assert(LATER < 16, "the low four bits of vmcnt");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | LATER);
 }
 
 }  // namespace

@@ -202,9 +202,11 @@ extern "C" kt_status kt_act8_restore(kt_dtype dt, int64_t rows, int64_t cols, co
     return launched(who, kt_launch_act8_restore(dt, rows, cols, q, e, y, ldy, stream));
 }
 
+static const int64_t MOST_WEIGHTS = 1 << 24;        // rows, columns: a step of the kernel has 31-bit offsets
+
 static bool weight_grad_sizes(int64_t tokens, int64_t out, int64_t in)
 {
-    return tokens >= 0 && tokens <= (1ll << 40) && out >= 1 && in >= 1 && out <= MOST_ACT8_COLS && in <= MOST_ACT8_COLS && out * in <= (1ll << 46);
+    return tokens >= 0 && tokens <= (1ll << 40) && out >= 1 && in >= 1 && out <= MOST_WEIGHTS && in <= MOST_WEIGHTS;
 }
 
 extern "C" int64_t kt_act8_weight_grad_workspace(kt_dtype dt, int64_t tokens, int64_t out, int64_t in)
@@ -219,7 +221,7 @@ extern "C" kt_status kt_act8_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t toke
     const char *who = "kt_act8_weight_grad";
     if (!is_type(dt) || !is_type(gdt)) return bad(who, "unknown element type");
     if (!sizes(tokens, out, lddy) || !sizes(out, in, lddw)) return bad(who, "tokens >= 0, out and in >= 1 and ld >= columns are needed");
-    if (!weight_grad_sizes(tokens, out, in)) return unsupported(who, "more than 2^40 tokens, 2^30 rows or columns, or 2^46 weights");
+    if (!weight_grad_sizes(tokens, out, in)) return unsupported(who, "more than 2^40 tokens, or 2^24 rows or columns");
     if (!dw || (tokens && (!dy || !q || !e))) return bad(who, "NULL dy, q, e or dw");
     const int64_t need = kt_weight_grad_ws(dt, tokens, out, in);
     if (need && (!ws || ws_bytes < need)) return bad(who, "the workspace is smaller than kt_act8_weight_grad_workspace says");

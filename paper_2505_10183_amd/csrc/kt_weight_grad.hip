@@ -1,23 +1,25 @@
 // The weight gradient of a linear layer from the 8-bit checkpoint of its input: dw[o][i] = sum_t dy[t][o] x8[t][i].
 //
 // Both operands run over t along their rows, so both are read across rows from LDS.  A workgroup makes a tile of BM x BN of dw: per
-// step, BK rows of dy and of x8 go from memory into registers while the step before is multiplied, x8 is turned into
+// step, K rows of dy and of x8 go from memory into registers one or two steps before they are needed, x8 is turned into
 // dy's type on its way into LDS (exact in bf16: 7 bits and a power of two), and the two halves of LDS take turns, one barrier
-// a step.  Where dw has too few tiles for the chip, t is cut into pieces whose sums a second kernel adds in their order.
+// a step.  Rows of dy at multiples of 16 bytes are brought into LDS by the loads themselves (Feed).  Both the conversion and the reads of the next fragments stand beside the products (sched_barrier): the matrix cores take
+// 32 cycles for one, in which a wavefront issues 8 other instructions.  Where dw has too few tiles for the chip, t is cut into
+// pieces whose sums a second kernel adds in their order.
 #include "kt_mfma.h"
 
 namespace {
 
-template <typename T> constexpr int BK = 64 / (int)sizeof(T);          // 32 rows of bf16, 16 of f32
-
-// Tile and wavefronts: WM x WN of them, each FM x FN products of 32 x 32.
-template <int WM_, int WN_, int FM_, int FN_> struct Shape {
+// Tile and wavefronts: WM x WN of them, each FM x FN products of 32 x 32; rows of bf16 a step (half as many of f32) with dy brought
+// by DMA, and through registers.
+template <int WM_, int WN_, int FM_, int FN_, int KD, int KR> struct Shape {
     static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_;
     static constexpr int BM = WM * FM * 32, BN = WN * FN * 32, BLOCK = WM * WN * 64;
+    template <typename T, bool DMA> static constexpr int K = (DMA ? KD : KR) * 2 / (int)sizeof(T);
 };
-typedef Shape<2, 4, 4, 2> Big;       // 256 x 256, 8 wavefronts
-typedef Shape<2, 2, 2, 2> Mid;       // 128 x 128, 4
-typedef Shape<2, 2, 1, 1> Small;     //  64 x  64, 4
+typedef Shape<2, 4, 4, 2, 64, 32> Big;      // 256 x 256, 8 wavefronts, 128 or 64 KiB of LDS
+typedef Shape<2, 2, 2, 2, 64, 64> Mid;      // 128 x 128, 4,  64 KiB
+typedef Shape<2, 2, 1, 1, 64, 64> Small;    //  64 x  64, 4,  32 KiB
 
 // Tile of a workgroup: those of one XCD (every eighth workgroup) are neighbours, dy's columns first, so that its L2 keeps a
 // strip of x8 and all of dy's current rows.
@@ -27,60 +29,90 @@ __device__ __forceinline__ int xcd_order(int b, int n)
     return x * q + min(x, r) + b / 8;
 }
 
-template <typename T, typename S, typename G, bool PIECES>
+template <typename T, typename S, typename G, bool PIECES, bool DMA>
 __global__ __launch_bounds__(S::BLOCK) void kt_weight_grad_kernel(const T *dy, int64_t lddy, const int8_t *q, const uint8_t *e,
                                                                   G *dw, int64_t lddw, int64_t tokens, int out, int in, int mt,
                                                                   int64_t piece)
 {
-    constexpr int K = BK<T>, V = VE<T>;
-    constexpr int AC = K * S::BM / V / S::BLOCK;            // 16-byte chunks of dy that a lane brings
+    constexpr int K = S::template K<T, DMA>, V = VE<T>;
+    constexpr int AC = DMA ? 0 : K * S::BM / V / S::BLOCK;  // 16-byte chunks of dy that pass through a lane
     constexpr int BC = K * S::BN / 16 / S::BLOCK > 0 ? K * S::BN / 16 / S::BLOCK : 1;        // 16 bytes of x8 each
     constexpr bool BPART = K * S::BN / 16 < S::BLOCK;       // the first lanes only
+    constexpr int BU = 16 / V;                              // 16-byte chunks in LDS that 16 bytes of x8 make
     typedef Tile<T, S::BM> TA;
     typedef Tile<T, S::BN> TB;
-    __shared__ __align__(16) char lds[2][TA::bytes(K) + TB::bytes(K)];
+    typedef typename Frag<T>::type F;
+    constexpr int HALF = TA::bytes(K) + TB::bytes(K);
+    extern __shared__ __align__(16) char lds[];             // two halves
 
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid & 63;
     const int tile = xcd_order(blockIdx.x, gridDim.x), o0 = tile % mt * S::BM, i0 = tile / mt * S::BN;
     const int64_t t0 = (int64_t)blockIdx.y * piece, t1 = min(tokens, t0 + piece);
     const int groups = (in + KT_ACT8_GROUP - 1) / KT_ACT8_GROUP, wide = groups * KT_ACT8_GROUP;
 
-    u32x4 a[AC], b[BC];
-    uint32_t eb[BC];
-    auto load = [&](int64_t t) {
+    // What a lane has on its way: rows of one step.
+    struct Coming {
+        u32x4 a[AC > 0 ? AC : 1], b[BC];
+        uint32_t e[BC];
+    } coming;
+    Feed<T, S::BM, K, S::BLOCK, true> feed(dy + t0 * lddy + o0, lddy, (int)min((int64_t)INT32_MAX, t1 - t0), DMA ? out - o0 : 0);
+    // x8: through buffers that end at row t1, whose zeros (q = 0, e = 0) make nothing of what the tile holds past it.  Columns past the last
+    // are the next row's or zeros and end in columns of the tile that are not stored.
+    int at_b[BC], at_e[BC];
+#pragma unroll
+    for (int u = 0; u < BC; ++u) {
+        const int n = tid + u * S::BLOCK, row = n / (S::BN / 16), c = i0 + n % (S::BN / 16) * 16;
+        at_b[u] = !BPART || row < K ? row * wide + c : INT32_MIN;
+        at_e[u] = !BPART || row < K ? row * groups + c / KT_ACT8_GROUP : INT32_MIN;
+    }
+    auto load_b = [&](int64_t t, Coming &x) {
+        const int rows = (int)max((int64_t)0, min((int64_t)K, t1 - t));
+#pragma unroll
+        for (int u = 0; u < BC; ++u) {
+            x.b[u] = buffer16(q + t * wide, rows * wide, at_b[u]);
+            x.e[u] = buffer1(e + t * groups, rows * groups, at_e[u]);
+        }
+    };
+    // dy through registers: rows at and past t1 and columns past the last are zeros.
+    auto load = [&](int64_t t, Coming &x) {
 #pragma unroll
         for (int u = 0; u < AC; ++u) {
             const int n = tid + u * S::BLOCK, row = n / (S::BM / V), c = o0 + n % (S::BM / V) * V;
-            a[u] = t + row < t1 ? ld_chunk(dy + (t + row) * lddy, c, out) : u32x4{0, 0, 0, 0};
+            x.a[u] = t + row < t1 ? ld_chunk(dy + (t + row) * lddy, c, out) : u32x4{0, 0, 0, 0};
         }
-#pragma unroll
-        for (int u = 0; u < BC; ++u) {
-            const int n = tid + u * S::BLOCK, row = n / (S::BN / 16), c = i0 + n % (S::BN / 16) * 16;
-            b[u] = u32x4{0, 0, 0, 0};
-            eb[u] = 0;
-            if ((!BPART || row < K) && t + row < t1 && c < wide) {
-                b[u] = *(const u32x4 *)(q + (t + row) * wide + c);
-                eb[u] = e[(t + row) * groups + c / KT_ACT8_GROUP];
-            }
-        }
+        load_b(t, x);
     };
-    auto store = [&](char *buf) {
+    // The same without a branch, so that the loads stay on their way together: what lies past the last column is the next row's
+    // beginning then, in columns that are not stored.  For rows below `last`: all that the tile reads of them lies inside dy and before t1.
+    uint32_t at_a[AC > 0 ? AC : 1];
 #pragma unroll
-        for (int u = 0; u < AC; ++u) {
+    for (int u = 0; u < AC; ++u) {
+        const int n = tid + u * S::BLOCK;
+        at_a[u] = (uint32_t)(n / (S::BM / V)) * (uint32_t)(lddy * sizeof(T)) + (uint32_t)(o0 + n % (S::BM / V) * V) * (uint32_t)sizeof(T);
+    }
+    auto load_inside = [&](int64_t t, Coming &x) {
+        const char *pa = (const char *)(dy + t * lddy);
+#pragma unroll
+        for (int u = 0; u < AC; ++u) x.a[u] = ld16(pa + at_a[u]);
+        load_b(t, x);
+    };
+    int64_t last = lddy < 1 << 23 && (tokens - 1) * lddy + out >= o0 + S::BM ? min(t1, ((tokens - 1) * lddy + out - o0 - S::BM) / lddy + 1) : 0;
+    if (DMA) last = INT64_MAX / 2;
+    // Chunk number `u` of the AC + BC * BU that a lane writes into LDS.
+    constexpr int STORES = AC + BC * BU;
+    auto store = [&](char *buf, const Coming &x, auto u0) {
+        constexpr int u = u0;
+        if constexpr (u < AC) {
             const int n = tid + u * S::BLOCK;
-            *(u32x4 *)(buf + TA::at(n / (S::BM / V), n % (S::BM / V))) = a[u];
-        }
-        char *bb = buf + TA::bytes(K);
+            *(u32x4 *)(buf + TA::at(n / (S::BM / V), n % (S::BM / V))) = x.a[u];
+        } else {
+            constexpr int w = (u - AC) / BU, j = (u - AC) % BU;
+            const int n = tid + w * S::BLOCK, row = n / (S::BN / 16), c = n % (S::BN / 16);
+            if (BPART && row >= K) return;
+            float f[V];
 #pragma unroll
-        for (int u = 0; u < BC; ++u) {
-            const int n = tid + u * S::BLOCK, row = n / (S::BN / 16), c = n % (S::BN / 16);
-            if (BPART && row >= K) break;
-            const float step = step_of(eb[u]);
-            float f[16];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) from_bytes(b[u][j], step, f + 4 * j);
-#pragma unroll
-            for (int j = 0; j < 16 / V; ++j) *(u32x4 *)(bb + TB::at(row, c * (16 / V) + j)) = narrow<T>(f + j * V);
+            for (int k = 0; k < V / 4; ++k) from_bytes(x.b[w][j * (V / 4) + k], step_of(x.e[w]), f + 4 * k);
+            *(u32x4 *)(buf + TA::bytes(K) + TB::at(row, c * BU + j)) = narrow<T>(f);
         }
     };
 
@@ -91,29 +123,57 @@ __global__ __launch_bounds__(S::BLOCK) void kt_weight_grad_kernel(const T *dy, i
         for (int n = 0; n < S::FN; ++n) acc[m][n] = f32x16{0};
     const int m0 = wave / S::WN * S::FM * 32, n0 = wave % S::WN * S::FN * 32;
 
-    load(t0);
-    store(lds[0]);
-    __syncthreads();
-    int half = 0;
-    for (int64_t t = t0; t < t1; t += K, half ^= 1) {
-        const bool more = t + K < t1;
-        if (more) load(t + K);
-        const char *ta = lds[half], *tb = ta + TA::bytes(K);
-#pragma unroll
-        for (int c = 0; c < K / 16; ++c) {
-            typename Frag<T>::type fa[S::FM], fb[S::FN];
-#pragma unroll
-            for (int m = 0; m < S::FM; ++m) fa[m] = load_t<T, S::BM>(ta, c, m0 + 32 * m);
-#pragma unroll
-            for (int n = 0; n < S::FN; ++n) fb[n] = load_t<T, S::BN>(tb, c, n0 + 32 * n);
-#pragma unroll
-            for (int m = 0; m < S::FM; ++m)
-#pragma unroll
-                for (int n = 0; n < S::FN; ++n) mma(acc[m][n], fa[m], fb[n]);
-        }
-        if (more) store(lds[half ^ 1]);
+    // One step: the products of `now`, beside them what is coming goes into `next`.
+    constexpr int PER = S::FM * S::FN, N = K / 16 * PER, READS = S::FM + S::FN;
+    auto step = [&](const char *now, char *next, const Coming &x) {
+        const char *ta = now, *tb = now + TA::bytes(K);
+        constexpr int SETS = sizeof(T) == 2 ? 2 : 1;        // f32: products of 512 cycles need no reads ahead
+        F fa[SETS][S::FM], fb[SETS][S::FN];
+        auto read = [&](auto c0, auto r0) {
+            constexpr int c = c0, r = r0;
+            if constexpr (r < S::FM) fa[c % SETS][r] = load_t<T, S::BM>(ta, c, m0 + 32 * r);
+            else fb[c % SETS][r - S::FM] = load_t<T, S::BN>(tb, c, n0 + 32 * (r - S::FM));
+        };
+        auto product = [&](auto n1) {
+            constexpr int n = n1, c = n / PER, i = n % PER;
+            if constexpr (SETS == 1 && c && i == 0) span<0, READS>([&](auto r) { read(std::integral_constant<int, c>(), r); });
+            mma(acc[i / S::FN][i % S::FN], fa[c % SETS][i / S::FN], fb[c % SETS][i % S::FN]);
+            if constexpr (SETS == 2 && c + 1 < K / 16)
+                span<i * READS / PER, (i + 1) * READS / PER>([&](auto r) { read(std::integral_constant<int, c + 1>(), r); });
+            // the second half of the products: what is coming has had longer to arrive
+            constexpr int late = N / 2, from = n < late ? 0 : (n - late) * STORES / (N - late), to = n < late ? 0 : (n - late + 1) * STORES / (N - late);
+            span<from, to>([&](auto u) { store(next, x, u); });
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        span<0, READS>([&](auto r) { read(std::integral_constant<int, 0>(), r); });
+        __builtin_amdgcn_sched_barrier(0);
+        span<0, N>(product);
+    };
+
+    // in pairs of steps: rows past the last are zeros
+    auto half = [&](int64_t t, char *now, char *next, auto bring) {
+        if (DMA) feed.start(next, (int)(t - t0) + K);
+        step(now, next, coming);
+        bring(t + 2 * K, coming);
+        if (DMA) arrived<2 * BC>();                         // the loads of the line before may still be on their way
+        __syncthreads();
+    };
+    auto pair = [&](int64_t t, auto bring) {
+        half(t, lds, lds + HALF, bring);
+        half(t + K, lds + HALF, lds, bring);
+    };
+    int64_t t = t0;
+    if (t < t1) {
+        if (DMA) feed.start(lds, 0);
+        load(t0, coming);
+        span<0, STORES>([&](auto u) { store(lds, coming, u); });
+        load(t0 + K, coming);
+        if (DMA) arrived();
         __syncthreads();
     }
+    for (; t < t1 && t + 4 * K <= last; t += 2 * K) pair(t, load_inside);
+    if (!DMA)
+        for (; t < t1; t += 2 * K) pair(t, load);
     if (PIECES) dw += (int64_t)blockIdx.y * out * lddw;
     const int col = lane & 31, h = lane >> 5;
 #pragma unroll
@@ -151,9 +211,9 @@ struct Cut {
 };
 Cut cut(kt_dtype dt, int64_t tokens, int64_t out, int64_t in)
 {
-    const int k = dt == KT_F32 ? BK<float> : BK<bf16>;
+    const int k = dt == KT_F32 ? 32 : 64;
     auto tiles = [&](int64_t s) { return ((out + s - 1) / s) * ((in + s - 1) / s); };
-    Cut c{tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64, 1, tokens};
+    Cut c{dt == KT_BF16 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64, 1, tokens};
     const int64_t n = tiles(c.side);
     if (n < 256) {
         int64_t p = 512 / n, most = tokens / 256;
@@ -168,22 +228,38 @@ Cut cut(kt_dtype dt, int64_t tokens, int64_t out, int64_t in)
 }
 int64_t part_ld(int64_t in) { return (in + 3) / 4 * 4; }
 
-template <typename T, typename S, typename G, bool PIECES>
+template <typename T, typename S, typename G, bool PIECES, bool DMA>
 int go(const T *dy, int64_t lddy, const int8_t *q, const uint8_t *e, G *dw, int64_t lddw, int64_t tokens, int out, int in,
        const Cut &c, hipStream_t s)
 {
     const int mt = (out + S::BM - 1) / S::BM, nt = (in + S::BN - 1) / S::BN;
-    kt_weight_grad_kernel<T, S, G, PIECES><<<dim3((unsigned)mt * nt, c.pieces), S::BLOCK, 0, s>>>(dy, lddy, q, e, dw, lddw, tokens, out, in, mt, c.piece);
+    constexpr int LDS = 2 * (Tile<T, S::BM>::bytes(S::template K<T, DMA>) + Tile<T, S::BN>::bytes(S::template K<T, DMA>));
+    if (LDS > 65536) {
+        const hipError_t e1 = hipFuncSetAttribute((const void *)kt_weight_grad_kernel<T, S, G, PIECES, DMA>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        if (e1 != hipSuccess) return (int)e1;
+    }
+    kt_weight_grad_kernel<T, S, G, PIECES, DMA><<<dim3((unsigned)mt * nt, c.pieces), S::BLOCK, LDS, s>>>(dy, lddy, q, e, dw, lddw, tokens, out, in, mt, c.piece);
     return (int)hipGetLastError();
 }
 
-template <typename T, typename G, bool PIECES>
+template <typename T, typename G, bool PIECES, bool DMA>
 int by_side(const T *dy, int64_t lddy, const int8_t *q, const uint8_t *e, G *dw, int64_t lddw, int64_t tokens, int out, int in,
             const Cut &c, hipStream_t s)
 {
-    if (c.side == 256) return go<T, Big, G, PIECES>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
-    if (c.side == 128) return go<T, Mid, G, PIECES>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
-    return go<T, Small, G, PIECES>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
+    if constexpr (sizeof(T) == 2) {
+        if (c.side == 256) return go<T, Big, G, PIECES, DMA>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
+    }
+    if (c.side == 128) return go<T, Mid, G, PIECES, DMA>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
+    return go<T, Small, G, PIECES, DMA>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
+}
+template <typename T, typename G, bool PIECES>
+int by_rows(const T *dy, int64_t lddy, const int8_t *q, const uint8_t *e, G *dw, int64_t lddw, int64_t tokens, int out, int in,
+            const Cut &c, hipStream_t s)
+{
+    constexpr int64_t TO = 16 / sizeof(T);
+    if (reinterpret_cast<uintptr_t>(dy) % 16 == 0 && lddy % TO == 0 && out % TO == 0 && lddy * (int64_t)sizeof(T) < 1 << 24 && c.piece < 1 << 30)
+        return by_side<T, G, PIECES, true>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
+    return by_side<T, G, PIECES, false>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
 }
 
 template <typename T, typename G>
@@ -191,9 +267,9 @@ int weight_grad(kt_dtype dt, const T *dy, int64_t lddy, const int8_t *q, const u
                 int out, int in, float *ws, hipStream_t s)
 {
     const Cut c = cut(dt, tokens, out, in);
-    if (c.pieces == 1) return by_side<T, G, false>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
+    if (c.pieces == 1) return by_rows<T, G, false>(dy, lddy, q, e, dw, lddw, tokens, out, in, c, s);
     const int ld = (int)part_ld(in);
-    const int err = by_side<T, float, true>(dy, lddy, q, e, ws, ld, tokens, out, in, c, s);
+    const int err = by_rows<T, float, true>(dy, lddy, q, e, ws, ld, tokens, out, in, c, s);
     if (err) return err;
     kt_weight_grad_sum_kernel<G><<<dim3((ld / 4 + 255) / 256, out < 65535 ? out : 65535), 256, 0, s>>>(ws, c.pieces, out, in, ld, dw, lddw);
     return (int)hipGetLastError();

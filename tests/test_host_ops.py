@@ -96,8 +96,8 @@ WEIGHT_GRAD = dict(dt=BF16, gdt=BF16, tokens=4096, out=64, inn=64, dy=at(0), ldd
 @pytest.mark.parametrize("changes,status,word", [
     (dict(dt=2), EINVAL, "type"), (dict(gdt=2), EINVAL, "type"), (dict(tokens=-1), EINVAL, "tokens"), (dict(out=0), EINVAL, "out"),
     (dict(inn=0), EINVAL, "in"), (dict(lddy=63), EINVAL, "ld"), (dict(lddw=63), EINVAL, "ld"),
-    (dict(tokens=(1 << 40) + 1), EUNSUPPORTED, "tokens"), (dict(out=(1 << 30) + 1, lddy=1 << 31), EUNSUPPORTED, "2^30"),
-    (dict(inn=(1 << 30) + 1, lddw=1 << 31), EUNSUPPORTED, "2^30"), (dict(out=1 << 24, inn=1 << 23, lddy=1 << 24, lddw=1 << 23), EUNSUPPORTED, "2^46"),
+    (dict(tokens=(1 << 40) + 1), EUNSUPPORTED, "tokens"), (dict(out=(1 << 24) + 1, lddy=1 << 25), EUNSUPPORTED, "2^24"),
+    (dict(inn=(1 << 24) + 1, lddw=1 << 25), EUNSUPPORTED, "2^24"),
     (dict(dy=0), EINVAL, "NULL"), (dict(q=0), EINVAL, "NULL"), (dict(e=0), EINVAL, "NULL"), (dict(dw=0), EINVAL, "NULL"),
     (dict(dw=0, tokens=0), EINVAL, "NULL"), (dict(ws=0), EINVAL, "workspace"), (dict(ws_bytes=1), EINVAL, "workspace"),
     (dict(dy=at(0) + 1), EALIGN, "dy"), (dict(q=at(1) + 8), EALIGN, "q"), (dict(dw=at(3) + 1), EALIGN, "dw"), (dict(ws=at(4) + 8), EALIGN, "ws"),
