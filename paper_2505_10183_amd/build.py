@@ -67,7 +67,8 @@ def build_marshal(verbose: bool = False) -> str:
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
            "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(base, "include"),
            "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "kt_marshal.cpp"), "-o", tmp,
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "kt_marshal.cpp"),
+           os.path.join(CSRC, "kt_marshal_ops.cpp"), "-o", tmp,
            "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
     if verbose:
         print(" ".join(cmd), flush=True)

@@ -19,6 +19,8 @@
 
 #include "kt.h"
 
+bool kt_add_ops(PyObject *module, PyObject *device, PyObject *stream, PyObject *attribute);     // kt_marshal_ops.cpp
+
 namespace {
 
 PyObject *ctypes_array = nullptr;       // ctypes.Array
@@ -334,5 +336,6 @@ PyMODINIT_FUNC PyInit__kt_marshal(void)
     if (!m) return nullptr;
     Py_INCREF(&calls_type);
     if (PyModule_AddObject(m, "Calls", reinterpret_cast<PyObject *>(&calls_type)) < 0) { Py_DECREF(m); return nullptr; }
+    if (!kt_add_ops(m, get_device, get_stream, cuda_stream)) { Py_DECREF(m); return nullptr; }
     return m;
 }

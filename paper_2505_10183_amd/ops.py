@@ -1,7 +1,8 @@
 """Binding of the operators of kt_ops.h: shapes and strides of torch tensors to the sizes and addresses that the C calls take.
 
 All results go into tensors that the caller gives.  The calls are asynchronous on `stream` (None: torch's current one; a torch
-stream or a raw handle).  A `workspace` is a tensor of at least as many bytes as the library asks for, on the GPU; None takes one from torch's
+stream or a raw handle).  Plain tensors go to the library through _kt_marshal.so, everything else, and
+everything where that is missing, through ctypes.  A `workspace` is a tensor of at least as many bytes as the library asks for, on the GPU; None takes one from torch's
 allocator for the call, tied to that stream.  There is no fallback: tensors that are not on the current GPU are refused.
 """
 from __future__ import annotations
@@ -54,6 +55,26 @@ def _library() -> ctypes.CDLL:
             getattr(L, n).restype = i32
         _lib = L
     return L
+
+
+_plain_of = {}      # the native calls of each loaded library
+_ENTRIES = ("kt_layernorm_fwd", "kt_layernorm_bwd_workspace", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore",
+            "kt_act8_weight_grad_workspace", "kt_act8_weight_grad", "kt_attention_fwd", "kt_attention_bwd_workspace", "kt_attention_bwd")
+
+
+def _plainly(name: str, *args) -> bool:
+    """Make the call natively; False where an argument is of a form that is left to the code below."""
+    L = _library()
+    calls = _plain_of.get(L)
+    if calls is None:
+        m = binding._marshal_module()
+        calls = _plain_of[L] = m.Ops(*[ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _ENTRIES]) if m else False
+    if not calls:
+        return False
+    status = getattr(calls, name)(*args)
+    if status:
+        _check(status, L)
+    return status is not None
 
 
 def _type(x, what: str) -> int:
@@ -135,6 +156,8 @@ def _workspace(given, need: int, stream, device) -> Tuple[int, int, Optional[tor
 def kt_layernorm_fwd(x, gamma, beta, eps: float, y, mean=None, rstd=None, y8=None, stream=None):
     """y = (x - mean) * rstd * gamma + beta over the last dimension; beta, and mean with rstd (float32, a value a row), may be
     None.  y8 = (q, e): the 8-bit checkpoint of y, written in the same pass.  y may be x itself."""
+    if _plainly("layernorm_fwd", x, gamma, beta, eps, y, mean, rstd, y8, stream):
+        return
     L = _library()
     p, rows, cols, ld = _matrix(x, "x")
     py, ldy = _like(y, rows, cols, x.dtype, "y")
@@ -153,6 +176,8 @@ def kt_layernorm_bwd_workspace(rows: int, cols: int) -> int:
 def kt_layernorm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta=None, workspace=None, stream=None):
     """Gradients of input, weight and bias.  x: the input, or (q, e) of its 8-bit checkpoint.  dgamma and dbeta have gamma's type and
     may lie in a bucket; dx may be dy or x itself."""
+    if _plainly("layernorm_bwd", dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream):
+        return
     L = _library()
     p, rows, cols, ld = _matrix(dy, "dy")
     px = ldx = q = e = 0
@@ -174,6 +199,8 @@ def kt_layernorm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta=None, workspace
 
 def kt_act8_save(x, q, e, stream=None):
     """The 8-bit checkpoint (q, e) of x; shapes as kt_act8_shapes says, over the last dimension."""
+    if _plainly("act8_save", x, q, e, stream):
+        return
     L = _library()
     p, rows, cols, ld = _matrix(x, "x")
     pq, pe = _act8(q, e, rows, cols, "checkpoint")
@@ -184,6 +211,8 @@ def kt_act8_save(x, q, e, stream=None):
 
 def kt_act8_restore(q, e, y, stream=None):
     """What the checkpoint (q, e) stands for, into y."""
+    if _plainly("act8_restore", q, e, y, stream):
+        return
     L = _library()
     p, rows, cols, ld = _matrix(y, "y")
     pq, pe = _act8(q, e, rows, cols, "checkpoint")
@@ -199,6 +228,8 @@ def kt_act8_weight_grad_workspace(dtype, tokens: int, out: int, inn: int) -> int
 def kt_act8_weight_grad(dy, q, e, dw, workspace=None, stream=None):
     """dw [out, in] = dy^T x8: the weight gradient of a linear layer from dy [tokens, out] and the 8-bit checkpoint of its
     input [tokens, in].  dw may be float32 or bfloat16 whatever dy is, and may lie in a bucket."""
+    if _plainly("act8_weight_grad", dy, q, e, dw, workspace, stream):
+        return
     L = _library()
     p, tokens, out, ld = _matrix(dy, "dy")
     pw, rows, inn, ldw = _matrix(dw, "dw")
@@ -237,6 +268,8 @@ def kt_attention_fwd(q, k, v, o, lse=None, causal: bool = False, scale: Optional
     """o = softmax(scale q k^T) v; all tensors [batch, tokens, heads, dim] with adjacent elements of a head and any strides else,
     k and v with a divisor of q's heads.  lse [batch, heads, queries] (float32): what the backward pass needs.  scale: None =
     1 / sqrt(dim).  causal: the last query sees the last key.  k_lens [batch] (int32): keys of each sequence, on the GPU."""
+    if _plainly("attention_fwd", q, k, v, o, lse, causal, scale, k_lens, stream):
+        return
     L = _library()
     a, qs, ks = _attention(q, k, causal, scale, k_lens)
     t = q.dtype
@@ -255,6 +288,8 @@ def kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal: bool = False, scal
                      workspace=None, stream=None):
     """Gradients of q, k and v from that of o; o and lse are what kt_attention_fwd left for the same arguments.  dq, dk and dv may
     be views of one buffer, as q, k and v may."""
+    if _plainly("attention_bwd", do, q, k, v, o, lse, dq, dk, dv, causal, scale, k_lens, workspace, stream):
+        return
     L = _library()
     a, qs, ks = _attention(q, k, causal, scale, k_lens)
     t = q.dtype
