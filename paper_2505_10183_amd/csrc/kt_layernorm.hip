@@ -95,7 +95,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_fwd_kernel(const T 
 #pragma unroll
             for (int j = 0; j < V; ++j) f[i][j] = __fmaf_rn(f[i][j] * rs, g[i][j], b[i][j]);
             const u32x4 out = narrow<T>(f[i]);
-            st_chunk(y + row * ldy, c, cols, out);
+            st_chunk<T, true>(y + row * ldy, c, cols, out);
             if constexpr (SAVE) {           // of the values that y keeps; columns past the last are 0: g = b = 0
                 widen<T>(out, f[i]);
                 if (c >= cols) {
@@ -130,7 +130,7 @@ template <typename T, int NV, bool X8> struct RowIn {
     float mu, rs;
 };
 
-template <typename T, typename P, int LANES, int NV, bool X8>
+template <typename T, typename P, int LANES, int NV, bool X8, bool NT>
 __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_bwd_kernel(const T *dy, int64_t lddy, const T *x, int64_t ldx,
                                                                         const int8_t *x8, const uint8_t *e8, const P *gamma,
                                                                         const float *mean, const float *rstd, T *dx,
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_bwd_kernel(const T 
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * LANES + lane) * V;
-            in.dy[i] = ld_chunk(dy + r * lddy, c, cols);
+            in.dy[i] = ld_chunk<T, NT>(dy + r * lddy, c, cols);
             if constexpr (X8) {
                 in.e[i] = 0;
 #pragma unroll
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_bwd_kernel(const T 
                     in.e[i] = e8[r * groups + c / KT_ACT8_GROUP];
                 }
             } else {
-                in.x[i] = ld_chunk(x + r * ldx, c, cols);
+                in.x[i] = ld_chunk<T, NT>(x + r * ldx, c, cols);
             }
         }
     };
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_bwd_kernel(const T 
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
             for (int j = 0; j < V; ++j) t[i][j] = (t[i][j] - __fmaf_rn(xh[i][j], m2, m1)) * in.rs;
-            st_chunk(dx + row * lddx, (i * LANES + lane) * V, cols, narrow<T>(t[i]));
+            st_chunk<T, true>(dx + row * lddx, (i * LANES + lane) * V, cols, narrow<T>(t[i]));
         }
     }
     float *pg = parts + (int64_t)blockIdx.x * 2 * pcols, *pb = pg + pcols;
@@ -319,10 +319,10 @@ int bwd(int64_t rows, int cols, const T *dy, int64_t lddy, const T *x, int64_t l
     if (parts) {
         const int e = with_shape<T>(cols, [&](auto L, auto N) {
             constexpr int LANES = decltype(L)::value, NV = decltype(N)::value;
-            if (x8)
-                kt_layernorm_bwd_kernel<T, P, LANES, NV, true><<<parts, BLOCK<LANES>, 0, s>>>(dy, lddy, nullptr, 0, x8, e8, gamma, mean, rstd, dx, lddx, ws, rows, cols, pcols);
-            else
-                kt_layernorm_bwd_kernel<T, P, LANES, NV, false><<<parts, BLOCK<LANES>, 0, s>>>(dy, lddy, x, ldx, nullptr, nullptr, gamma, mean, rstd, dx, lddx, ws, rows, cols, pcols);
+            const bool nt = rows_of_16(dy, lddy) && (x8 || rows_of_16(x, ldx));
+            auto kernel = x8 ? (nt ? kt_layernorm_bwd_kernel<T, P, LANES, NV, true, true> : kt_layernorm_bwd_kernel<T, P, LANES, NV, true, false>)
+                             : (nt ? kt_layernorm_bwd_kernel<T, P, LANES, NV, false, true> : kt_layernorm_bwd_kernel<T, P, LANES, NV, false, false>);
+            kernel<<<parts, BLOCK<LANES>, 0, s>>>(dy, lddy, x, ldx, x8, e8, gamma, mean, rstd, dx, lddx, ws, rows, cols, pcols);
             return (int)hipGetLastError();
         });
         if (e) return e;

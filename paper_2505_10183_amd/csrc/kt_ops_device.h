@@ -52,13 +52,27 @@ template <> __device__ __forceinline__ u32x4 narrow<bf16>(const float *f)
     return u32x4{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])};
 }
 
-__device__ __forceinline__ u32x4 ld16(const void *p) { return *(const u32x4_any *)p; }
-__device__ __forceinline__ void st16(void *p, u32x4 v) { *(u32x4_any *)p = v; }
+// NT: non-temporal, for data that streams through once.
+template <bool NT = false> __device__ __forceinline__ u32x4 ld16(const void *p)
+{
+    if constexpr (NT) return __builtin_nontemporal_load((const u32x4_any *)p);
+    else return *(const u32x4_any *)p;
+}
+template <bool NT = false> __device__ __forceinline__ void st16(void *p, u32x4 v)
+{
+    if constexpr (NT) __builtin_nontemporal_store(v, (u32x4_any *)p);
+    else *(u32x4_any *)p = v;
+}
+// Whether rows start at multiples of 16 bytes.
+template <typename T> bool rows_of_16(const T *p, int64_t ld)
+{
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)sizeof(T) % 16 == 0;
+}
 
 // The chunk of a row that starts at column c; columns at and past `cols` read as 0 and are not stored.
-template <typename T> __device__ __forceinline__ u32x4 ld_chunk(const T *row, int c, int cols)
+template <typename T, bool NT = false> __device__ __forceinline__ u32x4 ld_chunk(const T *row, int c, int cols)
 {
-    if (c + VE<T> <= cols) return ld16(row + c);
+    if (c + VE<T> <= cols) return ld16<NT>(row + c);
     u32x4 r{0, 0, 0, 0};
     if (c < cols) {
 #pragma unroll
@@ -71,9 +85,9 @@ template <typename T> __device__ __forceinline__ u32x4 ld_chunk(const T *row, in
     }
     return r;
 }
-template <typename T> __device__ __forceinline__ void st_chunk(T *row, int c, int cols, u32x4 v)
+template <typename T, bool NT = false> __device__ __forceinline__ void st_chunk(T *row, int c, int cols, u32x4 v)
 {
-    if (c + VE<T> <= cols) { st16(row + c, v); return; }
+    if (c + VE<T> <= cols) { st16<NT>(row + c, v); return; }
 #pragma unroll
     for (int j = 0; j < VE<T>; ++j) {
         if (c + j < cols) {
