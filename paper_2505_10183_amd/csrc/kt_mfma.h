@@ -214,7 +214,9 @@ template <typename T, int D, int R, int BLOCK, bool DMA> struct Feed {
 template <int LATER = 0> __device__ __forceinline__ void arrived()
 {
     static_assert(LATER < 16, "the low four bits of vmcnt");
+    asm volatile("" ::: "memory");          // the later loads stay before it: LATER counts them
     __builtin_amdgcn_s_waitcnt(0x0f70 | LATER);
+    asm volatile("" ::: "memory");
 }
 
 }  // namespace
