@@ -44,7 +44,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_fwd_kernel(const T 
     const int lane = threadIdx.x % LANES, groups = (cols + KT_ACT8_GROUP - 1) / KT_ACT8_GROUP;
     const int64_t step = (int64_t)gridDim.x * ROWS<LANES>;
     int64_t row = (int64_t)blockIdx.x * ROWS<LANES> + threadIdx.x / LANES;
-    const float inv_n = 1.0f / (float)cols;
+    const float n_cols = (float)cols;          // divided by: 1 / cols would add a rounding to every row's mean and rstd
     float g[NV][V], b[NV][V];
     u32x4 next[NV];
 #pragma unroll
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_fwd_kernel(const T 
 #pragma unroll
             for (int j = 0; j < V; ++j) s[0] += f[i][j];
         row_sum<WAVES<LANES>>(s, red, 0);
-        const float mu = s[0] * inv_n;
+        const float mu = s[0] / n_cols;
         s[0] = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_fwd_kernel(const T 
             }
         }
         row_sum<WAVES<LANES>>(s, red, 1);
-        const float rs = 1.0f / __fsqrt_rn(s[0] * inv_n + eps);
+        const float rs = 1.0f / __fsqrt_rn(s[0] / n_cols + eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * LANES + lane) * V;
