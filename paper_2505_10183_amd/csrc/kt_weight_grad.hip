@@ -3,9 +3,14 @@
 // Both operands run over t along their rows, so both are read across rows from LDS.  A workgroup makes a tile of BM x BN of dw: per
 // step, K rows of dy and of x8 go from memory into registers one or two steps before they are needed, x8 is turned into
 // dy's type on its way into LDS (exact in bf16: 7 bits and a power of two), and the two halves of LDS take turns, one barrier
-// a step.  Rows of dy at multiples of 16 bytes are brought into LDS by the loads themselves (Feed).  Both the conversion and the reads of the next fragments stand beside the products (sched_barrier): the matrix cores take
-// 32 cycles for one, in which a wavefront issues 8 other instructions.  Where dw has too few tiles for the chip, t is cut into
-// pieces whose sums a second kernel adds in their order.
+// a step.  Rows of dy at multiples of 16 bytes are brought into LDS by the loads themselves (Feed).  Both the conversion and the
+// reads of the next fragments stand beside the products (sched_barrier): the matrix cores take 32 cycles for one, in which a
+// wavefront issues 8 other instructions.  Where dw has too few tiles for the chip, t is cut into pieces whose sums a second kernel
+// adds in their order.
+//
+// Bound by the matrix cores and the clock they leave: 16384 x 2048 x 8192 bf16 476 us, 1.15 PFLOP/s (a library product of the same
+// sizes from bf16 in memory 554 us); they are busy 57 % of the cycles, LDS 36 % (7 % of them bank conflicts).  Few tiles are bound by one
+// workgroup's steps one after another: 4099 x 1001 x 4004 has 256 tiles of 128, 65 us; 197 x 768 x 768 f32 144 of 64, 10 us.
 #include "kt_mfma.h"
 
 namespace {
@@ -140,8 +145,10 @@ __global__ __launch_bounds__(S::BLOCK) void kt_weight_grad_kernel(const T *dy, i
             mma(acc[i / S::FN][i % S::FN], fa[c % SETS][i / S::FN], fb[c % SETS][i % S::FN]);
             if constexpr (SETS == 2 && c + 1 < K / 16)
                 span<i * READS / PER, (i + 1) * READS / PER>([&](auto r) { read(std::integral_constant<int, c + 1>(), r); });
-            // the second half of the products: what is coming has had longer to arrive
-            constexpr int late = N / 2, from = n < late ? 0 : (n - late) * STORES / (N - late), to = n < late ? 0 : (n - late + 1) * STORES / (N - late);
+            // late among the products: what is coming has had longer to arrive.  Under DMA the wait for x8 is one for dy's tile too, which
+            // was started after it: the last quarter (16384 x 2048 x 8192 bf16 493 -> 476 us); else the second half (65 us of 4099 x 1001 x
+            // 4004; the last quarter 69).
+            constexpr int late = DMA ? N * 3 / 4 : N / 2, from = n < late ? 0 : (n - late) * STORES / (N - late), to = n < late ? 0 : (n - late + 1) * STORES / (N - late);
             span<from, to>([&](auto u) { store(next, x, u); });
             __builtin_amdgcn_sched_barrier(0);
         };
