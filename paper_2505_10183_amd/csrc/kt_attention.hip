@@ -14,6 +14,13 @@
 // it in memory, and sums whose order is fixed.
 //
 // Rounding of P and dS to bf16 is that of the operands of the products (the softmax's sum takes P before it).
+//
+// Measured, and what bounds it: the matrix cores and the softmax's vector work, which only partly run side by side; LDS is busy
+// under 30 % of the cycles and memory idle.  bf16, 128 wide, 8 x 2048 causal, 16 heads, backward 590 us: dq 235 (0.88 PFLOP/s, matrix
+// cores busy 51 % of the cycles), dk and dv 355 (0.77, 36 %: 482 registers leave one wavefront to a SIMD, and nothing covers its
+// waits).  Forward, 2 x 8191 causal, 16 heads on 4, one sequence of any length: 420 to 480 us with its length, 56 %.
+// f32: eight matrix instructions of 64 cycles to a fragment; 32 x 197, 12 heads, 64 wide, backward 205 us: dq 81, 75 % busy, dk and
+// dv 132, 62 %; the eighth wavefront of 197 keys has no work.
 #include "kt_mfma.h"
 
 namespace {

@@ -8,6 +8,9 @@
 //
 // The backward pass keeps dy * xh and dy of its columns in registers over all rows of the workgroup; a workgroup writes one
 // partial sum per column, and a second kernel adds these in a fixed order.
+//
+// Measured: forward with checkpoint, 16384 x 2048 bf16 30 us (170 MB, 5.6 TB/s); backward 25216 x 768 f32 38 us and 4 for the sums (6.1
+// TB/s), 9001 x 1001 bf16 through a checkpoint 15 and 3 (3.0 TB/s: rows that start at odd addresses).  197 x 768 f32 is one launch, 3.9 us.
 #include "kt_ops_device.h"
 
 namespace {
