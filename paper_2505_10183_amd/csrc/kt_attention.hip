@@ -374,6 +374,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
     if (there) store_row<T, D>(a.dq.at(at.b, at.h) + q * a.dq.token, dq, a.scale, a.dim);
 }
 
+// One wavefront to a SIMD: f32 of 64 held to 256 registers for two of them spills 39 (32 x 197, 12 heads: backward 206 -> 227 us).
 template <typename T, int D, bool DMA>
 __global__ __launch_bounds__(BLOCK, 1) void kt_attention_dkv_kernel(Args<T> a, int blocks)
 {
