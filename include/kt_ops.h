@@ -159,7 +159,9 @@ KT_API kt_status kt_attention_fwd(const kt_attention *a, const kt_heads *q,
  *   dq = scale * ds k,  dk = scale * ds^T q,  dv = p^T d_o,
  * dk and dv summed over the query heads that share a key head.  Every element
  * of dq, dk and dv is written: 0 where a query sees no key, and for keys past
- * k_lens.
+ * k_lens, whatever d_o, q and o hold.  As in the forward pass the causal mask
+ * gives weight 0: a NaN or infinity in a query's row of q or d_o can reach dk or dv,
+ * and one in a key's row dq, of what it is hidden from in the same tile.
  *   ws  kt_attention_bwd_workspace(a) bytes.
  */
 KT_API int64_t kt_attention_bwd_workspace(const kt_attention *a);

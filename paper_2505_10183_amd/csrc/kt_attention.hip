@@ -110,8 +110,10 @@ __device__ __forceinline__ float other_half(float x)
 // Row of register r in a 32 x 32 result, of this lane's half.
 __device__ __forceinline__ int row_of(int r) { return r % 4 + 8 * (r / 4) + 4 * ((threadIdx.x & 63) >> 5); }
 
-// A transposed result [d][row] to the row in memory: four adjacent elements at a time.
-template <typename T, int D> __device__ __forceinline__ void store_row(T *row, const f32x16 (&acc)[D / 32], float by, int dim)
+// A transposed result [d][row] to the row in memory: four adjacent elements at a time.  !any: zeros, whatever the sum holds: weights of 0
+// leave it 0 * inf where another row of the tile is not finite.
+template <typename T, int D>
+__device__ __forceinline__ void store_row(T *row, const f32x16 (&acc)[D / 32], float by, bool any, int dim)
 {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
@@ -120,7 +122,7 @@ template <typename T, int D> __device__ __forceinline__ void store_row(T *row, c
             const int d = db * 32 + row_of(4 * i);
             float f[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = acc[db][4 * i + j] * by;
+            for (int j = 0; j < 4; ++j) f[j] = any ? acc[db][4 * i + j] * by : 0.0f;
             if (d + 4 <= dim) {
                 if constexpr (sizeof(T) == 4) {
                     st16(row + d, narrow<float>(f));
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
     }
     if (!there) return;
     l += other_half(l);
-    store_row<T, D>(a.o.at(at.b, at.h) + q * a.o.token, o, l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l, a.dim);
+    store_row<T, D>(a.o.at(at.b, at.h) + q * a.o.token, o, l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l, true, a.dim);
     if (a.lse && lane < 32) a.lse[((int64_t)at.b * a.heads + at.h) * a.nq + q] = l == 0.0f ? NEVER : (mc + __log2f(l)) * LN2;
 }
 
@@ -371,7 +373,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
         step(std::true_type(), k0, kt0, vt0, kt1, vt1);
         if (k0 + R < all) step(std::true_type(), k0 + R, kt1, vt1, kt0, vt0);
     }
-    if (there) store_row<T, D>(a.dq.at(at.b, at.h) + q * a.dq.token, dq, a.scale, a.dim);
+    if (there) store_row<T, D>(a.dq.at(at.b, at.h) + q * a.dq.token, dq, a.scale, true, a.dim);
 }
 
 // One wavefront to a SIMD: f32 of 64 held to 256 registers for two of them spills 39 (32 x 197, 12 heads: backward 206 -> 227 us).
@@ -450,8 +452,13 @@ __global__ __launch_bounds__(BLOCK, 1) void kt_attention_dkv_kernel(Args<T> a, i
             }
             auto weigh = [&](int qb, int r) {
                 float p = __builtin_amdgcn_exp2f(__fmaf_rn(s[qb][r], c2, -ref[qb][r / 4][r % 4]));
-                if constexpr (edge) p = there && q0 + 32 * qb + row_of(r) >= mine ? p : 0.0f;
-                dp[qb][r] = p * (dp[qb][r] - delta[qb][r / 4][r % 4]);
+                float d = p * (dp[qb][r] - delta[qb][r / 4][r % 4]);
+                if constexpr (edge) {               // after the product, which may be 0 * inf
+                    const bool sees = there && q0 + 32 * qb + row_of(r) >= mine;
+                    p = sees ? p : 0.0f;
+                    d = sees ? d : 0.0f;
+                }
+                dp[qb][r] = d;
                 s[qb][r] = p;
                 if (r % 8 == 7) {
                     pf[qb][r / 8] = frag_of<T>(s[qb], r / 8);
@@ -511,8 +518,8 @@ __global__ __launch_bounds__(BLOCK, 1) void kt_attention_dkv_kernel(Args<T> a, i
         }
     }
     if (key < a.nk) {
-        store_row<T, D>(a.dk.at(b, hk) + key * a.dk.token, dk, a.scale, a.dim);
-        store_row<T, D>(a.dv.at(b, hk) + key * a.dv.token, dv, 1.0f, a.dim);
+        store_row<T, D>(a.dk.at(b, hk) + key * a.dk.token, dk, a.scale, there, a.dim);
+        store_row<T, D>(a.dv.at(b, hk) + key * a.dv.token, dv, 1.0f, there, a.dim);
     }
 }
 

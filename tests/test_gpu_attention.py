@@ -304,3 +304,44 @@ def test_the_same_bits_every_time_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("where", ["d_o", "o", "q"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_keys_past_the_length_have_no_gradient_whatever_a_query_holds(dtype, causal, bad, where):
+    """Lengths inside a wavefront's 32 keys and a workgroup's 128: the keys past them get 0, and the other sequence the same bits."""
+    dt = DT[dtype]
+    g = gen(31)
+    q, o, do = (normal(g, 2, 200, 2, 64, dtype=dt) for _ in range(3))
+    k, v = (normal(g, 2, 200, 1, 64, dtype=dt) for _ in range(2))
+    lens = torch.tensor([70, 130], dtype=torch.int32, device=DEV)
+    lse = torch.full((2, 2, 200), 6.0, device=DEV)
+    out = []
+    for value in (None, bad):
+        if value is not None:
+            {"d_o": do, "o": o, "q": q}[where][0, 150, :, 3] = value
+        dq, dk, dv = torch.full_like(q, 5.0), torch.full_like(k, 5.0), torch.full_like(k, 5.0)
+        kt.kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal=causal, k_lens=lens)
+        for b in range(2):
+            assert not dk[b, int(lens[b]):].any() and not dv[b, int(lens[b]):].any(), (value, b)
+        out.append([t[1].clone() for t in (dq, dk, dv)])
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.parametrize("where", ["d_o", "o"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dk_of_keys_that_a_query_does_not_see(dtype, where):
+    """A NaN in d_o or o of query 40 under a causal mask: dk of keys past 40 takes ds = 0 from it, also in its own tile."""
+    dt = DT[dtype]
+    g = gen(32)
+    q, k, v, o, do = (normal(g, 1, 128, 1, 64, dtype=dt) for _ in range(5))
+    lse = torch.full((1, 1, 128), 6.0, device=DEV)
+    out = []
+    for value in (1.0, math.nan):
+        {"d_o": do, "o": o}[where][0, 40, 0, 3] = value
+        dq, dk, dv = (torch.empty_like(q) for _ in range(3))
+        kt.kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal=True)
+        out.append(dk)
+    assert torch.equal(out[0][:, 41:], out[1][:, 41:]) and out[1][:, :41].isnan().any()
