@@ -142,8 +142,8 @@ typedef struct {
 /*
  * o = softmax(scale * q k^T) v over the keys that a query sees, and lse, the
  * logarithm of the softmax's denominator [batch, heads, nq] in binary32.  A
- * query that sees no key gets o = 0 and lse = -inf.  Keys at and past k_lens[b]
- * are not read; a value k_lens[b] outside [0, nk] counts as the nearer end.
+ * query that sees no key gets o = 0 and lse = -inf whatever the keys hold.  Keys
+ * at and past k_lens[b] are not read; a value k_lens[b] outside [0, nk] counts as the nearer end.
  * The causal mask gives a key no weight, and does not stop a NaN or infinity
  * in a v row from reaching earlier queries of the same tile (0 * inf).
  * lse may be NULL (no backward pass).

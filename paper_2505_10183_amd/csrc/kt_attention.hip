@@ -266,7 +266,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
     }
     if (!there) return;
     l += other_half(l);
-    store_row<T, D>(a.o.at(at.b, at.h) + q * a.o.token, o, l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l, true, a.dim);
+    store_row<T, D>(a.o.at(at.b, at.h) + q * a.o.token, o, l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l, mine > 0, a.dim);
     if (a.lse && lane < 32) a.lse[((int64_t)at.b * a.heads + at.h) * a.nq + q] = l == 0.0f ? NEVER : (mc + __log2f(l)) * LN2;
 }
 
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
         step(std::true_type(), k0, kt0, vt0, kt1, vt1);
         if (k0 + R < all) step(std::true_type(), k0 + R, kt1, vt1, kt0, vt0);
     }
-    if (there) store_row<T, D>(a.dq.at(at.b, at.h) + q * a.dq.token, dq, a.scale, true, a.dim);
+    if (there) store_row<T, D>(a.dq.at(at.b, at.h) + q * a.dq.token, dq, a.scale, mine > 0, a.dim);
 }
 
 // One wavefront to a SIMD: f32 of 64 held to 256 registers for two of them spills 39 (32 x 197, 12 heads: backward 206 -> 227 us).

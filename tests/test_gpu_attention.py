@@ -345,3 +345,23 @@ def test_dk_of_keys_that_a_query_does_not_see(dtype, where):
         kt.kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal=True)
         out.append(dk)
     assert torch.equal(out[0][:, 41:], out[1][:, 41:]) and out[1][:, :41].isnan().any()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_queries_without_keys_get_0_whatever_the_keys_hold(dim, dtype, bad):
+    """100 queries on 70 keys under a causal mask: the first 30 see none, and share their tile with queries that see keys
+    with a NaN or an infinity."""
+    dt = DT[dtype]
+    g = gen(33)
+    q, do = (normal(g, 1, 100, 2, dim, dtype=dt) for _ in range(2))
+    for where in ("k", "v"):
+        k, v = (normal(g, 1, 70, 2, dim, dtype=dt) for _ in range(2))
+        {"k": k, "v": v}[where][0, 0, :, 5] = bad
+        o, lse = torch.full_like(q, 5.0), torch.full((1, 2, 100), 5.0, device=DEV)
+        kt.kt_attention_fwd(q, k, v, o, lse, causal=True)
+        assert not o[:, :30].any() and bool((lse[:, :, :30] == -math.inf).all()), where
+        dq, dk, dv = torch.full_like(q, 5.0), torch.empty_like(k), torch.empty_like(k)
+        kt.kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal=True)
+        assert not dq[:, :30].any(), where
