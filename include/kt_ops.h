@@ -128,7 +128,11 @@ typedef struct {
     int64_t batch, token, head;
 } kt_heads;
 
-/* Sizes and mask shared by the forward and the backward pass. */
+/*
+ * Sizes and mask shared by the forward and the backward pass.  KT_EUNSUPPORTED: dim over KT_ATTENTION_MAX_DIM, more than
+ * 2^30 queries, keys or sequences, more than 2^16 heads, or 2^24 workgroups: batch * heads * ceil(nq / 128), and
+ * in the backward pass batch * kv_heads * ceil(nk / 128).
+ */
 typedef struct {
     kt_dtype dt;                  /* type of all tensors but lse                         */
     int64_t batch, nq, nk;        /* sequences, queries and keys of each                 */

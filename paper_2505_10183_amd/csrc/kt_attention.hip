@@ -26,6 +26,7 @@
 namespace {
 
 constexpr int WAVES = 4, BLOCK = WAVES * 64, OWN = WAVES * 32;      // rows that a workgroup owns
+static_assert(BLOCK == KT_ATTENTION_BLOCK && OWN == KT_ATTENTION_OWN, "the host counts workgroups");
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float NEVER = -__builtin_huge_valf();
 

@@ -301,7 +301,16 @@ bool distinct(const Spread &t)
     return true;
 }
 
-kt_status attention_sizes(const char *who, const kt_attention *a)
+// Whether a workgroup for every KT_ATTENTION_OWN tokens of every head makes fewer than 2^32 lanes: HIP launches no more.  batch * heads is
+// at most 2^46.
+bool launchable(int64_t batch, int64_t heads, int64_t tokens)
+{
+    const int64_t most = UINT32_MAX / KT_ATTENTION_BLOCK, blocks = (tokens + KT_ATTENTION_OWN - 1) / KT_ATTENTION_OWN;
+    return blocks == 0 || batch * heads <= most / blocks;
+}
+
+// `bwd`: the backward pass also launches over the keys.
+kt_status attention_sizes(const char *who, const kt_attention *a, bool bwd)
 {
     if (!a) return bad(who, "NULL sizes");
     if (!is_type(a->dt)) return bad(who, "unknown element type");
@@ -311,8 +320,8 @@ kt_status attention_sizes(const char *who, const kt_attention *a)
     if (a->dim > KT_ATTENTION_MAX_DIM) return unsupported(who, "dim over KT_ATTENTION_MAX_DIM");
     if (a->nq > MOST_TOKENS || a->nk > MOST_TOKENS || a->heads > MOST_HEADS || a->batch > MOST_TOKENS)
         return unsupported(who, "more than 2^30 queries, keys or sequences, or 2^16 heads");
-    const int64_t most = a->nq > a->nk ? a->nq : a->nk;
-    if (a->batch * a->heads > INT32_MAX / (most / 128 + 1)) return unsupported(who, "more than 2^31 workgroups");
+    if (!launchable(a->batch, a->heads, a->nq) || (bwd && !launchable(a->batch, a->kv_heads, a->nk)))
+        return unsupported(who, "2^24 workgroups or more, each 128 queries or keys of a head");
     return aligned(who, "k_lens", a->k_lens, 4);
 }
 
@@ -360,7 +369,7 @@ extern "C" kt_status kt_attention_fwd(const kt_attention *a, const kt_heads *q, 
                                       const kt_heads *o, float *lse, void *stream)
 {
     const char *who = "kt_attention_fwd";
-    KT_TRY(attention_sizes(who, a));
+    KT_TRY(attention_sizes(who, a, false));
     KT_TRY(heads_tensor(who, "q", q, a, a->nq, a->heads, false));
     KT_TRY(heads_tensor(who, "k", k, a, a->nk, a->kv_heads, false));
     KT_TRY(heads_tensor(who, "v", v, a, a->nk, a->kv_heads, false));
@@ -377,7 +386,7 @@ extern "C" kt_status kt_attention_fwd(const kt_attention *a, const kt_heads *q, 
 
 extern "C" int64_t kt_attention_bwd_workspace(const kt_attention *a)
 {
-    return attention_sizes("kt_attention_bwd_workspace", a) == KT_OK ? kt_attention_bwd_ws(a) : 0;
+    return attention_sizes("kt_attention_bwd_workspace", a, true) == KT_OK ? kt_attention_bwd_ws(a) : 0;
 }
 
 extern "C" kt_status kt_attention_bwd(const kt_attention *a, const kt_heads *d_o, const kt_heads *q, const kt_heads *k,
@@ -385,7 +394,7 @@ extern "C" kt_status kt_attention_bwd(const kt_attention *a, const kt_heads *d_o
                                       const kt_heads *dk, const kt_heads *dv, void *ws, int64_t ws_bytes, void *stream)
 {
     const char *who = "kt_attention_bwd";
-    KT_TRY(attention_sizes(who, a));
+    KT_TRY(attention_sizes(who, a, true));
     KT_TRY(heads_tensor(who, "d_o", d_o, a, a->nq, a->heads, false));
     KT_TRY(heads_tensor(who, "q", q, a, a->nq, a->heads, false));
     KT_TRY(heads_tensor(who, "k", k, a, a->nk, a->kv_heads, false));

@@ -28,6 +28,8 @@ int64_t kt_weight_grad_ws(kt_dtype dt, int64_t tokens, int64_t out, int64_t in);
 int kt_launch_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t tokens, int out, int in, const void *dy, int64_t lddy,
                           const int8_t *q, const uint8_t *e, void *dw, int64_t lddw, float *ws, void *stream);
 
+// Lanes of attention's workgroups, and the queries or keys of one head that a workgroup owns.
+constexpr int KT_ATTENTION_BLOCK = 256, KT_ATTENTION_OWN = 128;
 int64_t kt_attention_bwd_ws(const kt_attention *a);
 int kt_launch_attention_fwd(const kt_attention *a, const kt_heads *q, const kt_heads *k, const kt_heads *v, const kt_heads *o,
                             float *lse, void *stream);

@@ -249,3 +249,18 @@ def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
         else:
             with pytest.raises((ValueError, RuntimeError, AssertionError)):
                 f()
+
+
+def test_attention_refuses_what_hip_cannot_launch():
+    """2^24 workgroups of 256 lanes are 2^32 lanes.  One less passes this check: those calls are refused for a NULL tensor only."""
+    word, n = "workgroups", 1 << 24
+    for name in ("kt_attention_fwd", "kt_attention_bwd"):
+        for sizes in (dict(batch=n // 16, heads=16, kv_heads=16, nq=1, nk=1), dict(batch=n // 16, heads=16, kv_heads=1, nq=128, nk=1),
+                      dict(batch=n // 32, heads=16, kv_heads=16, nq=129, nk=1), dict(batch=1 << 30, heads=1 << 16, kv_heads=1, nq=1 << 30, nk=1)):
+            attention(name, EUNSUPPORTED, word, **sizes)
+        for sizes in (dict(batch=n - 1, heads=1, kv_heads=1, nq=128, nk=128), dict(batch=n // 4 - 1, heads=4, kv_heads=4, nq=1, nk=1),
+                      dict(batch=1 << 30, heads=1, kv_heads=1, nq=0, nk=0)):
+            attention(name, EINVAL, "NULL v", [("v", None)], **sizes)
+    keys = dict(batch=1 << 10, heads=16, kv_heads=16, nq=1, nk=(1 << 17) + 1)
+    attention("kt_attention_bwd", EUNSUPPORTED, word, **keys)
+    attention("kt_attention_fwd", EINVAL, "NULL v", [("v", None)], **keys)
