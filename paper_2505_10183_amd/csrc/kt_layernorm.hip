@@ -147,7 +147,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_bwd_kernel(const T 
     const int lane = threadIdx.x % LANES, groups = (cols + KT_ACT8_GROUP - 1) / KT_ACT8_GROUP;
     const int64_t step = (int64_t)gridDim.x * ROWS<LANES>;
     int64_t row = (int64_t)blockIdx.x * ROWS<LANES> + threadIdx.x / LANES;
-    const float inv_n = 1.0f / (float)cols;
+    const float n_cols = (float)cols;          // divided by, as in the forward pass
     float g[NV][V], dg[NV][V], db[NV][V];
     auto load = [&](int64_t r, RowIn<T, NV, X8> &in) {
         in.mu = mean[r];
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(BLOCK<LANES>) void kt_layernorm_bwd_kernel(const T 
             }
         }
         row_sum<WAVES<LANES>>(s, red, turn);
-        const float m1 = s[0] * inv_n, m2 = s[1] * inv_n;
+        const float m1 = s[0] / n_cols, m2 = s[1] / n_cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
 #pragma unroll

@@ -225,3 +225,16 @@ def test_in_a_graph_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((y, dx, dg, db), want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [41, 47, 82, 768, 1001, 2998, 8198])
+def test_a_constant_gradient_has_no_effect_through_the_mean(cols, dtype):
+    """t = 1 in every column and xh = 0: dx = 1 - mean(t) with the exact sum `cols`, whose division is exact."""
+    dt = DT[dtype]
+    x, dy = torch.zeros(5, cols, dtype=dt, device=DEV), torch.ones(5, cols, dtype=dt, device=DEV)
+    gamma = torch.ones(cols, device=DEV)
+    mean, rstd = torch.zeros(5, device=DEV), torch.ones(5, device=DEV)
+    dx, dgamma = torch.full_like(x, 5.0), torch.empty_like(gamma)
+    kt.kt_layernorm_bwd(dy, x, gamma, mean, rstd, dx, dgamma)
+    assert not dx.any()
