@@ -111,3 +111,17 @@ def test_written_into_a_bucket():
         made.append(dw.t.contiguous())
     plan.kt_bucket_pack(-1, made, packed)
     assert all(torch.equal(a, b) for a, b in zip(packed, direct))
+
+
+# Tiles of 128 and 256 and their pieces: 192 to 255 tiles and 512 tokens or more are cut in two, no whole step at their ends.
+@pytest.mark.parametrize("dtype,grad,pieces,tokens,out,inn", [
+    ("bf16", "bf16", 1, 300, 1792, 1800), ("bf16", "f32", 2, 1111, 1792, 1800), ("f32", "f32", 1, 300, 1792, 1800), ("f32", "bf16", 2, 1111, 1792, 1800),
+    ("bf16", "bf16", 1, 300, 3600, 3700), ("bf16", "bf16", 2, 1111, 3600, 3700), ("bf16", "f32", 2, 1111, 3592, 3490)])
+def test_tiles_and_pieces(dtype, grad, pieces, tokens, out, inn):
+    need = kt.kt_act8_weight_grad_workspace(DT[dtype], tokens, out, inn)
+    assert need == (0 if pieces == 1 else pieces * out * ((inn + 3) // 4 * 4) * 4)
+    for gap, off in ((0, 0), (3, 1)):               # rows of dy at multiples of 16 bytes, and not
+        dy, q, e, dw = case(tokens, out, inn, DT[dtype], DT[grad], gap, off)
+        kt.kt_act8_weight_grad(dy.t, q, e, dw.t)
+        check(dy.t, q, e, dw.t, inn, (gap, off))
+        assert dw.intact()
