@@ -106,3 +106,13 @@ def test_it_learns(example, dtype):
     x, target = normal(g, 4, 65, 128, dtype=dt), normal(g, 4, 65, 128, dtype=dt)
     losses = example.train(block, x, target, 12, 2.0)
     assert all(torch.isfinite(torch.tensor(losses))) and losses[-1] < 0.9 * losses[0], losses
+
+
+def test_it_learns_with_its_own_arguments(example, capsys, monkeypatch):
+    """As the command runs it: every loss is finite and below the first."""
+    monkeypatch.setattr(sys, "argv", [PATH])
+    example.main()
+    line = capsys.readouterr().out.splitlines()[0].split()
+    losses = [float(v) for v in line[1:]]
+    assert line[0] == "loss" and len(losses) == 5
+    assert all(v < losses[0] for v in losses[1:]) and losses[0] < 3.0, losses
