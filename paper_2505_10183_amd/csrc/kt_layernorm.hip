@@ -277,21 +277,22 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void kt_layernorm_sum_kernel(const 
     else if (c >= pcols && c < pcols + cols && dbeta) dbeta[c - pcols] = (P)s;
 }
 
-// Lanes and chunks for a row: the fewest lanes that hold it in MAX_NV chunks each.
+// f with N lanes and `nv` chunks a lane, at least NV of them: the kernels for the most columns that N lanes can have, and no more.
+template <typename T, int N, int NV, typename F> int with_chunks(int nv, F f)
+{
+    constexpr int MOST = (KT_LAYERNORM_MAX_COLS / VE<T> + N - 1) / N;
+    if constexpr (NV < MAX_NV && NV < MOST)
+        if (nv > NV) return with_chunks<T, N, NV + 1>(nv, f);
+    return f(std::integral_constant<int, N>(), std::integral_constant<int, NV>());
+}
+// Lanes and chunks for a row: the fewest lanes that hold it in MAX_NV chunks each.  With four times the lanes of the step below a row has
+// two chunks or more.
 template <typename T, typename F> int with_shape(int cols, F f)
 {
     const int chunks = (cols + VE<T> - 1) / VE<T>;
-    auto lanes = [&](auto L) -> int {
-        constexpr int N = decltype(L)::value;
-        const int nv = (chunks + N - 1) / N;
-        if (nv <= 1) return f(L, std::integral_constant<int, 1>());
-        if (nv == 2) return f(L, std::integral_constant<int, 2>());
-        if (nv == 3) return f(L, std::integral_constant<int, 3>());
-        return f(L, std::integral_constant<int, MAX_NV>());
-    };
-    if (chunks <= 64 * MAX_NV) return lanes(std::integral_constant<int, 64>());
-    if (chunks <= 256 * MAX_NV) return lanes(std::integral_constant<int, 256>());
-    return lanes(std::integral_constant<int, 1024>());
+    if (chunks <= 64 * MAX_NV) return with_chunks<T, 64, 1>((chunks + 63) / 64, f);
+    if (chunks <= 256 * MAX_NV) return with_chunks<T, 256, 2>((chunks + 255) / 256, f);
+    return with_chunks<T, 1024, 2>((chunks + 1023) / 1024, f);
 }
 static_assert(1024 * MAX_NV * VE<float> >= KT_LAYERNORM_MAX_COLS, "f32 rows need more lanes");
 

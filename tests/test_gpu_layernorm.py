@@ -238,3 +238,13 @@ def test_a_constant_gradient_has_no_effect_through_the_mean(cols, dtype):
     dx, dgamma = torch.full_like(x, 5.0), torch.empty_like(gamma)
     kt.kt_layernorm_bwd(dy, x, gamma, mean, rstd, dx, dgamma)
     assert not dx.any()
+
+
+@pytest.mark.parametrize("pdtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_three_chunks_a_lane_of_four_wavefronts(dtype, pdtype):
+    """5 000 columns of bf16, 2 500 of f32."""
+    cols = 5000 if dtype == "bf16" else 2500
+    test_forward(7, cols, dtype, pdtype)
+    for eight in (False, True):
+        test_backward(7, cols, dtype, pdtype, eight)
