@@ -74,7 +74,9 @@ kt_status apart_or_same(const char *who, const Block &out, const Block &other)
 bool sizes(int64_t rows, int64_t cols, int64_t ld)
 {
     const int64_t most = INT64_MAX / 16;
-    return rows >= 0 && cols >= 1 && ld >= cols && ld <= most && (rows == 0 || ld <= most / rows);
+    if (rows < 0 || cols < 1 || ld < cols || ld > most) return false;
+    const int64_t eight = kt_act8_groups(cols) * KT_ACT8_GROUP;
+    return rows == 0 || (ld > eight ? ld : eight) <= most / rows;
 }
 
 #define KT_TRY(call)                        \
@@ -220,7 +222,7 @@ extern "C" kt_status kt_act8_weight_grad(kt_dtype dt, kt_dtype gdt, int64_t toke
 {
     const char *who = "kt_act8_weight_grad";
     if (!is_type(dt) || !is_type(gdt)) return bad(who, "unknown element type");
-    if (!sizes(tokens, out, lddy) || !sizes(out, in, lddw)) return bad(who, "tokens >= 0, out and in >= 1 and ld >= columns are needed");
+    if (!sizes(tokens, out, lddy) || !sizes(tokens, in, in) || !sizes(out, in, lddw)) return bad(who, "tokens >= 0, out and in >= 1 and ld >= columns are needed");
     if (!weight_grad_sizes(tokens, out, in)) return unsupported(who, "more than 2^40 tokens, or 2^24 rows or columns");
     if (!dw || (tokens && (!dy || !q || !e))) return bad(who, "NULL dy, q, e or dw");
     const int64_t need = kt_weight_grad_ws(dt, tokens, out, in);

@@ -264,3 +264,15 @@ def test_attention_refuses_what_hip_cannot_launch():
     keys = dict(batch=1 << 10, heads=16, kv_heads=16, nq=1, nk=(1 << 17) + 1)
     attention("kt_attention_bwd", EUNSUPPORTED, word, **keys)
     attention("kt_attention_fwd", EINVAL, "NULL v", [("v", None)], **keys)
+
+
+def test_sizes_whose_checkpoint_cannot_be_addressed_are_refused():
+    """One column takes 32 bytes of a checkpoint: 2^58 rows are 2^63 bytes of q.  Each address here is far from the others."""
+    rows = 1 << 58
+    far = dict(rows=rows, cols=1, ldx=1, x=at(0), q=1 << 62, e=1 << 61)
+    call("kt_act8_save", dict(SAVE, **far), EINVAL, "rows")
+    call("kt_act8_restore", dict(dt=F32, rows=rows, cols=1, q=1 << 62, e=1 << 61, y=at(0), ldy=1, stream=0), EINVAL, "rows")
+    call("kt_layernorm_fwd", dict(LN_FWD, rows=rows, cols=1, ldx=1, ldy=1, y=1 << 60, mean=0, rstd=0, y8=1 << 62, e8=1 << 61), EINVAL, "rows")
+    # 2^40 tokens of one column of dy, the checkpoint 2^24 columns wide: 2^64 bytes
+    call("kt_act8_weight_grad", dict(WEIGHT_GRAD, tokens=1 << 40, out=1, inn=1 << 24, lddy=1, lddw=1 << 24, q=1 << 50, e=1 << 45, dw=1 << 44,
+                                     ws=1 << 56, ws_bytes=1 << 50), EINVAL, "tokens")
