@@ -15,8 +15,9 @@
  *  - Weight gradients may be written where a bucket keeps them: any address
  *    that is a multiple of the element size will do.
  *  - Sums, softmax statistics and products are held in binary32; a result is
- *    rounded to bf16 once, to nearest-even.  Results depend on the arguments
- *    alone: no atomics, every sum has a fixed order.
+ *    rounded to bf16 once, to nearest-even.  bf16 attention rounds more on the
+ *    way, as it says below.  Results depend on the arguments alone: no atomics,
+ *    every sum has a fixed order.
  *  - A matrix [rows, cols] has adjacent columns and rows `ld` elements apart
  *    (ld >= cols).  Rows may be 0: then weight gradients are written as 0.
  *  - Outputs must not overlap inputs or each other, except where a call says so.
@@ -87,8 +88,10 @@ KT_API kt_status kt_layernorm_bwd(kt_dtype dt, kt_dtype pdt, int64_t rows,
  * largest magnitude of the 32 and 2^E <= a < 2^(E+1):
  *   e = max(E - 6 + 127, 1),  q = rint(x * 2^(127 - e)) clamped to [-127, 127]
  * (ties to even).  The scale being a power of two, the one rounding is that of q:
- * at most half a step of 2^(e - 127) <= a / 64, one step for a member that is
- * clamped (a >= 127.5 steps); every value that q stands for is exact in bf16.
+ * at most half a step of 2^(e - 127), one step for a member that is clamped
+ * (a >= 127.5 steps); every value that q stands for is exact in bf16.  A step is at
+ * most a / 64 where a >= 2^-120; below that e stays 1 and a step 2^-126, and
+ * members of up to half of it become 0.
  * A group with a member that is not finite has e = 255 and q = 0 and stands for
  * NaN throughout, so that an overflow is not hidden.
  * A checkpoint takes 1.03 bytes an element.
@@ -144,6 +147,13 @@ typedef struct {
 } kt_attention;
 
 /*
+ * Rounding in bf16: the probabilities are rounded to bf16 as an operand of the
+ * product with v, and in the backward pass p and ds as operands of theirs; the
+ * sum of the softmax takes them before that.  delta comes from o as it was stored.
+ * So o stands 2.0e-3 from the formulas in norm and the gradients 2.4e-3; rounding
+ * once at the end leaves 1.5e-3 and 1.8e-3 (normal inputs, 2048 and 8191 keys,
+ * causal).  f32 has no rounding but that of its own arithmetic.
+ *
  * o = softmax(scale * q k^T) v over the keys that a query sees, and lse, the
  * logarithm of the softmax's denominator [batch, heads, nq] in binary32.  A
  * query that sees no key gets o = 0 and lse = -inf whatever the keys hold.  Keys
