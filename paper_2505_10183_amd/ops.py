@@ -4,6 +4,9 @@ All results go into tensors that the caller gives.  The calls are asynchronous o
 stream or a raw handle).  Plain tensors go to the library through _kt_marshal.so, everything else, and
 everything where that is missing, through ctypes.  A `workspace` is a tensor of at least as many bytes as the library asks for, on the GPU; None takes one from torch's
 allocator for the call, tied to that stream.  There is no fallback: tensors that are not on the current GPU are refused.
+
+The calls stand outside autograd, as those of binding.py do: inputs that require a gradient are taken as they are, outputs carry no
+graph, and version counters do not move; the backward pass is the caller's own sequence of calls.
 """
 from __future__ import annotations
 
