@@ -139,6 +139,19 @@ __device__ __forceinline__ void store_row(T *row, const f32x16 (&acc)[D / 32], f
         }
 }
 
+// The binary32 row in memory is added to a transposed result.
+template <int D> __device__ __forceinline__ void add_row(const float *row, f32x16 (&acc)[D / 32], int dim)
+{
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32x4 v = ld_chunk(row, db * 32 + row_of(4 * i), dim);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[db][4 * i + j] += as_f(v[j]);
+        }
+}
+
 // Rows of OWN and head of a workgroup.  The last rows of all heads come first: under a causal mask they have the most keys, and the
 // short ones fill the end of the launch.  (Head by head on each XCD, so that its L2 holds a head's keys: the long blocks of the last
 // heads end late; 8 x 2048 causal, 16 heads of 128: dk and dv 370 -> 427 us.)
@@ -377,6 +390,13 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || D == 64 ? 2 : 1) void kt_a
     if (there) store_row<T, D>(a.dq.at(at.b, at.h) + q * a.dq.token, dq, a.scale, mine > 0, a.dim);
 }
 
+// Tiles of queries after which f32 puts its sums into the rows of dk and dv in memory, which this workgroup alone writes, and begins
+// new ones: 512 queries.  One chain over all of them loses digits that the type has: 4 heads of 4 096 queries to a key head stood
+// 2.4e-6 from the formulas in norm, in pieces 8e-7.  It costs 3 % of the backward pass 64 wide (4 x 1024, 12 heads, 473 -> 485 us)
+// and 5 to 8 % 128 wide (951 -> 994), where the rows' way through memory takes registers that the steps need.  bf16 rounds to
+// 2^-8 at the end.
+constexpr int PIECE = 16;
+
 // One wavefront to a SIMD: f32 of 64 held to 256 registers for two of them spills 39 (32 x 197, 12 heads: backward 206 -> 227 us).
 template <typename T, int D, bool DMA>
 __global__ __launch_bounds__(BLOCK, 1) void kt_attention_dkv_kernel(Args<T> a, int blocks)
@@ -508,19 +528,46 @@ __global__ __launch_bounds__(BLOCK, 1) void kt_attention_dkv_kernel(Args<T> a, i
     }
     arrived();
     __syncthreads();
+    T *dk_row = a.dk.at(b, hk) + key * a.dk.token, *dv_row = a.dv.at(b, hk) + key * a.dv.token;
+    constexpr bool PIECES = sizeof(T) == 4;
+    int left = PIECE;                               // tiles until the sums are put into memory
+    bool begun = false;                             // the rows in memory hold the sums of earlier pieces
     while (q0 < upto) {
-        while (q0 < mid && q0 < upto) {             // of the last head q0 ends at upto, of the others at from again
+        while (q0 < mid && q0 < upto && left) {     // of the last head q0 ends at upto, of the others at from again
             step(std::true_type(), qt0, dt0, stat0, qt1, dt1, stat1);
             step(std::true_type(), qt1, dt1, stat1, qt0, dt0, stat0);
+            if constexpr (PIECES) left -= 2;
         }
-        while (q0 >= mid && q0 < upto) {
+        while (q0 >= mid && q0 < upto && left) {
             step(std::false_type(), qt0, dt0, stat0, qt1, dt1, stat1);
             step(std::false_type(), qt1, dt1, stat1, qt0, dt0, stat0);
+            if constexpr (PIECES) left -= 2;
+        }
+        if constexpr (PIECES) {
+            if (left || q0 >= upto) continue;
+            if (key < a.nk) {
+                if (begun) {
+                    add_row<D>(dk_row, dk, a.dim);
+                    add_row<D>(dv_row, dv, a.dim);
+                }
+                store_row<T, D>(dk_row, dk, 1.0f, there, a.dim);
+                store_row<T, D>(dv_row, dv, 1.0f, there, a.dim);
+            }
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{0};
+            begun = true;
+            left = PIECE;
         }
     }
     if (key < a.nk) {
-        store_row<T, D>(a.dk.at(b, hk) + key * a.dk.token, dk, a.scale, there, a.dim);
-        store_row<T, D>(a.dv.at(b, hk) + key * a.dv.token, dv, 1.0f, there, a.dim);
+        if constexpr (PIECES) {
+            if (begun) {
+                add_row<D>(dk_row, dk, a.dim);
+                add_row<D>(dv_row, dv, a.dim);
+            }
+        }
+        store_row<T, D>(dk_row, dk, a.scale, there, a.dim);
+        store_row<T, D>(dv_row, dv, 1.0f, there, a.dim);
     }
 }
 

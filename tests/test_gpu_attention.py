@@ -365,3 +365,24 @@ def test_queries_without_keys_get_0_whatever_the_keys_hold(dim, dtype, bad):
         dq, dk, dv = torch.full_like(q, 5.0), torch.empty_like(k), torch.empty_like(k)
         kt.kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal=True)
         assert not dq[:, :30].any(), where
+
+
+@pytest.mark.parametrize("dim,gap", [(64, 0), (128, 0), (80, 3), (33, 0)])
+@pytest.mark.parametrize("value", [0.1, 0.7, 0.9])
+def test_long_sums_of_dk_and_dv_keep_their_digits(value, dim, gap):
+    """16 heads of 4 096 queries share a key head: 65 536 terms.  With k = v = 0 and lse = 0 every p is 1, with one element of o at -1
+    every ds is d_o's value c, so that dv = dk = 65536 c.  All partial sums have the terms' sign: each addition is off by u of the
+    total at most, 512 in a piece, 128 of pieces, 8 for what else there is.  (One chain of 65 536 is 1e-4 off and more.)"""
+    c = float(torch.tensor(value))
+    B, nq, nk, H = 2, 4096, 40, 16
+    wide = lambda n, h, v: torch.full((B, n, h, dim + gap), v, device=DEV)[..., :dim]  # noqa: E731
+    q, o, do = wide(nq, H, 1.0), wide(nq, H, 0.0), wide(nq, H, c)
+    o[..., 0] = -1.0
+    k, v = wide(nk, 1, 0.0), wide(nk, 1, 0.0)
+    dq, dk, dv = wide(nq, H, 5.0), wide(nk, 1, math.nan), wide(nk, 1, math.nan)
+    lens = torch.tensor([nk, nk - 7], dtype=torch.int32, device=DEV)
+    kt.kt_attention_bwd(do, q, k, v, o, torch.zeros(B, H, nq, device=DEV), dq, dk, dv, scale=1.0, k_lens=lens)
+    want = torch.full((B, nk, 1, dim), c * nq * H, dtype=torch.float64, device=DEV)
+    want[1, nk - 7:] = 0.0
+    within(dk, want, (512 + 128 + 8) * U * want, "dk")
+    within(dv, want, (512 + 128 + 8) * U * want, "dv")
