@@ -16,11 +16,17 @@
 // Rounding of P and dS to bf16 is that of the operands of the products (the softmax's sum takes P before it).
 //
 // Measured, and what bounds it: the matrix cores and the softmax's vector work, which only partly run side by side; LDS is busy
-// under 30 % of the cycles and memory idle.  bf16, 128 wide, 8 x 2048 causal, 16 heads, backward 590 us: dq 235 (0.88 PFLOP/s, matrix
-// cores busy 51 % of the cycles), dk and dv 355 (0.77, 36 %: 482 registers leave one wavefront to a SIMD, and nothing covers its
-// waits).  Forward, 2 x 8191 causal, 16 heads on 4, one sequence of any length: 420 to 480 us with its length, 56 %.
-// f32: eight matrix instructions of 64 cycles to a fragment; 32 x 197, 12 heads, 64 wide, backward 205 us: dq 81, 75 % busy, dk and
-// dv 132, 62 %; the eighth wavefront of 197 keys has no work.
+// under 30 % of the cycles and memory idle.  Passes are timed by events among others; single kernels in a kernel trace, under which the long
+// ones run up to 10 % longer than in such passes.  bf16, 128 wide, 8 x 2048 causal, 16 heads, backward 580 to 605 us a pass; in the trace
+// dq 232 (0.89 PFLOP/s, matrix cores busy 52 % of the cycles), dk and dv 410 (0.67, 36 %: 480 registers leave one wavefront to a SIMD, and
+// nothing covers its waits).  Forward, 2 x 8191 causal, 16 heads on 4, one sequence of any length: 415 to 490 us with its length, 55 %.
+// f32: eight matrix instructions of 64 cycles to a fragment; 32 x 197, 12 heads, 64 wide, backward 206 to 209 us: dq 82, 74 % busy, dk and
+// dv 136, 60 %; the eighth wavefront of 197 keys has no work.
+//
+// Registers spilled to memory (one wavefront or two to a SIMD, see __launch_bounds__): bf16, 128 wide, off 16 bytes forward 42 and dq 790 (8 x
+// 2048 causal, 16 heads, rows 129 apart: forward 350 us for 184, backward 1 460 for 600); f32, 128 wide dk and dv 63, off 16 bytes 215.
+// One workgroup to 128 queries (dk and dv: keys) of a head whatever their number: 8 heads of 4 096 queries on one key head of 4 096 keys
+// are 32 workgroups of dk and dv, backward 980 us; 1 query of 16 heads on 8 192 keys 134 us forward.
 #include "kt_mfma.h"
 
 namespace {

@@ -9,8 +9,13 @@
 // The backward pass keeps dy * xh and dy of its columns in registers over all rows of the workgroup; a workgroup writes one
 // partial sum per column, and a second kernel adds these in a fixed order.
 //
-// Measured: forward with checkpoint, 16384 x 2048 bf16 30 us (170 MB, 5.6 TB/s); backward 25216 x 768 f32 38 us and 4 for the sums (6.1
-// TB/s), 9001 x 1001 bf16 through a checkpoint 15 and 3 (3.0 TB/s: rows that start at odd addresses).  197 x 768 f32 is one launch, 3.9 us.
+// Measured (kernel trace; data that was used just before is partly in the last-level cache): forward with checkpoint, 16384 x 2048 bf16 30 us
+// (170 MB, 5.6 TB/s; 39 amid a block's training step); backward 25216 x 768 f32 39 us and 5 for the sums (6.0 TB/s), 9001 x 1001 bf16 through
+// a checkpoint 15 and 4 (3.0 TB/s: rows that start at odd addresses), 16384 x 2048 bf16 through a checkpoint 41 with the sums, 27 at 6.33
+// TB/s.  197 x 768 f32 is one launch, 4 us.
+//
+// Wide rows in the backward pass hold more than registers do: with 1 024 lanes 14 to 231 registers are spilled for f32, 28 to 56 for bf16 (8192 x
+// 8192 f32 148 us, 5.4 TB/s; 4096 x 16384 f32 319 us, 2.5, bf16 135, 3.0).
 #include "kt_ops_device.h"
 
 namespace {
@@ -337,8 +342,9 @@ int bwd(int64_t rows, int cols, const T *dy, int64_t lddy, const T *x, int64_t l
 
 }  // namespace
 
-// Workgroups of the backward pass, each with one partial sum per column: two to a CU, fewer where they would have under
-// 4 rows to a wavefront each.
+// Workgroups of the backward pass, each with one partial sum per column: two to a CU, fewer where they would have under 16 rows each, which
+// is 4 to a wavefront where a wavefront takes a row.  Where several take one, a workgroup has its 16 rows one after another, and few rows
+// leave most of the chip idle: 1 000 rows of 8 192 are 63 workgroups, 38 us in bf16 for 8 at 6.33 TB/s.
 int64_t kt_layernorm_bwd_parts(int64_t rows, int64_t)
 {
     const int64_t need = (rows + 15) / 16;

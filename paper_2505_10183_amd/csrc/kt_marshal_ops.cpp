@@ -1,8 +1,8 @@
 // The hot half of the operators' binding (ops.py): plain tensors on the current GPU, straight to the C calls.  A call that has
 // anything else among its arguments returns None, and the other half, which raises every error of marshalling, makes it.
 //
-// On small tensors the host decides: layer norm of 197 x 768 took 9.9 us a call through ctypes and 4.5 us with the arguments at hand,
-// of which the launch is 4; attention's backward pass, three launches of which need 13 us, took 47 us.
+// On small tensors the host decides: layer norm of 197 x 768 takes 9.5 us a call through ctypes and 3.6 here, attention's forward pass over 16
+// queries and keys 10.1 and 5.8.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/ATen.h>

@@ -8,9 +8,10 @@
 // wavefront issues 8 other instructions.  Where dw has too few tiles for the chip, t is cut into pieces whose sums a second kernel
 // adds in their order.
 //
-// Bound by the matrix cores and the clock they leave: 16384 x 2048 x 8192 bf16 476 us, 1.15 PFLOP/s (a library product of the same
-// sizes from bf16 in memory 554 us); they are busy 57 % of the cycles, LDS 36 % (7 % of them bank conflicts).  Few tiles are bound by one
-// workgroup's steps one after another: 4099 x 1001 x 4004 has 256 tiles of 128, 65 us; 197 x 768 x 768 f32 144 of 64, 10 us.
+// Bound by the matrix cores and the clock they leave: 16384 x 2048 x 8192 bf16 468 to 499 us with the card, 1.10 to 1.17 PFLOP/s (a library
+// product of the same sizes from bf16 in memory 554 us); they are busy 58 % of the cycles, LDS 37 % (7 % of them bank conflicts).  Few tiles
+// are bound by one workgroup's steps one after another: 4099 x 1001 x 4004 has 256 tiles of 128, 65 us; 197 x 768 x 768 f32 144 of 64, 10 us.
+// (Passes among others, by events; a kernel trace shows 508 and 74 us.)
 #include "kt_mfma.h"
 
 namespace {
@@ -211,7 +212,16 @@ __global__ __launch_bounds__(256) void kt_weight_grad_sum_kernel(const float *pa
     }
 }
 
-// How a product is cut: tile side, pieces of t, rows in a piece.
+// How a product is cut: tile side, pieces of t, rows in a piece.  Both sides of each bound, in us, bf16 with 16 384 tokens where not said:
+//  - the largest side that makes 192 tiles: 6144 x 2048 (192 tiles of 256) 433 whole, in tiles of 128 547; 1024 x 8192 (128 tiles of 256)
+//    401 whole, in tiles of 128 302.  f32: 2048 x 2048 of 6 304 tokens 475 in tiles of 128, 480 in tiles of 64; 768 x 2304 (108 tiles of 128)
+//    471, in tiles of 64 273.
+//  - pieces below 256 tiles, about two workgroups to a CU: 768 x 768 (144 tiles of 64) 162 whole, 87 in two, 63 in three.
+//  - 256 tokens to a piece: 768 x 768 of 300 tokens 5.8 whole, 9.0 in two; of 1 024 tokens 13.2 and 12.6 (of 512 the rule loses: 6.6 and 9.8).
+//  - 16 pieces: 96 x 130 (6 tiles) 26 in eight, 19 in sixteen.
+// The rule does not count the rounds in which workgroups fill the chip, and loses where they fill it badly: 192 to 255 tiles of 256 are cut in
+// two (one workgroup to a CU, so 384 take two rounds: 6144 x 2048 470, whole 433); 2048 x 2048 (256 tiles of 128) stays whole at 243, as 64
+// tiles of 256 in four pieces it takes 151; 4099 x 1001 x 4004 67, in four pieces of tiles of 256 57.
 struct Cut {
     int side, pieces;
     int64_t piece;
