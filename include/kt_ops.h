@@ -186,6 +186,43 @@ KT_API kt_status kt_attention_bwd(const kt_attention *a, const kt_heads *d_o,
                                   const kt_heads *dk, const kt_heads *dv,
                                   void *ws, int64_t ws_bytes, void *stream);
 
+/* ---- embedding ------------------------------------------------------------------ */
+
+/* The type of token ids and targets. */
+typedef enum { KT_I32 = 0, KT_I64 = 1 } kt_index;
+
+/*
+ * y[t] = scale * w[ids[t]]: rows of the table w [vocab, width].  An id outside
+ * [0, vocab) stands for no token: its row of y is 0, and no row of w is read.
+ *   dt   type of y [tokens, width];  wdt: type of w;  it: type of ids [tokens].
+ * The product is made in binary32.  KT_EUNSUPPORTED: more than 2^30 tokens or rows,
+ * or 2^24 columns.
+ */
+KT_API kt_status kt_embedding_fwd(kt_dtype dt, kt_dtype wdt, kt_index it,
+                                  int64_t tokens, int64_t vocab, int64_t width,
+                                  const void *ids, const void *w, int64_t ldw,
+                                  float scale, void *y, int64_t ldy, void *stream);
+
+/*
+ * The gradient of the table: dw[v] = scale * sum over the tokens t with
+ * ids[t] = v of dy[t], in the order of t in pieces that depend on the number of
+ * tokens alone.  Rows of dy without a token (an id outside [0, vocab)) are not read.
+ *   dt          type of dy [tokens, width];  wdt: type of dw [vocab, width].
+ *   accumulate  0: every row of dw is written, those without a token as 0.
+ *               Otherwise the sums are added to dw (and rounded once more), and
+ *               rows without a token stay as they are: the second gradient of a
+ *               table that is also the weight of the last layer.
+ *   ws          kt_embedding_bwd_workspace(...) bytes.
+ */
+KT_API int64_t kt_embedding_bwd_workspace(int64_t tokens, int64_t vocab,
+                                          int64_t width);
+KT_API kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it,
+                                  int64_t tokens, int64_t vocab, int64_t width,
+                                  const void *ids, const void *dy, int64_t lddy,
+                                  float scale, void *dw, int64_t lddw,
+                                  int accumulate, void *ws, int64_t ws_bytes,
+                                  void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,6 +29,9 @@ struct Entries {
     decltype(&kt_attention_fwd) attention_fwd;
     decltype(&kt_attention_bwd_workspace) attention_bwd_workspace;
     decltype(&kt_attention_bwd) attention_bwd;
+    decltype(&kt_embedding_fwd) embedding_fwd;
+    decltype(&kt_embedding_bwd_workspace) embedding_bwd_workspace;
+    decltype(&kt_embedding_bwd) embedding_bwd;
 };
 constexpr int ENTRIES = sizeof(Entries) / sizeof(void *);
 
@@ -89,6 +92,21 @@ struct Args {
         const at::Tensor &t = tensor(x);
         if (!ok || t.scalar_type() != type || t.numel() != n || !t.is_contiguous()) return fail(), nullptr;
         return t.data_ptr();
+    }
+    // n token ids of either type
+    void *ids(PyObject *x, int64_t n, kt_index *type)
+    {
+        const at::Tensor &t = tensor(x);
+        *type = KT_I32;
+        if (!ok) return nullptr;
+        if (t.scalar_type() == at::kLong) *type = KT_I64;
+        return vector(x, n, *type == KT_I64 ? at::kLong : at::kInt);
+    }
+    bool truth(PyObject *x)
+    {
+        const int v = PyObject_IsTrue(x);
+        if (v < 0) fail();
+        return v > 0;
     }
     double real(PyObject *x)
     {
@@ -339,9 +357,38 @@ KT_OP(attention_bwd, 14)
     return finish(x, [&] { return f.attention_bwd(&s, &d, &q, &k, &v, &o, lse, &dq, &dk, &dv, ws, size, x.stream); });
 }
 
+// ids, w, y, scale, stream
+KT_OP(embedding_fwd, 5)
+{
+    const Matrix w(x, a[1]), y(x, a[2]);
+    if (w.cols != y.cols) x.fail();
+    kt_index it;
+    const void *ids = x.ids(a[0], y.rows, &it);
+    const float scale = (float)x.real(a[3]);
+    return finish(x, [&] { return f.embedding_fwd(y.type, w.type, it, y.rows, w.rows, y.cols, ids, w.p, w.ld, scale, y.p, y.ld, x.stream); });
+}
+
+// ids, dy, dw, scale, accumulate, workspace, stream
+KT_OP(embedding_bwd, 7)
+{
+    const Matrix dy(x, a[1]), dw(x, a[2]);
+    if (dw.cols != dy.cols) x.fail();
+    kt_index it;
+    const void *ids = x.ids(a[0], dy.rows, &it);
+    const float scale = (float)x.real(a[3]);
+    const int accumulate = x.truth(a[4]);
+    int64_t size;
+    if (!x.ok) Py_RETURN_NONE;
+    void *ws = x.workspace(a[5], f.embedding_bwd_workspace(dy.rows, dw.rows, dy.cols), &size);
+    return finish(x, [&] {
+        return f.embedding_bwd(dy.type, dw.type, it, dy.rows, dw.rows, dy.cols, ids, dy.p, dy.ld, scale, dw.p, dw.ld, accumulate, ws, size, x.stream);
+    });
+}
+
 #define KT_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {KT_METHOD(layernorm_fwd), KT_METHOD(layernorm_bwd), KT_METHOD(act8_save), KT_METHOD(act8_restore),
-                         KT_METHOD(act8_weight_grad), KT_METHOD(attention_fwd), KT_METHOD(attention_bwd), {nullptr, nullptr, 0, nullptr}};
+                         KT_METHOD(act8_weight_grad), KT_METHOD(attention_fwd), KT_METHOD(attention_bwd), KT_METHOD(embedding_fwd),
+                         KT_METHOD(embedding_bwd), {nullptr, nullptr, 0, nullptr}};
 
 // Ops(addresses of the entry points, in the order of Entries)
 PyObject *ops_new(PyTypeObject *type, PyObject *args, PyObject *)

@@ -420,3 +420,66 @@ extern "C" kt_status kt_attention_bwd(const kt_attention *a, const kt_heads *d_o
     KT_TRY(all_apart(who, outs, 4, ins, 7));
     return launched(who, kt_launch_attention_bwd(a, d_o, q, k, v, o, lse, dq, dk, dv, (float *)ws, stream));
 }
+
+// ---- embedding ---------------------------------------------------------------------
+
+namespace {
+
+const int64_t MOST_IDS = 1 << 30, MOST_WIDTH = 1 << 24;         // 31-bit numbers in the kernels
+
+bool is_index(kt_index t) { return t == KT_I32 || t == KT_I64; }
+int64_t size_of(kt_index t) { return t == KT_I32 ? 4 : 8; }
+bool embedding_sizes(int64_t tokens, int64_t vocab, int64_t width)
+{
+    return tokens >= 0 && vocab >= 1 && width >= 1 && tokens <= MOST_IDS && vocab <= MOST_IDS && width <= MOST_WIDTH;
+}
+
+}  // namespace
+
+extern "C" kt_status kt_embedding_fwd(kt_dtype dt, kt_dtype wdt, kt_index it, int64_t tokens, int64_t vocab, int64_t width,
+                                      const void *ids, const void *w, int64_t ldw, float scale, void *y, int64_t ldy, void *stream)
+{
+    const char *who = "kt_embedding_fwd";
+    if (!is_type(dt) || !is_type(wdt) || !is_index(it)) return bad(who, "unknown element type");
+    if (vocab < 1 || !sizes(tokens, width, ldy) || !sizes(vocab, width, ldw)) return bad(who, "tokens >= 0, vocab and width >= 1 and ld >= width are needed");
+    if (!embedding_sizes(tokens, vocab, width)) return unsupported(who, "more than 2^30 tokens or rows, or 2^24 columns");
+    if (!std::isfinite(scale)) return bad(who, "scale must be finite");
+    if (tokens == 0) return KT_OK;
+    if (!ids || !w || !y) return bad(who, "NULL ids, w or y");
+    KT_TRY(aligned(who, "ids", ids, size_of(it)));
+    KT_TRY(aligned(who, "w", w, size_of(wdt)));
+    KT_TRY(aligned(who, "y", y, size_of(dt)));
+    const Block out = matrix("y", y, dt, tokens, width, ldy);
+    KT_TRY(apart(who, out, flat("ids", ids, tokens * size_of(it))));
+    KT_TRY(apart(who, out, matrix("w", w, wdt, vocab, width, ldw)));
+    return launched(who, kt_launch_embedding_fwd(dt, wdt, it, tokens, (int)vocab, (int)width, ids, w, ldw, scale, y, ldy, stream));
+}
+
+extern "C" int64_t kt_embedding_bwd_workspace(int64_t tokens, int64_t vocab, int64_t width)
+{
+    return embedding_sizes(tokens, vocab, width) ? kt_embedding_bwd_ws(tokens, vocab, width) : 0;
+}
+
+extern "C" kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it, int64_t tokens, int64_t vocab, int64_t width,
+                                      const void *ids, const void *dy, int64_t lddy, float scale, void *dw, int64_t lddw,
+                                      int accumulate, void *ws, int64_t ws_bytes, void *stream)
+{
+    const char *who = "kt_embedding_bwd";
+    if (!is_type(dt) || !is_type(wdt) || !is_index(it)) return bad(who, "unknown element type");
+    if (vocab < 1 || !sizes(tokens, width, lddy) || !sizes(vocab, width, lddw)) return bad(who, "tokens >= 0, vocab and width >= 1 and ld >= width are needed");
+    if (!embedding_sizes(tokens, vocab, width)) return unsupported(who, "more than 2^30 tokens or rows, or 2^24 columns");
+    if (!std::isfinite(scale)) return bad(who, "scale must be finite");
+    if (!dw || (tokens && (!ids || !dy))) return bad(who, "NULL ids, dy or dw");
+    const int64_t need = kt_embedding_bwd_ws(tokens, vocab, width);
+    if (need && (!ws || ws_bytes < need)) return bad(who, "the workspace is smaller than kt_embedding_bwd_workspace says");
+    KT_TRY(aligned(who, "ids", ids, size_of(it)));
+    KT_TRY(aligned(who, "dy", dy, size_of(dt)));
+    KT_TRY(aligned(who, "dw", dw, size_of(wdt)));
+    KT_TRY(aligned(who, "ws", ws, 16));
+    const Block outs[] = {matrix("dw", dw, wdt, vocab, width, lddw), flat("ws", ws, need)};
+    const Block ins[] = {flat("ids", ids, tokens * size_of(it)), matrix("dy", dy, dt, tokens, width, lddy)};
+    for (const Block &o : outs)
+        for (const Block &i : ins) KT_TRY(apart(who, o, i));
+    KT_TRY(apart(who, outs[1], outs[0]));
+    return launched(who, kt_launch_embedding_bwd(dt, wdt, it, tokens, (int)vocab, (int)width, ids, dy, lddy, scale, dw, lddw, accumulate != 0, ws, stream));
+}

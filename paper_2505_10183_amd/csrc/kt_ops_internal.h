@@ -37,4 +37,10 @@ int kt_launch_attention_bwd(const kt_attention *a, const kt_heads *d_o, const kt
                             const kt_heads *o, const float *lse, const kt_heads *dq, const kt_heads *dk, const kt_heads *dv,
                             float *ws, void *stream);
 
+int kt_launch_embedding_fwd(kt_dtype dt, kt_dtype wdt, kt_index it, int64_t tokens, int vocab, int width, const void *ids, const void *w,
+                            int64_t ldw, float scale, void *y, int64_t ldy, void *stream);
+int64_t kt_embedding_bwd_ws(int64_t tokens, int64_t vocab, int64_t width);
+int kt_launch_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it, int64_t tokens, int vocab, int width, const void *ids, const void *dy,
+                            int64_t lddy, float scale, void *dw, int64_t lddw, bool add, void *ws, void *stream);
+
 #endif

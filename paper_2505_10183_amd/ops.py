@@ -19,6 +19,7 @@ from . import binding
 from .binding import KT_BF16, KT_F32, _check, _stream
 
 _TYPES = {torch.float32: KT_F32, torch.bfloat16: KT_BF16}
+_INDEX = {torch.int32: 0, torch.int64: 1}
 _lib = None         # the library that the prototypes below were given to
 
 ACT8_GROUP = 32
@@ -53,8 +54,12 @@ def _library() -> ctypes.CDLL:
         L.kt_attention_bwd_workspace.argtypes = [ap]
         L.kt_attention_bwd_workspace.restype = i64
         L.kt_attention_bwd.argtypes = [ap, hp, hp, hp, hp, hp, vp, hp, hp, hp, vp, i64, vp]
+        L.kt_embedding_fwd.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, f32, vp, i64, vp]
+        L.kt_embedding_bwd_workspace.argtypes = [i64, i64, i64]
+        L.kt_embedding_bwd_workspace.restype = i64
+        L.kt_embedding_bwd.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, f32, vp, i64, i32, vp, i64, vp]
         for n in ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore", "kt_act8_weight_grad",
-                  "kt_attention_fwd", "kt_attention_bwd"):
+                  "kt_attention_fwd", "kt_attention_bwd", "kt_embedding_fwd", "kt_embedding_bwd"):
             getattr(L, n).restype = i32
         _lib = L
     return L
@@ -62,7 +67,8 @@ def _library() -> ctypes.CDLL:
 
 _plain_of = {}      # the native calls of each loaded library
 _ENTRIES = ("kt_layernorm_fwd", "kt_layernorm_bwd_workspace", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore",
-            "kt_act8_weight_grad_workspace", "kt_act8_weight_grad", "kt_attention_fwd", "kt_attention_bwd_workspace", "kt_attention_bwd")
+            "kt_act8_weight_grad_workspace", "kt_act8_weight_grad", "kt_attention_fwd", "kt_attention_bwd_workspace", "kt_attention_bwd",
+            "kt_embedding_fwd", "kt_embedding_bwd_workspace", "kt_embedding_bwd")
 
 
 def _plainly(name: str, *args) -> bool:
@@ -117,6 +123,14 @@ def _vector(x, n: int, dtype, what: str) -> int:
     if x.dtype != dtype or x.numel() != n or not x.is_contiguous():
         raise ValueError("%s: %d adjacent elements of %s are needed, got %s %s" % (what, n, dtype, tuple(x.shape), x.dtype))
     return x.data_ptr()
+
+
+def _ids(x, n: int, what: str) -> Tuple[int, int]:
+    """(type, address) of n token ids."""
+    t = _INDEX.get(x.dtype)
+    if t is None:
+        raise ValueError("%s: int32 or int64 is needed, got %s" % (what, x.dtype))
+    return t, _vector(x, n, x.dtype, what)
 
 
 def _like(x, rows: int, cols: int, dtype, what: str) -> Tuple[int, int]:
@@ -300,5 +314,43 @@ def kt_attention_bwd(do, q, k, v, o, lse, dq, dk, dv, causal: bool = False, scal
     status = L.kt_attention_bwd(a, _heads(do, qs, t, "do"), _heads(q, qs, t, "q"), _heads(k, ks, t, "k"), _heads(v, ks, t, "v"),
                                 _heads(o, qs, t, "o"), _vector(lse, qs[0] * qs[1] * qs[2], torch.float32, "lse"),
                                 _heads(dq, qs, t, "dq"), _heads(dk, ks, t, "dk"), _heads(dv, ks, t, "dv"), ws, size, _stream(stream))
+    if status:
+        _check(status, L)
+
+
+def kt_embedding_fwd(ids, w, y, scale: float = 1.0, stream=None):
+    """y = scale * w[ids]: rows of the table w [vocab, width] by token, ids int32 or int64 of any shape, y of ids' shape and the width.  An id
+    outside [0, vocab) stands for no token: its row is 0."""
+    if _plainly("embedding_fwd", ids, w, y, scale, stream):
+        return
+    L = _library()
+    py, tokens, width, ldy = _matrix(y, "y")
+    pw, vocab, cols, ldw = _matrix(w, "w")
+    if cols != width:
+        raise ValueError("w: %d columns are needed, got %d" % (width, cols))
+    it, pi = _ids(ids, tokens, "ids")
+    status = L.kt_embedding_fwd(_type(y, "y"), _type(w, "w"), it, tokens, vocab, width, pi, pw, ldw, scale, py, ldy, _stream(stream))
+    if status:
+        _check(status, L)
+
+
+def kt_embedding_bwd_workspace(tokens: int, vocab: int, width: int) -> int:
+    return _library().kt_embedding_bwd_workspace(tokens, vocab, width)
+
+
+def kt_embedding_bwd(ids, dy, dw, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None):
+    """dw [vocab, width]: the gradient of the table from dy [tokens, width], all rows of it, or (accumulate) added to what dw holds.  dw may be
+    float32 or bfloat16 whatever dy is, and may lie in a bucket."""
+    if _plainly("embedding_bwd", ids, dy, dw, scale, accumulate, workspace, stream):
+        return
+    L = _library()
+    p, tokens, width, ld = _matrix(dy, "dy")
+    pw, vocab, cols, ldw = _matrix(dw, "dw")
+    if cols != width:
+        raise ValueError("dw: %d columns are needed, got %d" % (width, cols))
+    it, pi = _ids(ids, tokens, "ids")
+    ws, size, held = _workspace(workspace, L.kt_embedding_bwd_workspace(tokens, vocab, width), stream, dy.device)
+    status = L.kt_embedding_bwd(_type(dy, "dy"), _type(dw, "dw"), it, tokens, vocab, width, pi, p, ld, scale, pw, ldw, 1 if accumulate else 0, ws, size,
+                                _stream(stream))
     if status:
         _check(status, L)
