@@ -223,6 +223,52 @@ KT_API kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it,
                                   int accumulate, void *ws, int64_t ws_bytes,
                                   void *stream);
 
+/* ---- softmax cross entropy of a linear layer -------------------------------------- */
+
+/*
+ * loss[t] = lse[t] - z[t, targets[t]] with the logits z = x w^T and lse[t] = log of
+ * the sum over the vocabulary of exp(z[t]): the loss of a layer whose outputs,
+ * tokens x vocab of them, are nowhere kept.  A target outside [0, vocab) is none:
+ * loss and lse are 0 there, whatever the token's row of x holds.
+ *   dt       type of x [tokens, width] and w [vocab, width];  it: of targets [tokens].
+ *   lse      for the backward pass; NULL: not wanted.
+ *   ws       kt_linear_xent_fwd_workspace(...) bytes.
+ * Logits are products of dt pairs summed in binary32, and not rounded.  Where one is not
+ * finite the token's loss is not either.  x and w may have any stride and start; rows that are
+ * not multiples of 16 bytes, or do not begin at one, are copied into the workspace first.
+ * KT_EUNSUPPORTED: more than 2^24 tokens or rows of w, 2^20 columns, 2^38 elements of x.
+ */
+KT_API int64_t kt_linear_xent_fwd_workspace(kt_dtype dt, int64_t tokens,
+                                            int64_t vocab, int64_t width);
+KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
+                                    int64_t vocab, int64_t width, const void *x,
+                                    int64_t ldx, const void *w, int64_t ldw,
+                                    const void *targets, float *loss, float *lse,
+                                    void *ws, int64_t ws_bytes, void *stream);
+
+/*
+ * The gradients of x and w from dloss, that of each token's loss (of their mean: 1 over
+ * their number), and lse as the forward pass left it.  In pieces of the vocabulary,
+ *   dz = dloss * (exp(z - lse) - [v = target]),  dx = sum over v of dz w,
+ *   dw = sum over t of dz^T x.
+ * Every element of dx and dw is written.  A token without a target, or with dloss 0,
+ * takes no part whatever its row of x holds; its row of dx is 0.
+ *   dt       type of x, w, dx and dw.  dx or dw may be NULL: not wanted.
+ *   ws       kt_linear_xent_bwd_workspace(...) bytes: up to 2^27 elements of dz, a row of
+ *            binary32 sums for each token, and copies as in the forward pass.
+ * Rounding in bf16: dz is rounded to bf16 as an operand of both products.  f32 has no
+ * rounding but that of its own arithmetic.
+ */
+KT_API int64_t kt_linear_xent_bwd_workspace(kt_dtype dt, int64_t tokens,
+                                            int64_t vocab, int64_t width);
+KT_API kt_status kt_linear_xent_bwd(kt_dtype dt, kt_index it, int64_t tokens,
+                                    int64_t vocab, int64_t width,
+                                    const float *dloss, const void *x, int64_t ldx,
+                                    const void *w, int64_t ldw, const void *targets,
+                                    const float *lse, void *dx, int64_t lddx,
+                                    void *dw, int64_t lddw, void *ws,
+                                    int64_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

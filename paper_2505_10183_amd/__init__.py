@@ -22,4 +22,5 @@ def __getattr__(name):
 _OPERATORS = ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_layernorm_bwd_workspace", "kt_act8_shapes", "kt_act8_save", "kt_act8_restore",
               "kt_act8_weight_grad", "kt_act8_weight_grad_workspace",
               "kt_attention_fwd", "kt_attention_bwd", "kt_attention_bwd_workspace",
-              "kt_embedding_fwd", "kt_embedding_bwd", "kt_embedding_bwd_workspace")
+              "kt_embedding_fwd", "kt_embedding_bwd", "kt_embedding_bwd_workspace",
+              "kt_linear_xent_fwd", "kt_linear_xent_fwd_workspace", "kt_linear_xent_bwd", "kt_linear_xent_bwd_workspace")

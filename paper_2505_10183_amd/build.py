@@ -30,7 +30,7 @@ def build(verbose: bool = False, extra_defines=(), out: str = LIB) -> str:
     tag = "" if out == LIB else ".variant%d" % os.getpid()
     for name in ("kt_plan.cpp", "kt_sampler.cpp", "kt_api.cpp", "kt_pack_unpack.hip", "kt_reduce.hip",
                  "kt_fused.hip", "kt_sgd.hip", "kt_fused_sgd.hip", "kt_static.hip", "kt_ops.cpp", "kt_layernorm.hip", "kt_act8.hip",
-                 "kt_weight_grad.hip", "kt_attention.hip", "kt_embedding.hip"):
+                 "kt_weight_grad.hip", "kt_attention.hip", "kt_embedding.hip", "kt_xent.hip"):
         src = os.path.join(CSRC, name)
         obj = os.path.join(CSRC, os.path.splitext(name)[0] + tag + ".o")
         cmd = [HIPCC] + COMMON + list(extra_defines)

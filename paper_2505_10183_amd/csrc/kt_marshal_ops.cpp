@@ -32,6 +32,10 @@ struct Entries {
     decltype(&kt_embedding_fwd) embedding_fwd;
     decltype(&kt_embedding_bwd_workspace) embedding_bwd_workspace;
     decltype(&kt_embedding_bwd) embedding_bwd;
+    decltype(&kt_linear_xent_fwd_workspace) linear_xent_fwd_workspace;
+    decltype(&kt_linear_xent_fwd) linear_xent_fwd;
+    decltype(&kt_linear_xent_bwd_workspace) linear_xent_bwd_workspace;
+    decltype(&kt_linear_xent_bwd) linear_xent_bwd;
 };
 constexpr int ENTRIES = sizeof(Entries) / sizeof(void *);
 
@@ -385,10 +389,49 @@ KT_OP(embedding_bwd, 7)
     });
 }
 
+// x, w, targets, loss, lse, workspace, stream
+KT_OP(linear_xent_fwd, 7)
+{
+    const Matrix in(x, a[0]), w(x, a[1]);
+    if (w.cols != in.cols || w.scalar != in.scalar) x.fail();
+    kt_index it;
+    const void *targets = x.ids(a[2], in.rows, &it);
+    float *loss = static_cast<float *>(x.vector(a[3], in.rows, at::kFloat)), *lse = static_cast<float *>(x.vector(a[4], in.rows, at::kFloat));
+    int64_t size;
+    if (!x.ok) Py_RETURN_NONE;
+    void *ws = x.workspace(a[5], f.linear_xent_fwd_workspace(in.type, in.rows, w.rows, in.cols), &size);
+    return finish(x, [&] { return f.linear_xent_fwd(in.type, it, in.rows, w.rows, in.cols, in.p, in.ld, w.p, w.ld, targets, loss, lse, ws, size, x.stream); });
+}
+
+// dloss, x, w, targets, lse, dx, dw, workspace, stream
+KT_OP(linear_xent_bwd, 9)
+{
+    const Matrix in(x, a[1]), w(x, a[2]);
+    if (w.cols != in.cols || w.scalar != in.scalar) x.fail();
+    kt_index it;
+    const void *targets = x.ids(a[3], in.rows, &it);
+    const float *dloss = static_cast<float *>(x.vector(a[0], in.rows, at::kFloat)), *lse = static_cast<float *>(x.vector(a[4], in.rows, at::kFloat));
+    void *out[2] = {nullptr, nullptr};
+    int64_t ld[2] = {in.cols, in.cols};
+    for (int i = 0; i < 2; ++i) {
+        if (a[5 + i] == Py_None) continue;
+        const Matrix d(x, a[5 + i]);
+        d.like(x, i == 0 ? in : w);
+        out[i] = d.p;
+        ld[i] = d.ld;
+    }
+    int64_t size;
+    if (!x.ok) Py_RETURN_NONE;
+    void *ws = x.workspace(a[7], f.linear_xent_bwd_workspace(in.type, in.rows, w.rows, in.cols), &size);
+    return finish(x, [&] {
+        return f.linear_xent_bwd(in.type, it, in.rows, w.rows, in.cols, dloss, in.p, in.ld, w.p, w.ld, targets, lse, out[0], ld[0], out[1], ld[1], ws, size, x.stream);
+    });
+}
+
 #define KT_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {KT_METHOD(layernorm_fwd), KT_METHOD(layernorm_bwd), KT_METHOD(act8_save), KT_METHOD(act8_restore),
                          KT_METHOD(act8_weight_grad), KT_METHOD(attention_fwd), KT_METHOD(attention_bwd), KT_METHOD(embedding_fwd),
-                         KT_METHOD(embedding_bwd), {nullptr, nullptr, 0, nullptr}};
+                         KT_METHOD(embedding_bwd), KT_METHOD(linear_xent_fwd), KT_METHOD(linear_xent_bwd), {nullptr, nullptr, 0, nullptr}};
 
 // Ops(addresses of the entry points, in the order of Entries)
 PyObject *ops_new(PyTypeObject *type, PyObject *args, PyObject *)

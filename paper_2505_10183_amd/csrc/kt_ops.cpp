@@ -483,3 +483,88 @@ extern "C" kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it, in
     KT_TRY(apart(who, outs[1], outs[0]));
     return launched(who, kt_launch_embedding_bwd(dt, wdt, it, tokens, (int)vocab, (int)width, ids, dy, lddy, scale, dw, lddw, accumulate != 0, ws, stream));
 }
+
+// ---- cross entropy of a linear layer --------------------------------------------------
+
+namespace {
+
+// 31-bit numbers in the kernels, launches of fewer than 2^32 lanes, offsets within a tile of a copy of 31 bits
+const int64_t MOST_ROWS = 1 << 24, MOST_XENT_WIDTH = 1 << 20, MOST_X = 1ll << 38;
+
+bool xent_sizes(int64_t tokens, int64_t vocab, int64_t width)
+{
+    return tokens >= 0 && vocab >= 1 && width >= 1 && tokens <= MOST_ROWS && vocab <= MOST_ROWS && width <= MOST_XENT_WIDTH && tokens * width <= MOST_X;
+}
+const char *const XENT_SIZES = "more than 2^24 tokens or rows of w, 2^20 columns, or 2^38 elements of x";
+
+}  // namespace
+
+extern "C" int64_t kt_linear_xent_fwd_workspace(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
+{
+    return is_type(dt) && xent_sizes(tokens, vocab, width) && tokens ? kt_linear_xent_ws(dt, tokens, vocab, width, false) : 0;
+}
+
+extern "C" int64_t kt_linear_xent_bwd_workspace(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
+{
+    return is_type(dt) && xent_sizes(tokens, vocab, width) && tokens ? kt_linear_xent_ws(dt, tokens, vocab, width, true) : 0;
+}
+
+extern "C" kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t vocab, int64_t width, const void *x, int64_t ldx,
+                                        const void *w, int64_t ldw, const void *targets, float *loss, float *lse, void *ws,
+                                        int64_t ws_bytes, void *stream)
+{
+    const char *who = "kt_linear_xent_fwd";
+    if (!is_type(dt) || !is_index(it)) return bad(who, "unknown element type");
+    if (vocab < 1 || !sizes(tokens, width, ldx) || !sizes(vocab, width, ldw)) return bad(who, "tokens >= 0, vocab and width >= 1 and ld >= width are needed");
+    if (!xent_sizes(tokens, vocab, width)) return unsupported(who, XENT_SIZES);
+    if (tokens == 0) return KT_OK;
+    if (!x || !w || !targets || !loss) return bad(who, "NULL x, w, targets or loss");
+    const int64_t need = kt_linear_xent_ws(dt, tokens, vocab, width, false);
+    if (!ws || ws_bytes < need) return bad(who, "the workspace is smaller than kt_linear_xent_fwd_workspace says");
+    KT_TRY(aligned(who, "x", x, size_of(dt)));
+    KT_TRY(aligned(who, "w", w, size_of(dt)));
+    KT_TRY(aligned(who, "targets", targets, size_of(it)));
+    KT_TRY(aligned(who, "loss", loss, 4));
+    KT_TRY(aligned(who, "lse", lse, 4));
+    KT_TRY(aligned(who, "ws", ws, 16));
+    const Block outs[] = {flat("loss", loss, tokens * 4), flat("lse", lse, tokens * 4), flat("ws", ws, need)};
+    const Block ins[] = {matrix("x", x, dt, tokens, width, ldx), matrix("w", w, dt, vocab, width, ldw), flat("targets", targets, tokens * size_of(it))};
+    for (size_t i = 0; i < sizeof outs / sizeof *outs; ++i) {
+        for (const Block &b : ins) KT_TRY(apart(who, outs[i], b));
+        for (size_t j = 0; j < i; ++j) KT_TRY(apart(who, outs[i], outs[j]));
+    }
+    return launched(who, kt_launch_linear_xent_fwd(dt, it, tokens, vocab, width, x, ldx, w, ldw, targets, loss, lse, ws, stream));
+}
+
+extern "C" kt_status kt_linear_xent_bwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t vocab, int64_t width, const float *dloss,
+                                        const void *x, int64_t ldx, const void *w, int64_t ldw, const void *targets, const float *lse,
+                                        void *dx, int64_t lddx, void *dw, int64_t lddw, void *ws, int64_t ws_bytes, void *stream)
+{
+    const char *who = "kt_linear_xent_bwd";
+    if (!is_type(dt) || !is_index(it)) return bad(who, "unknown element type");
+    if (!dx) lddx = width;
+    if (!dw) lddw = width;
+    if (vocab < 1 || !sizes(tokens, width, ldx) || !sizes(vocab, width, ldw) || !sizes(tokens, width, lddx) || !sizes(vocab, width, lddw))
+        return bad(who, "tokens >= 0, vocab and width >= 1 and ld >= width are needed");
+    if (!xent_sizes(tokens, vocab, width)) return unsupported(who, XENT_SIZES);
+    if (!dx && !dw && tokens) return bad(who, "NULL dx and dw");
+    if (tokens && (!dloss || !x || !w || !targets || !lse)) return bad(who, "NULL dloss, x, w, targets or lse");
+    const int64_t need = tokens ? kt_linear_xent_ws(dt, tokens, vocab, width, true) : 0;
+    if (need && (!ws || ws_bytes < need)) return bad(who, "the workspace is smaller than kt_linear_xent_bwd_workspace says");
+    KT_TRY(aligned(who, "x", x, size_of(dt)));
+    KT_TRY(aligned(who, "w", w, size_of(dt)));
+    KT_TRY(aligned(who, "dx", dx, size_of(dt)));
+    KT_TRY(aligned(who, "dw", dw, size_of(dt)));
+    KT_TRY(aligned(who, "targets", targets, size_of(it)));
+    KT_TRY(aligned(who, "dloss", dloss, 4));
+    KT_TRY(aligned(who, "lse", lse, 4));
+    KT_TRY(aligned(who, "ws", ws, 16));
+    const Block outs[] = {matrix("dx", dx, dt, tokens, width, lddx), matrix("dw", dw, dt, vocab, width, lddw), flat("ws", ws, need)};
+    const Block ins[] = {matrix("x", x, dt, tokens, width, ldx), matrix("w", w, dt, vocab, width, ldw), flat("targets", targets, tokens * size_of(it)),
+                         flat("dloss", dloss, tokens * 4), flat("lse", lse, tokens * 4)};
+    for (size_t i = 0; i < sizeof outs / sizeof *outs; ++i) {
+        for (const Block &b : ins) KT_TRY(apart(who, outs[i], b));
+        for (size_t j = 0; j < i; ++j) KT_TRY(apart(who, outs[i], outs[j]));
+    }
+    return launched(who, kt_launch_linear_xent_bwd(dt, it, tokens, vocab, width, dloss, x, ldx, w, ldw, targets, lse, dx, lddx, dw, lddw, ws, stream));
+}

@@ -42,5 +42,11 @@ int kt_launch_embedding_fwd(kt_dtype dt, kt_dtype wdt, kt_index it, int64_t toke
 int64_t kt_embedding_bwd_ws(int64_t tokens, int64_t vocab, int64_t width);
 int kt_launch_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it, int64_t tokens, int vocab, int width, const void *ids, const void *dy,
                             int64_t lddy, float scale, void *dw, int64_t lddw, bool add, void *ws, void *stream);
+int64_t kt_linear_xent_ws(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd);
+int kt_launch_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t vocab, int64_t width, const void *x, int64_t ldx, const void *w,
+                              int64_t ldw, const void *targets, float *loss, float *lse, void *ws, void *stream);
+int kt_launch_linear_xent_bwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t vocab, int64_t width, const float *dloss, const void *x, int64_t ldx,
+                              const void *w, int64_t ldw, const void *targets, const float *lse, void *dx, int64_t lddx, void *dw, int64_t lddw,
+                              void *ws, void *stream);
 
 #endif

@@ -1,0 +1,689 @@
+// Softmax cross entropy of a linear layer, loss[t] = log sum_v exp(z[t][v]) - z[t][target_t] with z = x w^T, and its gradients
+// dz = dloss (exp(z - lse) - [v = target]),  dx = dz w,  dw = dz^T x.  The logits z are nowhere kept.
+//
+// All of it is products in tiles.  The forward pass leaves of a tile of z the largest value and the sum of the exponentials for every
+// token, which a small kernel joins.  The backward pass goes over pieces of the vocabulary: it makes z of a piece again, leaves dz in the
+// workspace in the operands' type, and takes the other two products from there; dx is carried from piece to piece in binary32.
+// dz is rounded to bf16 as an operand of bf16 products, as attention's probabilities are: its error, 2^-9 of an element's size, is below
+// that of the result's own rounding once some elements of either sign are added.
+//
+// Tokens without a target (or with dloss 0) take no part: their rows are made zeros where they are read, whatever they hold, tiles and steps
+// that hold no others are left out.
+#include "kt_mfma.h"
+
+namespace {
+
+// ---- a product ---------------------------------------------------------------------
+//
+// D[m][n] = sum_k A(m, k) B(n, k), a workgroup for a tile of BM x BN.  An operand is `along` k (k adjacent in memory) or across it (m or n
+// adjacent).  Its tiles of K steps of k are brought by loads that write LDS themselves, those of the next step beside the products of this one.
+// k runs 16 c + 8 h + j over the element j of chunk c, for both kinds.  The 32 rows of a fragment of A are taken in an order that
+// gives a lane of D 16 neighbouring m: register r of half h is row 16 h + r.
+
+// Row of the matrix that row i of a fragment holds.
+__device__ __forceinline__ int spread_of(int i) { return (i >> 2 & 1) * 16 + (i >> 3) * 4 + (i & 3); }
+
+// Tile and wavefronts: WM x WN of them, each FM x FN products of 32 x 32.
+template <int WM_, int WN_, int FM_, int FN_> struct Shape {
+    static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_;
+    static constexpr int BM = WM * FM * 32, BN = WN * FN * 32, BLOCK = WM * WN * 64;
+};
+typedef Shape<2, 4, 4, 2> Big;      // 256 x 256, 8 wavefronts, 128 KiB of LDS
+typedef Shape<2, 2, 2, 2> Mid;      // 128 x 128, 4,  64 KiB
+typedef Shape<2, 2, 1, 1> Small;    //  64 x  64, 4,  32 KiB
+template <typename T> constexpr int STEP = 128 / (int)sizeof(T);       // k of a step
+
+template <typename T> struct Operand {
+    const T *p;
+    int64_t ld;
+    int count;                      // of m or n; a multiple of 16 bytes where those are adjacent
+};
+
+typedef const uint64_t __attribute__((address_space(4))) *Words;
+// Which of the tokens from k on take part, a bit each; null: all of them.
+__device__ __forceinline__ uint64_t live_of(Words live, int k)
+{
+    return live ? live[k >> 6] >> (k & 63) : ~0ull;
+}
+
+// Tiles of one operand on their way from memory to LDS, SIDE of m or n by STEP of k.
+template <typename T, int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct Bring {
+    static constexpr int V = VE<T>, K = STEP<T>, W = ALONG ? K : SIDE, R = ALONG ? SIDE : K, N = R * W / V / BLOCK;
+    static_assert(N >= 1, "a chunk for every lane");
+    typedef Tile<T, W> Rows;
+    const T *p;
+    int64_t ld;
+    int count, at[N];
+    __device__ __forceinline__ static int row_of(int u) { return (threadIdx.x + u * BLOCK) / (W / V); }
+    __device__ __forceinline__ static int col_of(int u)
+    {
+        const int n = threadIdx.x + u * BLOCK;
+        return (n % (W / V) ^ Rows::swizzle(n / (W / V))) * V;
+    }
+    __device__ __forceinline__ Bring(const Operand<T> &o, int first) : p(ALONG ? o.p + first * o.ld : o.p + first), ld(o.ld), count(min(SIDE, o.count - first))
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int r = row_of(u), row = ALONG && SPREAD ? (r & ~31) + spread_of(r & 31) : r, c = col_of(u);
+            at[u] = (ALONG ? row : c) < count ? (row * (int)ld + c) * (int)sizeof(T) : INT32_MIN;
+        }
+    }
+    // Starts bringing the steps from k on into `tile`; `left`: steps until the end.  What lies past an end is zeros and is not read, and so
+    // are steps whose bit of `live` is 0 (across only).
+    __device__ __forceinline__ void start(char *tile, int k, int left, uint64_t live)
+    {
+        const int up = (min(left, K) + V - 1) / V * V;
+        if (ALONG && left < K) {
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                if (col_of(u) >= up) at[u] = INT32_MIN;
+        }
+        const T *from = ALONG ? p + k : p + k * ld;
+        const int bytes = (ALONG ? (count - 1) * (int)ld + up : (min(left, K) - 1) * (int)ld + count) * (int)sizeof(T);
+        const uint64_t base = (uint64_t)from;
+        const u32x4 rs{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+        const uint32_t to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int off = ALONG || (live >> row_of(u) & 1) ? at[u] : INT32_MIN;
+            // as Feed::bring
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :: "s"(to + u * BLOCK * 16), "v"(off), "s"(rs) : "memory");
+        }
+    }
+};
+
+// Fragment of 32 m or n from `first` on, chunk c of the step.
+template <typename T, int SIDE, bool ALONG, bool SPREAD>
+__device__ __forceinline__ typename Frag<T>::type fragment(const char *tile, int first, int c)
+{
+    if constexpr (ALONG) {
+        return load_r<T, STEP<T>>(tile, first, c);
+    } else if constexpr (sizeof(T) == 2) {
+        const int l = threadIdx.x & 63, h = l >> 5, g = l >> 4 & 1, i = l & 15, j = i & 3;
+        const int col = first + (SPREAD ? g * 8 + (j & 1) * 16 + (j >> 1) * 4 : g * 16 + j * 4);
+        s16x4 v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int row = 16 * c + 8 * h + 4 * k + (i >> 2);
+            const char *p = tile + Tile<T, SIDE>::at(row, col >> 3) + (col & 7) * 2;
+            v[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KT_LDS s16x4 *)p);
+        }
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        const int l = threadIdx.x & 63, h = l >> 5, col = first + (SPREAD ? spread_of(l & 31) : l & 31);
+        f32x8 v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int row = 16 * c + 8 * h + j;
+            v[j] = *(const float *)(tile + Tile<T, SIDE>::at(row, col >> 2) + (col & 3) * 4);
+        }
+        return v;
+    }
+}
+
+// Tile number `b` of mt x nt: those of one XCD (every eighth workgroup) follow each other, in blocks of 8 n by as many m as
+// are at work, so that its L2 keeps their operands.
+struct Place {
+    int m, n;
+};
+__device__ __forceinline__ Place place(int b, int mt, int nt)
+{
+    const int all = mt * nt, q = all / 8, r = all % 8, x = b % 8, i = x * q + min(x, r) + b / 8;
+    const int group = i / (8 * mt), wide = min(8, nt - group * 8), j = i - group * 8 * mt;
+    return Place{j / wide, group * 8 + j % wide};
+}
+
+// E: what becomes of the tile.  E::skip(n0, count): nothing to multiply;  E::begin(acc, ...) the sums' start;  E::end(acc, ...).
+template <typename T, typename S, bool AA, bool BA, typename E>
+__global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a, Operand<T> b, int steps, int piece, const uint64_t *live_, int mt, int nt, E e)
+{
+    constexpr int K = STEP<T>;
+    typedef Bring<T, S::BM, S::BLOCK, AA, true> BringA;
+    typedef Bring<T, S::BN, S::BLOCK, BA, false> BringB;
+    typedef typename Frag<T>::type F;
+    constexpr int ABYTES = S::BM * 128, HALF = (S::BM + S::BN) * 128;
+    extern __shared__ __align__(16) char lds[];             // two halves
+
+    const Words live = (Words)(uintptr_t)live_;
+    const int wave = wave_id(), lane = threadIdx.x & 63;
+    const Place at = place(blockIdx.x, mt, nt);
+    const int m0 = at.m * S::BM, n0 = at.n * S::BN, wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
+    const int k0 = blockIdx.y * piece, k1 = min(steps, k0 + piece);
+
+    f32x16 acc[S::FM][S::FN];
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int n = 0; n < S::FN; ++n)
+#pragma unroll
+            for (int m = 0; m < S::FM; ++m) f(m, n);
+    };
+    each([&](int m, int n) { acc[m][n] = f32x16{0}; });
+    if (!e.skip(n0, S::BN)) {
+        BringA from_a(a, m0);
+        BringB from_b(b, n0);
+        // the next step that has a live token
+        auto next = [&](int k) {
+            if constexpr (!AA && !BA)
+                while (k < k1 && (live_of(live, k) & (K == 64 ? ~0ull : 0xffffffffull)) == 0) k += K;
+            return k;
+        };
+        auto bring = [&](char *to, int k) {
+            const uint64_t bits = !AA && !BA ? live_of(live, k) : ~0ull;
+            from_a.start(to, k, k1 - k, bits);
+            from_b.start(to + ABYTES, k, k1 - k, bits);
+        };
+        constexpr int PER = S::FM * S::FN, N = K / 16 * PER, READS = S::FM + S::FN, SETS = sizeof(T) == 2 ? 2 : 1;
+        auto step = [&](const char *now) {
+            F fa[SETS][S::FM], fb[SETS][S::FN];
+            auto read = [&](auto c0, auto r0) {
+                constexpr int c = c0, r = r0;
+                if constexpr (r < S::FM) fa[c % SETS][r] = fragment<T, S::BM, AA, true>(now, wm + 32 * r, c);
+                else fb[c % SETS][r - S::FM] = fragment<T, S::BN, BA, false>(now + ABYTES, wn + 32 * (r - S::FM), c);
+            };
+            span<0, READS>([&](auto r) { read(std::integral_constant<int, 0>(), r); });
+            __builtin_amdgcn_sched_barrier(0);
+            span<0, N>([&](auto n1) {
+                constexpr int n = n1, c = n / PER, i = n % PER;
+                if constexpr (SETS == 1 && c && i == 0) span<0, READS>([&](auto r) { read(std::integral_constant<int, c>(), r); });
+                mma(acc[i / S::FN][i % S::FN], fa[c % SETS][i / S::FN], fb[c % SETS][i % S::FN]);
+                if constexpr (SETS == 2 && c + 1 < K / 16)
+                    span<i * READS / PER, (i + 1) * READS / PER>([&](auto r) { read(std::integral_constant<int, c + 1>(), r); });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        int k = next(k0);
+        if (k < k1) bring(lds, k);
+        e.begin(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31));
+        char *now = lds, *then = lds + HALF;
+        while (k < k1) {
+            arrived();
+            __syncthreads();
+            const int after = next(k + K);
+            if (after < k1) bring(then, after);
+            step(now);
+            char *const swap = now;
+            now = then;
+            then = swap;
+            k = after;
+        }
+    }
+    e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), wave / S::WN + S::WM * at.m);
+}
+
+// ---- what becomes of a tile ----------------------------------------------------------
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+template <typename I> __device__ __forceinline__ int target_of(const I *targets, int n, int tokens, int vocab)
+{
+    if (n >= tokens) return -1;
+    const I t = targets[n];
+    return t >= 0 && t < (I)vocab ? (int)t : -1;
+}
+
+// Forward: for a wavefront's vocabulary rows the largest logit of each token and the sum of the exponentials over it; the
+// target's logit.
+template <typename I> struct Stats {
+    f32x2 *parts;                   // [part][tokens]
+    float *hit;                     // [tokens]
+    const I *targets;
+    int tokens, vocab, first, end_;         // the piece of the vocabulary: rows [first, end)
+    int part0;
+    __device__ __forceinline__ bool skip(int n0, int count) const
+    {
+        bool any = false;
+        for (int i = threadIdx.x; i < count; i += blockDim.x) any |= target_of(targets, n0 + i, tokens, vocab) >= 0;
+        return !__syncthreads_or(any);
+    }
+    template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int part) const
+    {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int t = n + 32 * j, target = target_of(targets, t, tokens, vocab) - first;
+            const int room = end_ - first - m, want = target - m;
+            float top = -INFINITY, at = 0;
+            bool mine = false;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (32 * i + r >= room) acc[i][j][r] = -INFINITY;
+                    top = fmaxf(top, acc[i][j][r]);
+                    if (32 * i + r == want) at = acc[i][j][r], mine = true;
+                }
+            if (mine) hit[t] = at;
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top == -INFINITY ? 0.0f : top;
+            float sum = 0;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E);
+            sum += __shfl_xor(sum, 32);
+            if ((threadIdx.x & 32) == 0 && t < tokens) parts[(int64_t)(part0 + part) * tokens + t] = f32x2{top, sum};
+        }
+    }
+};
+
+// Backward: dz of a piece of the vocabulary, rows of tokens `ld` apart; columns past the vocabulary and rows of tokens that take
+// no part are zeros.
+template <typename T, typename I> struct Slope {
+    T *dz;
+    int64_t ld;
+    const float *lse, *dloss;
+    const I *targets;
+    const uint64_t *live;
+    int tokens, vocab, first, end_;
+    __device__ __forceinline__ bool skip(int n0, int count) const
+    {
+        uint64_t any = 0;
+        for (int i = 0; i < count && n0 + i < tokens; i += 64) any |= ((Words)(uintptr_t)live)[(n0 + i) >> 6];
+        return any == 0;
+    }
+    template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int) const
+    {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int t = n + 32 * j;
+            if (t >= tokens) continue;
+            const int target = target_of(targets, t, tokens, vocab) - first;
+            const float up = dloss[t], base = lse[t];
+            const bool on = live[t >> 6] >> (t & 63) & 1;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                if (m + 32 * i >= ld) continue;
+                float f[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int v = m + 32 * i + r;
+                    const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E) - (v == target ? 1.0f : 0.0f);
+                    f[r] = on && v < end_ - first ? p * up : 0.0f;
+                }
+                T *row = dz + t * ld + m + 32 * i;
+#pragma unroll
+                for (int c = 0; c < 16; c += VE<T>) st16(row + c, narrow<T>(f + c));
+            }
+        }
+    }
+};
+
+// A sum in binary32 (pieces of k: one matrix for each), or the result.  `sums` rows are `lds` apart, a multiple of 16, and whole.
+template <typename G> struct Result {
+    G *out;                         // float: the sums themselves
+    int64_t ld, apart;              // rows; matrices of the pieces of k
+    const float *start;             // what the sums start from, or null; rows `lds` apart
+    int64_t lds;
+    const uint64_t *live;           // rows that are not zeros, or null: all
+    int rows, cols;                 // cols of the sums: up to a multiple of 16
+    __device__ __forceinline__ bool skip(int n0, int count) const
+    {
+        if (!live) return false;
+        uint64_t any = 0;
+        for (int i = 0; i < count && n0 + i < rows; i += 64) any |= ((Words)(uintptr_t)live)[(n0 + i) >> 6];
+        return any == 0;
+    }
+    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int m, int n) const
+    {
+        if (!start) return;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                if (n + 32 * j >= rows || m + 32 * i >= cols) continue;
+                const float *p = start + blockIdx.y * apart + (n + 32 * j) * lds + m + 32 * i;
+#pragma unroll
+                for (int c = 0; c < 16; c += 4) {
+                    const u32x4 v = *(const u32x4 *)(p + c);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][c + r] = as_f(v[r]);
+                }
+            }
+    }
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int) const
+    {
+        G *to = out + blockIdx.y * apart;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int row = n + 32 * j;
+            if (row >= rows) continue;
+            const bool on = !live || (live[row >> 6] >> (row & 63) & 1);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int c0 = m + 32 * i;
+                float f[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) f[r] = on ? acc[i][j][r] : 0.0f;
+#pragma unroll
+                for (int c = 0; c < 16; c += VE<G>) {
+                    if (c0 + c < cols) st_chunk(to + row * ld, c0 + c, cols, narrow<G>(f + c));
+                }
+            }
+        }
+    }
+};
+
+// ---- the small kernels beside them ---------------------------------------------------
+
+// Rows at multiples of 16 bytes for tensors that have none: zeros up to `ld`.
+template <typename T>
+__global__ __launch_bounds__(256) void kt_xent_align_kernel(const T *x, int64_t ldx, int cols, T *y, int64_t ld, int64_t rows)
+{
+    const int parts = (int)((ld + 64 * VE<T> - 1) / (64 * VE<T>));
+    for (int64_t n = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; n < rows * parts; n += (int64_t)gridDim.x * 4) {
+        const int64_t row = n / parts;
+        const int c = (int)(n % parts) * 64 * VE<T> + (threadIdx.x & 63) * VE<T>;
+        if (c < ld) *(u32x4 *)(y + row * ld + c) = ld_chunk(x + row * ldx, c, cols);
+    }
+}
+
+// lse and loss from the parts' largest values and sums: 256 / TOKENS lanes for a token, each a stretch of the parts.
+template <typename I, int TOKENS>
+__global__ __launch_bounds__(256) void kt_xent_join_kernel(const f32x2 *parts, int count, const float *hit, const I *targets, int tokens,
+                                                           int vocab, float *loss, float *lse)
+{
+    constexpr int EACH = 256 / TOKENS;
+    __shared__ f32x2 of[EACH][TOKENS];
+    const int i = threadIdx.x % TOKENS, w = threadIdx.x / TOKENS;
+    const int64_t t = (int64_t)blockIdx.x * TOKENS + i;
+    const bool on = t < tokens && target_of(targets, (int)min(t, (int64_t)INT32_MAX), tokens, vocab) >= 0;
+    float top = -INFINITY, sum = 0;
+    auto add = [&](f32x2 p) {
+        const float m = fmaxf(top, p[0]), base = m == -INFINITY ? 0.0f : m;
+        sum = sum * __builtin_amdgcn_exp2f((top - base) * LOG2E) + p[1] * __builtin_amdgcn_exp2f((p[0] - base) * LOG2E);
+        top = m;
+    };
+    if (on) {
+        const int each = (count + EACH - 1) / EACH, a = TOKENS == 1 ? w : w * each, b = TOKENS == 1 ? count : min(count, a + each);
+#pragma unroll 8
+        for (int k = a; k < b; k += TOKENS == 1 ? EACH : 1) add(parts[(int64_t)k * tokens + t]);
+    }
+    of[w][i] = f32x2{top, sum};
+    __syncthreads();
+    if (w || t >= tokens) return;
+    for (int k = 1; k < EACH; ++k) add(of[k][i]);
+    const float all = top + __builtin_amdgcn_logf(sum) * LN2;
+    loss[t] = on ? all - hit[t] : 0.0f;
+    if (lse) lse[t] = on ? all : 0.0f;
+}
+
+// A bit for every token that takes part.
+template <typename I>
+__global__ __launch_bounds__(256) void kt_xent_live_kernel(const I *targets, const float *dloss, int tokens, int vocab, uint64_t *live)
+{
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool on = t < tokens && target_of(targets, (int)min(t, (int64_t)INT32_MAX), tokens, vocab) >= 0 && dloss[t] != 0.0f;
+    const uint64_t word = __ballot(on);
+    if ((threadIdx.x & 63) == 0 && t < tokens) live[t >> 6] = word;
+}
+
+// The sum of pieces of k, in their order; rows of the pieces `ldp` apart.
+template <typename G>
+__global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, int pieces, int64_t apart, int ldp, int rows, int cols, G *out, int64_t ld)
+{
+    const int across = (cols + 3) / 4;
+    for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < (int64_t)rows * across; n += (int64_t)gridDim.x * 256) {
+        const int64_t row = n / across;
+        const int c = (int)(n % across) * 4;
+        const float *p = parts + row * ldp + c;
+        f32x4 s = *(const f32x4 *)p;
+        for (int k = 1; k < pieces; ++k) s += *(const f32x4 *)(p + k * apart);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < cols) out[row * ld + c + j] = (G)s[j];
+    }
+}
+
+// ---- how the work is cut ---------------------------------------------------------------
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int64_t over(int64_t n, int64_t by) { return (n + by - 1) / by; }
+
+// The tile's side for a product of m x n: the largest that makes 192 tiles.
+int side_of(kt_dtype dt, int64_t m, int64_t n)
+{
+    auto tiles = [&](int64_t s) { return over(m, s) * over(n, s); };
+    return dt == KT_BF16 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
+}
+// Pieces of k where the tiles are fewer than the CUs: 256 steps of k in a piece at least, 16 pieces at most.
+struct Pieces {
+    int count, piece;
+};
+Pieces pieces_of(kt_dtype dt, int64_t m, int64_t n, int64_t k)
+{
+    const int s = side_of(dt, m, n), step = dt == KT_F32 ? 32 : 64;
+    const int64_t tiles = over(m, s) * over(n, s);
+    int64_t p = tiles > 0 && tiles < 256 ? 512 / tiles : 1;
+    if (p > k / 256) p = k / 256;
+    if (p > 16) p = 16;
+    if (p < 2) return Pieces{1, (int)up(k < 1 ? 1 : k, 64)};
+    const int64_t piece = up(over(k, p), 64 > step ? 64 : step);
+    return Pieces{(int)over(k, piece), (int)piece};
+}
+
+// Whether loads of 16 bytes can take a matrix as it is: rows at multiples of 16 bytes, offsets within a tile of 31 bits.
+template <typename T> bool plain(const T *p, int64_t ld, int64_t width)
+{
+    return rows_of_16(p, ld) && width % VE<T> == 0 && ld * (int64_t)sizeof(T) <= 1 << 22;
+}
+
+// What a call needs of the workspace, and its cut.  Other matrices are copied to rows of a multiple of 16 bytes first (the weight up to 32 MiB of it
+// at a time), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
+struct Plan {
+    int64_t es, wide;               // bytes of an element; elements to a row of a copy
+    int64_t copy;                   // rows of the weight copied at a time
+    int64_t most, piece;            // rows of the vocabulary in a piece: with the weight as it is; with copies
+    int side;                       // forward
+    int64_t ldp;                    // backward: elements to a row of sums
+    Pieces kx;                      // of the vocabulary's pieces, for dx
+    int64_t x, w, parts, hit, dz, live, acc, sums, bytes;       // where in the workspace
+};
+int64_t at_most(int64_t a, int64_t b) { return a < b ? a : b; }
+// Rows of a multiple of 256 that keep rows * of below `most`.
+int64_t rows_in(int64_t most, int64_t of, int64_t vocab)
+{
+    int64_t r = most / (of < 1 ? 1 : of) / 256 * 256;
+    if (r < 256) r = 256;
+    return at_most(r, up(vocab, 256));
+}
+Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd)
+{
+    Plan p{};
+    p.es = dt == KT_F32 ? 4 : 2;
+    p.wide = up(width, 64);
+    p.copy = rows_in(32 << 20, p.wide * p.es, vocab);
+    // backward: dz of up to 2^27 elements, 256 MiB of bf16, what the last-level cache holds; forward: a launch of up to 2^20 tiles of 256
+    p.most = rows_in(bwd ? 1ll << 27 : 1ll << 36, tokens, vocab);
+    if (bwd) p.most = at_most(p.most, 1 << 18);
+    p.piece = at_most(p.most, p.copy);
+    p.side = side_of(dt, vocab, tokens);
+    p.ldp = up(width, 16);
+    auto take = [&](int64_t bytes) {
+        const int64_t from = p.bytes;
+        p.bytes += up(bytes, 256);
+        return from;
+    };
+    p.x = take(tokens * p.wide * p.es);
+    p.w = take(p.piece * p.wide * p.es);
+    if (!bwd) {
+        p.parts = take(over(vocab, p.side) * 2 * tokens * 8);
+        p.hit = take(tokens * 4);
+        return p;
+    }
+    p.live = take(over(tokens, 64) * 8);
+    p.dz = take(tokens * p.most * p.es);
+    p.kx = pieces_of(dt, width, tokens, at_most(p.most, vocab));
+    if (p.kx.count > 1 || p.piece < vocab) p.acc = take(p.kx.count * tokens * p.ldp * 4);
+    // the weight's gradient, cut over the tokens: whichever of the two pieces takes more
+    int64_t most = 0;
+    for (int64_t rows : {at_most(p.most, vocab), at_most(p.piece, vocab), vocab % p.most, vocab % p.piece}) {
+        if (rows == 0) continue;
+        const Pieces k = pieces_of(dt, width, rows, tokens);
+        if (k.count > 1 && k.count * rows > most) most = k.count * rows;
+    }
+    p.sums = take(most * p.ldp * 4);
+    return p;
+}
+
+template <typename T, typename S, bool AA, bool BA, typename E>
+int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Pieces &k, const uint64_t *live, const E &e, hipStream_t s)
+{
+    constexpr int LDS = 2 * (S::BM + S::BN) * 128;
+    const auto kernel = kt_xent_product_kernel<T, S, AA, BA, E>;
+    if (LDS > 65536) {
+        const hipError_t e1 = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        if (e1 != hipSuccess) return (int)e1;
+    }
+    const int64_t mt = over(m, S::BM), nt = over(n, S::BN);
+    kernel<<<dim3((unsigned)(mt * nt), (unsigned)k.count), S::BLOCK, LDS, s>>>(a, b, (int)steps, k.piece, live, (int)mt, (int)nt, e);
+    return (int)hipGetLastError();
+}
+// The product of A [m x steps] and B [n x steps] in tiles of `side`.
+template <typename T, bool AA, bool BA, typename E>
+int product(int side, const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Pieces &k, const uint64_t *live, const E &e,
+            hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (side == 256) return launch_tiles<T, Big, AA, BA>(a, m, b, n, steps, k, live, e, s);
+    }
+    if (side == 128) return launch_tiles<T, Mid, AA, BA>(a, m, b, n, steps, k, live, e, s);
+    return launch_tiles<T, Small, AA, BA>(a, m, b, n, steps, k, live, e, s);
+}
+
+#define KT_GO(call)                    \
+    do {                               \
+        const int go_ = (call);        \
+        if (go_) return go_;           \
+    } while (0)
+
+// x or rows of w as the products take them: as they are, or copied.
+template <typename T> int aligned_rows(bool as_is, const T *x, int64_t ldx, int64_t width, int64_t rows, T *copy, int64_t wide, Operand<T> *to, hipStream_t s)
+{
+    to->count = (int)rows;
+    if (as_is) {
+        to->p = x;
+        to->ld = ldx;
+        return 0;
+    }
+    to->p = copy;
+    to->ld = wide;
+    if (rows == 0) return 0;
+    const int64_t blocks = over(rows * over(wide, 64 * VE<T>), 4);
+    kt_xent_align_kernel<T><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, rows);
+    return (int)hipGetLastError();
+}
+
+template <typename T, typename I>
+int fwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, int64_t ldx, const T *w, int64_t ldw, const I *targets, float *loss,
+        float *lse, char *ws, hipStream_t s)
+{
+    const Plan p = plan_of(dt, tokens, vocab, width, false);
+    f32x2 *parts = (f32x2 *)(ws + p.parts);
+    float *hit = (float *)(ws + p.hit);
+    const bool w_as_is = plain(w, ldw, width);
+    Operand<T> a, b;
+    KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
+    for (int64_t v = 0, rows; v < vocab; v += rows) {
+        rows = at_most(w_as_is ? p.most : p.piece, vocab - v);
+        KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
+        const Stats<I> e{parts, hit, targets, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / (p.side / 2))};
+        KT_GO((product<T, true, true>(p.side, a, rows, b, tokens, width, Pieces{1, (int)up(width, 64)}, nullptr, e, s)));
+    }
+    const int count = (int)over(vocab, p.side) * 2;
+    if (tokens >= 512) kt_xent_join_kernel<I, 32><<<(unsigned)over(tokens, 32), 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
+    else kt_xent_join_kernel<I, 1><<<(unsigned)tokens, 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
+    return (int)hipGetLastError();
+}
+
+template <typename G> int sum(const float *parts, const Pieces &k, int64_t apart, int64_t ldp, int64_t rows, int64_t cols, G *out, int64_t ld, hipStream_t s)
+{
+    const int64_t blocks = over(rows * over(cols, 4), 256);
+    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.count, apart, (int)ldp, (int)rows, (int)cols, out, ld);
+    return (int)hipGetLastError();
+}
+
+template <typename T, typename I>
+int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *dloss, const T *x, int64_t ldx, const T *w, int64_t ldw,
+        const I *targets, const float *lse, T *dx, int64_t lddx, T *dw, int64_t lddw, char *ws, hipStream_t s)
+{
+    const Plan p = plan_of(dt, tokens, vocab, width, true);
+    uint64_t *live = (uint64_t *)(ws + p.live);
+    T *dz = (T *)(ws + p.dz);
+    float *acc = (float *)(ws + p.acc), *sums = (float *)(ws + p.sums);
+    const bool w_as_is = plain(w, ldw, width);
+    const int64_t cols = up(width, VE<T>);              // of an operand: what a copy has past the width is zeros
+    const int64_t piece = w_as_is ? p.most : p.piece;
+    Operand<T> a, b;
+    KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
+    if (tokens) {
+        kt_xent_live_kernel<I><<<(unsigned)over(tokens, 256), 256, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, live);
+        KT_GO((int)hipGetLastError());
+    }
+    for (int64_t v = 0, rows; v < vocab; v += rows) {
+        rows = at_most(piece, vocab - v);
+        if (tokens) {
+            KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
+            const Slope<T, I> e{dz, p.most, lse, dloss, targets, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
+            KT_GO((product<T, true, true>(side_of(dt, rows, tokens), a, rows, b, tokens, width, Pieces{1, (int)up(width, 64)}, nullptr, e, s)));
+        }
+        if (dx && tokens) {
+            const Operand<T> wide{a.p, a.ld, (int)cols}, slope{dz, p.most, (int)tokens};
+            const bool first = v == 0, last = v + rows == vocab;
+            const int64_t apart = tokens * p.ldp;
+            const int side = side_of(dt, width, tokens);
+            if (last && p.kx.count == 1) {
+                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, p.ldp, live, (int)tokens, (int)width};
+                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, p.kx, nullptr, e, s)));
+            } else {
+                const Result<float> e{acc, p.ldp, apart, first ? nullptr : acc, p.ldp, live, (int)tokens, (int)p.ldp};
+                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, p.kx, nullptr, e, s)));
+                if (last) KT_GO(sum(acc, p.kx, apart, p.ldp, tokens, width, dx, lddx, s));
+            }
+        }
+        if (dw) {
+            const Operand<T> wide{b.p, b.ld, (int)cols}, slope{dz, p.most, (int)up(rows, VE<T>)};
+            const Pieces k = pieces_of(dt, width, rows, tokens);
+            const int side = side_of(dt, width, rows);
+            if (k.count == 1) {
+                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, 0, nullptr, (int)rows, (int)width};
+                KT_GO((product<T, false, false>(side, wide, width, slope, rows, tokens, k, live, e, s)));
+            } else {
+                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, 0, nullptr, (int)rows, (int)p.ldp};
+                KT_GO((product<T, false, false>(side, wide, width, slope, rows, tokens, k, live, e, s)));
+                KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, s));
+            }
+        }
+    }
+    return 0;
+}
+
+template <typename F> int by_types(kt_dtype dt, kt_index it, F f)
+{
+    auto index = [&](auto t) { return it == KT_I32 ? f(t, int32_t()) : f(t, int64_t()); };
+    return dt == KT_F32 ? index(float()) : index(bf16());
+}
+
+}  // namespace
+
+int64_t kt_linear_xent_ws(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd) { return plan_of(dt, tokens, vocab, width, bwd).bytes; }
+
+int kt_launch_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t vocab, int64_t width, const void *x, int64_t ldx, const void *w,
+                              int64_t ldw, const void *targets, float *loss, float *lse, void *ws, void *stream)
+{
+    return by_types(dt, it, [&](auto t, auto i) {
+        typedef decltype(t) T;
+        return fwd(dt, tokens, vocab, width, (const T *)x, ldx, (const T *)w, ldw, (const decltype(i) *)targets, loss, lse, (char *)ws, (hipStream_t)stream);
+    });
+}
+
+int kt_launch_linear_xent_bwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t vocab, int64_t width, const float *dloss, const void *x, int64_t ldx,
+                              const void *w, int64_t ldw, const void *targets, const float *lse, void *dx, int64_t lddx, void *dw, int64_t lddw,
+                              void *ws, void *stream)
+{
+    return by_types(dt, it, [&](auto t, auto i) {
+        typedef decltype(t) T;
+        return bwd(dt, tokens, vocab, width, dloss, (const T *)x, ldx, (const T *)w, ldw, (const decltype(i) *)targets, lse, (T *)dx, lddx, (T *)dw, lddw, (char *)ws, (hipStream_t)stream);
+    });
+}

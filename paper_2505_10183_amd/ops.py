@@ -58,8 +58,14 @@ def _library() -> ctypes.CDLL:
         L.kt_embedding_bwd_workspace.argtypes = [i64, i64, i64]
         L.kt_embedding_bwd_workspace.restype = i64
         L.kt_embedding_bwd.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, f32, vp, i64, i32, vp, i64, vp]
+        for n in ("kt_linear_xent_fwd_workspace", "kt_linear_xent_bwd_workspace"):
+            getattr(L, n).argtypes = [i32, i64, i64, i64]
+            getattr(L, n).restype = i64
+        L.kt_linear_xent_fwd.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]
+        L.kt_linear_xent_bwd.argtypes = [i32, i32, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp]
         for n in ("kt_layernorm_fwd", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore", "kt_act8_weight_grad",
-                  "kt_attention_fwd", "kt_attention_bwd", "kt_embedding_fwd", "kt_embedding_bwd"):
+                  "kt_attention_fwd", "kt_attention_bwd", "kt_embedding_fwd", "kt_embedding_bwd",
+                  "kt_linear_xent_fwd", "kt_linear_xent_bwd"):
             getattr(L, n).restype = i32
         _lib = L
     return L
@@ -68,7 +74,8 @@ def _library() -> ctypes.CDLL:
 _plain_of = {}      # the native calls of each loaded library
 _ENTRIES = ("kt_layernorm_fwd", "kt_layernorm_bwd_workspace", "kt_layernorm_bwd", "kt_act8_save", "kt_act8_restore",
             "kt_act8_weight_grad_workspace", "kt_act8_weight_grad", "kt_attention_fwd", "kt_attention_bwd_workspace", "kt_attention_bwd",
-            "kt_embedding_fwd", "kt_embedding_bwd_workspace", "kt_embedding_bwd")
+            "kt_embedding_fwd", "kt_embedding_bwd_workspace", "kt_embedding_bwd",
+            "kt_linear_xent_fwd_workspace", "kt_linear_xent_fwd", "kt_linear_xent_bwd_workspace", "kt_linear_xent_bwd")
 
 
 def _plainly(name: str, *args) -> bool:
@@ -352,5 +359,54 @@ def kt_embedding_bwd(ids, dy, dw, scale: float = 1.0, accumulate: bool = False, 
     ws, size, held = _workspace(workspace, L.kt_embedding_bwd_workspace(tokens, vocab, width), stream, dy.device)
     status = L.kt_embedding_bwd(_type(dy, "dy"), _type(dw, "dw"), it, tokens, vocab, width, pi, p, ld, scale, pw, ldw, 1 if accumulate else 0, ws, size,
                                 _stream(stream))
+    if status:
+        _check(status, L)
+
+
+def kt_linear_xent_fwd_workspace(dtype, tokens: int, vocab: int, width: int) -> int:
+    return _library().kt_linear_xent_fwd_workspace(_TYPES[dtype], tokens, vocab, width)
+
+
+def kt_linear_xent_fwd(x, w, targets, loss, lse=None, workspace=None, stream=None):
+    """loss = lse - z[target], lse = log of the sum of exp(z), z = x w^T for x [tokens, width] and w [vocab, width], a value a token (float32); the
+    logits are nowhere kept.  targets: int32 or int64; one outside [0, vocab) is none, loss and lse are 0 there.  lse: what the
+    backward pass needs."""
+    if _plainly("linear_xent_fwd", x, w, targets, loss, lse, workspace, stream):
+        return
+    L = _library()
+    px, tokens, width, ldx = _matrix(x, "x")
+    pw, vocab, cols, ldw = _matrix(w, "w")
+    if cols != width or w.dtype != x.dtype:
+        raise ValueError("w: %d columns of %s are needed, got %d of %s" % (width, x.dtype, cols, w.dtype))
+    t = _type(x, "x")
+    it, pt = _ids(targets, tokens, "targets")
+    ws, size, held = _workspace(workspace, L.kt_linear_xent_fwd_workspace(t, tokens, vocab, width), stream, x.device)
+    status = L.kt_linear_xent_fwd(t, it, tokens, vocab, width, px, ldx, pw, ldw, pt, _vector(loss, tokens, torch.float32, "loss"),
+                                  _vector(lse, tokens, torch.float32, "lse"), ws, size, _stream(stream))
+    if status:
+        _check(status, L)
+
+
+def kt_linear_xent_bwd_workspace(dtype, tokens: int, vocab: int, width: int) -> int:
+    return _library().kt_linear_xent_bwd_workspace(_TYPES[dtype], tokens, vocab, width)
+
+
+def kt_linear_xent_bwd(dloss, x, w, targets, lse, dx=None, dw=None, workspace=None, stream=None):
+    """Gradients of x and w from that of each token's loss; x, w, targets and lse as kt_linear_xent_fwd had and left them.  dx and dw have x's
+    type; one of them may be None (not wanted); dw may lie in a bucket."""
+    if _plainly("linear_xent_bwd", dloss, x, w, targets, lse, dx, dw, workspace, stream):
+        return
+    L = _library()
+    px, tokens, width, ldx = _matrix(x, "x")
+    pw, vocab, cols, ldw = _matrix(w, "w")
+    if cols != width or w.dtype != x.dtype:
+        raise ValueError("w: %d columns of %s are needed, got %d of %s" % (width, x.dtype, cols, w.dtype))
+    t = _type(x, "x")
+    it, pt = _ids(targets, tokens, "targets")
+    pdx, lddx = (0, width) if dx is None else _like(dx, tokens, width, x.dtype, "dx")
+    pdw, lddw = (0, width) if dw is None else _like(dw, vocab, width, x.dtype, "dw")
+    ws, size, held = _workspace(workspace, L.kt_linear_xent_bwd_workspace(t, tokens, vocab, width), stream, x.device)
+    status = L.kt_linear_xent_bwd(t, it, tokens, vocab, width, _vector(dloss, tokens, torch.float32, "dloss"), px, ldx, pw, ldw, pt,
+                                  _vector(lse, tokens, torch.float32, "lse"), pdx, lddx, pdw, lddw, ws, size, _stream(stream))
     if status:
         _check(status, L)
