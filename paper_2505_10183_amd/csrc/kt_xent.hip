@@ -16,22 +16,25 @@ namespace {
 // ---- a product ---------------------------------------------------------------------
 //
 // D[m][n] = sum_k A(m, k) B(n, k), a workgroup for a tile of BM x BN.  An operand is `along` k (k adjacent in memory) or across it (m or n
-// adjacent).  Its tiles of K steps of k are brought by loads that write LDS themselves, those of the next step beside the products of this one.
-// k runs 16 c + 8 h + j over the element j of chunk c, for both kinds.  The 32 rows of a fragment of A are taken in an order that
+// adjacent).  Its tiles of STEP k are brought by loads that write LDS themselves, some steps ahead, into slots that take turns.  The barrier
+// before a step's last products says that all of it is read (its slot is free again) and that the next one has arrived, so that the fragments of the next step's
+// first products are read beside the last products of this one: the matrix cores wait for nothing but the barrier itself.
+// A fragment is 16 bytes a lane for both types: lane l holds V of k (V c + ... : chunk c of a step, half h = l / 32, k = V (2 c + h) + j) of its row.  The 32 rows of a fragment of A are taken in an order that
 // gives a lane of D 16 neighbouring m: register r of half h is row 16 h + r.
 
 // Row of the matrix that row i of a fragment holds.
 __device__ __forceinline__ int spread_of(int i) { return (i >> 2 & 1) * 16 + (i >> 3) * 4 + (i & 3); }
 
 // Tile and wavefronts: WM x WN of them, each FM x FN products of 32 x 32.
-template <int WM_, int WN_, int FM_, int FN_> struct Shape {
-    static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_;
+template <int WM_, int WN_, int FM_, int FN_, int SLOTS_> struct Shape {
+    static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, SLOTS = SLOTS_;
     static constexpr int BM = WM * FM * 32, BN = WN * FN * 32, BLOCK = WM * WN * 64;
 };
-typedef Shape<2, 4, 4, 2> Big;      // 256 x 256, 8 wavefronts, 128 KiB of LDS
-typedef Shape<2, 2, 2, 2> Mid;      // 128 x 128, 4,  64 KiB
-typedef Shape<2, 2, 1, 1> Small;    //  64 x  64, 4,  32 KiB
-template <typename T> constexpr int STEP = 128 / (int)sizeof(T);       // k of a step
+typedef Shape<2, 4, 4, 2, 2> Big;       // 256 x 256, 8 wavefronts, 128 KiB of LDS
+typedef Shape<2, 2, 2, 2, 2> Mid;       // 128 x 128, 4,  64 KiB
+typedef Shape<2, 2, 1, 1, 2> Small;     //  64 x  64, 4,  32 KiB
+constexpr int ROW = 128;                                                // bytes of k in a step: a line
+template <typename T> constexpr int STEP = ROW / (int)sizeof(T);       // k of a step
 
 template <typename T> struct Operand {
     const T *p;
@@ -40,10 +43,12 @@ template <typename T> struct Operand {
 };
 
 typedef const uint64_t __attribute__((address_space(4))) *Words;
-// Which of the tokens from k on take part, a bit each; null: all of them.
-__device__ __forceinline__ uint64_t live_of(Words live, int k)
+// Which of the tokens of the step at k take part, a bit each; null: all of them.
+template <typename T> __device__ __forceinline__ uint64_t live_of(Words live, int k)
 {
-    return live ? live[k >> 6] >> (k & 63) : ~0ull;
+    if (!live) return ~0ull;
+    if constexpr (STEP<T> == 64) return live[k >> 6];
+    else return live[k >> 6] >> (k & 63) & 0xffffffffu;
 }
 
 // Tiles of one operand on their way from memory to LDS, SIDE of m or n by STEP of k.
@@ -68,9 +73,12 @@ template <typename T, int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct Bring
             at[u] = (ALONG ? row : c) < count ? (row * (int)ld + c) * (int)sizeof(T) : INT32_MIN;
         }
     }
-    // Starts bringing the steps from k on into `tile`; `left`: steps until the end.  What lies past an end is zeros and is not read, and so
+    // The steps from k on, `left` of them until the end, into `tile`, as N loads one by one.  What lies past an end is zeros and is not read, and so
     // are steps whose bit of `live` is 0 (across only).
-    __device__ __forceinline__ void start(char *tile, int k, int left, uint64_t live)
+    u32x4 rs;
+    uint32_t to;
+    uint64_t live;
+    __device__ __forceinline__ void aim(char *tile, int k, int left, uint64_t live_)
     {
         const int up = (min(left, K) + V - 1) / V * V;
         if (ALONG && left < K) {
@@ -78,29 +86,40 @@ template <typename T, int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct Bring
             for (int u = 0; u < N; ++u)
                 if (col_of(u) >= up) at[u] = INT32_MIN;
         }
-        const T *from = ALONG ? p + k : p + k * ld;
+        const uint64_t base = (uint64_t)(ALONG ? p + k : p + k * ld);
         const int bytes = (ALONG ? (count - 1) * (int)ld + up : (min(left, K) - 1) * (int)ld + count) * (int)sizeof(T);
-        const uint64_t base = (uint64_t)from;
-        const u32x4 rs{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
-        const uint32_t to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
-#pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int off = ALONG || (live >> row_of(u) & 1) ? at[u] : INT32_MIN;
-            // as Feed::bring
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                         :: "s"(to + u * BLOCK * 16), "v"(off), "s"(rs) : "memory");
-        }
+        rs = u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+        to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
+        live = live_;
+    }
+    __device__ __forceinline__ void load(int u) const
+    {
+        const int off = ALONG || (live >> row_of(u) & 1) ? at[u] : INT32_MIN;
+        // as Feed::bring
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :: "s"(to + u * BLOCK * 16), "v"(off), "s"(rs) : "memory");
     }
 };
 
+template <typename T> struct Part;
+template <> struct Part<bf16> { typedef bf16x8 type; };
+template <> struct Part<float> { typedef f32x4 type; };
+__device__ __forceinline__ void multiply(f32x16 &d, bf16x8 a, bf16x8 b) { mma(d, a, b); }
+__device__ __forceinline__ void multiply(f32x16 &d, f32x4 a, f32x4 b)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], d, 0, 0, 0);
+}
+
 // Fragment of 32 m or n from `first` on, chunk c of the step.
 template <typename T, int SIDE, bool ALONG, bool SPREAD>
-__device__ __forceinline__ typename Frag<T>::type fragment(const char *tile, int first, int c)
+__device__ __forceinline__ typename Part<T>::type fragment(const char *tile, int first, int c)
 {
+    const int l = threadIdx.x & 63, h = l >> 5;
     if constexpr (ALONG) {
-        return load_r<T, STEP<T>>(tile, first, c);
+        return *(const typename Part<T>::type *)(tile + Tile<T, STEP<T>>::at(first + (l & 31), 2 * c + h));
     } else if constexpr (sizeof(T) == 2) {
-        const int l = threadIdx.x & 63, h = l >> 5, g = l >> 4 & 1, i = l & 15, j = i & 3;
+        const int g = l >> 4 & 1, i = l & 15, j = i & 3;
         const int col = first + (SPREAD ? g * 8 + (j & 1) * 16 + (j >> 1) * 4 : g * 16 + j * 4);
         s16x4 v[2];
 #pragma unroll
@@ -111,27 +130,32 @@ __device__ __forceinline__ typename Frag<T>::type fragment(const char *tile, int
         }
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-        const int l = threadIdx.x & 63, h = l >> 5, col = first + (SPREAD ? spread_of(l & 31) : l & 31);
-        f32x8 v;
+        const int col = first + (SPREAD ? spread_of(l & 31) : l & 31);
+        f32x4 v;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int row = 16 * c + 8 * h + j;
-            v[j] = *(const float *)(tile + Tile<T, SIDE>::at(row, col >> 2) + (col & 3) * 4);
-        }
+        for (int j = 0; j < 4; ++j) v[j] = *(const float *)(tile + Tile<T, SIDE>::at(8 * c + 4 * h + j, col >> 2) + (col & 3) * 4);
         return v;
     }
 }
 
-// Tile number `b` of mt x nt: those of one XCD (every eighth workgroup) follow each other, in blocks of 8 n by as many m as
+// Tile number `b` of mt x nt: those of one XCD (every eighth workgroup) follow each other, in blocks of ACROSS n by as many m as
 // are at work, so that its L2 keeps their operands.
 struct Place {
     int m, n;
 };
+constexpr int ACROSS = 4;
 __device__ __forceinline__ Place place(int b, int mt, int nt)
 {
     const int all = mt * nt, q = all / 8, r = all % 8, x = b % 8, i = x * q + min(x, r) + b / 8;
-    const int group = i / (8 * mt), wide = min(8, nt - group * 8), j = i - group * 8 * mt;
-    return Place{j / wide, group * 8 + j % wide};
+    const int group = i / (ACROSS * mt), wide = min(ACROSS, nt - group * ACROSS), j = i - group * ACROSS * mt;
+    return Place{j / wide, group * ACROSS + j % wide};
+}
+
+// Until all but LATER of this wavefront's loads into LDS have arrived and it has read what it asked LDS for, and until all wavefronts are here.
+template <int LATER> __device__ __forceinline__ void meet()
+{
+    static_assert(LATER < 16, "the low four bits of vmcnt");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LATER) : "memory");
 }
 
 // E: what becomes of the tile.  E::skip(n0, count): nothing to multiply;  E::begin(acc, ...) the sums' start;  E::end(acc, ...).
@@ -141,9 +165,9 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
     constexpr int K = STEP<T>;
     typedef Bring<T, S::BM, S::BLOCK, AA, true> BringA;
     typedef Bring<T, S::BN, S::BLOCK, BA, false> BringB;
-    typedef typename Frag<T>::type F;
-    constexpr int ABYTES = S::BM * 128, HALF = (S::BM + S::BN) * 128;
-    extern __shared__ __align__(16) char lds[];             // two halves
+    typedef typename Part<T>::type F;
+    constexpr int ABYTES = S::BM * ROW, SLOT = (S::BM + S::BN) * ROW, LOADS = BringA::N + BringB::N, SLOTS = S::SLOTS;
+    extern __shared__ __align__(16) char lds[];             // SLOTS slots
 
     const Words live = (Words)(uintptr_t)live_;
     const int wave = wave_id(), lane = threadIdx.x & 63;
@@ -152,63 +176,77 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
     const int k0 = blockIdx.y * piece, k1 = min(steps, k0 + piece);
 
     f32x16 acc[S::FM][S::FN];
-    auto each = [&](auto f) {
 #pragma unroll
-        for (int n = 0; n < S::FN; ++n)
+    for (int m = 0; m < S::FM; ++m)
 #pragma unroll
-            for (int m = 0; m < S::FM; ++m) f(m, n);
-    };
-    each([&](int m, int n) { acc[m][n] = f32x16{0}; });
+        for (int n = 0; n < S::FN; ++n) acc[m][n] = f32x16{0};
     if (!e.skip(n0, S::BN)) {
         BringA from_a(a, m0);
         BringB from_b(b, n0);
         // the next step that has a live token
         auto next = [&](int k) {
             if constexpr (!AA && !BA)
-                while (k < k1 && (live_of(live, k) & (K == 64 ? ~0ull : 0xffffffffull)) == 0) k += K;
+                while (k < k1 && live_of<T>(live, k) == 0) k += K;
             return k;
         };
-        auto bring = [&](char *to, int k) {
-            const uint64_t bits = !AA && !BA ? live_of(live, k) : ~0ull;
-            from_a.start(to, k, k1 - k, bits);
-            from_b.start(to + ABYTES, k, k1 - k, bits);
+        auto aim = [&](char *to, int k) __attribute__((always_inline)) {
+            const uint64_t bits = !AA && !BA ? live_of<T>(live, k) : ~0ull;
+            from_a.aim(to, k, k1 - k, bits);
+            from_b.aim(to + ABYTES, k, k1 - k, bits);
         };
-        constexpr int PER = S::FM * S::FN, N = K / 16 * PER, READS = S::FM + S::FN, SETS = sizeof(T) == 2 ? 2 : 1;
-        auto step = [&](const char *now) {
-            F fa[SETS][S::FM], fb[SETS][S::FN];
-            auto read = [&](auto c0, auto r0) {
-                constexpr int c = c0, r = r0;
-                if constexpr (r < S::FM) fa[c % SETS][r] = fragment<T, S::BM, AA, true>(now, wm + 32 * r, c);
-                else fb[c % SETS][r - S::FM] = fragment<T, S::BN, BA, false>(now + ABYTES, wn + 32 * (r - S::FM), c);
-            };
-            span<0, READS>([&](auto r) { read(std::integral_constant<int, 0>(), r); });
-            __builtin_amdgcn_sched_barrier(0);
-            span<0, N>([&](auto n1) {
+        auto load = [&](auto u0) __attribute__((always_inline)) {
+            constexpr int u = u0;
+            if constexpr (u < BringA::N) from_a.load(u);
+            else from_b.load(u - BringA::N);
+        };
+        constexpr int PER = S::FM * S::FN, CHUNKS = ROW / 32, READS = S::FM + S::FN;
+        static_assert(CHUNKS % 2 == 0, "two sets of fragments take turns");
+        F fa[2][S::FM], fb[2][S::FN];
+        // fragment number r of a chunk, in the order in which the products need them
+        auto read = [&](const char *slot, auto c0, auto r0) __attribute__((always_inline)) {
+            constexpr int c = c0, r = r0;
+            if constexpr (r == 0) fa[c % 2][0] = fragment<T, S::BM, AA, true>(slot, wm, c);
+            else if constexpr (r <= S::FN) fb[c % 2][r - 1] = fragment<T, S::BN, BA, false>(slot + ABYTES, wn + 32 * (r - 1), c);
+            else fa[c % 2][r - S::FN] = fragment<T, S::BM, AA, true>(slot, wm + 32 * (r - S::FN), c);
+        };
+        int k = next(k0), ahead = 0;            // the next step to bring; steps brought and not done
+        for (; ahead < SLOTS && k < k1; ++ahead, k = next(k + K)) {
+            aim(lds + ahead * SLOT, k);
+            span<0, LOADS>(load);
+        }
+        e.begin(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31));
+        meet<0>();
+        span<0, READS>([&](auto r) { read(lds, std::integral_constant<int, 0>(), r); });
+        __builtin_amdgcn_sched_barrier(0);
+        for (int slot = 0; ahead > 0;) {
+            const int after = slot + 1 == SLOTS ? 0 : slot + 1;
+            char *const now = lds + slot * SLOT, *const then = lds + after * SLOT;
+            const bool more = k < k1;
+            span<0, CHUNKS * PER>([&](auto n1) {
                 constexpr int n = n1, c = n / PER, i = n % PER;
-                if constexpr (SETS == 1 && c && i == 0) span<0, READS>([&](auto r) { read(std::integral_constant<int, c>(), r); });
-                mma(acc[i / S::FN][i % S::FN], fa[c % SETS][i / S::FN], fb[c % SETS][i % S::FN]);
-                if constexpr (SETS == 2 && c + 1 < K / 16)
-                    span<i * READS / PER, (i + 1) * READS / PER>([&](auto r) { read(std::integral_constant<int, c + 1>(), r); });
+                if constexpr (c == CHUNKS - 1 && i == 0) {
+                    if (ahead == SLOTS) meet<(SLOTS - 2) * LOADS>();
+                    else meet<0>();
+                    if (more) aim(now, k);
+                }
+                multiply(acc[i / S::FN][i % S::FN], fa[c % 2][i / S::FN], fb[c % 2][i % S::FN]);
+                // beside each product from the first on, so that the last ones are there for the next chunk's first products
+                constexpr int RATE = (READS + PER - 1) / PER;
+                span<(i * RATE < READS ? i * RATE : READS), ((i + 1) * RATE < READS ? (i + 1) * RATE : READS)>([&](auto r) {
+                    read(c + 1 < CHUNKS ? now : then, std::integral_constant<int, (c + 1) % CHUNKS>(), r);
+                });
+                if constexpr (c == CHUNKS - 1) {
+                    if (more) span<i * LOADS / PER, (i + 1) * LOADS / PER>(load);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             });
-        };
-        int k = next(k0);
-        if (k < k1) bring(lds, k);
-        e.begin(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31));
-        char *now = lds, *then = lds + HALF;
-        while (k < k1) {
-            arrived();
-            __syncthreads();
-            const int after = next(k + K);
-            if (after < k1) bring(then, after);
-            step(now);
-            char *const swap = now;
-            now = then;
-            then = swap;
-            k = after;
+            if (more) k = next(k + K);
+            else --ahead;
+            slot = after;
         }
     }
-    e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), wave / S::WN + S::WM * at.m);
+    if constexpr (E::ROWS) __syncthreads();                 // LDS is read: the epilogue takes it
+    e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), wave / S::WN + S::WM * at.m, lds + wave * (32 * S::FM * 32 * 4));
 }
 
 // ---- what becomes of a tile ----------------------------------------------------------
@@ -222,9 +260,36 @@ template <typename I> __device__ __forceinline__ int target_of(const I *targets,
     return t >= 0 && t < (I)vocab ? (int)t : -1;
 }
 
+// 32 rows (lanes) of FM * 32 columns to memory in whole lines: each lane's 16 neighbouring columns go into this wavefront's part of LDS and
+// come back a row after the other.  The chunks of a row are exchanged, so that lanes of different rows use different banks.
+// f(i, values): the 16 values of column 32 i + 16 h on;  out: the matrix at the first row and column;  rows, cols: what of it is there.
+template <int FM, typename G, typename F> __device__ __forceinline__ void store_rows(char *scratch, G *out, int64_t ld, int rows, int cols, F f)
+{
+    constexpr int CHUNKS = FM * 32 / VE<G>;
+    static_assert((CHUNKS & (CHUNKS - 1)) == 0, "chunks of a row are exchanged among a power of two");
+    const int lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
+    u32x4 *const to = (u32x4 *)scratch;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        float v[16];
+        f(i, v);
+#pragma unroll
+        for (int c = 0; c < 16; c += VE<G>) to[l * CHUNKS + (((32 * i + 16 * h + c) / VE<G>) ^ (l & (CHUNKS - 1)))] = narrow<G>(v + c);
+    }
+    __builtin_amdgcn_wave_barrier();                        // of one wavefront: LDS serves it in order
+#pragma unroll
+    for (int u = 0; u < 32 * CHUNKS / 64; ++u) {
+        const int n = u * 64 + lane, row = n / CHUNKS, c = n % CHUNKS;
+        const u32x4 v = to[row * CHUNKS + (c ^ (row & (CHUNKS - 1)))];
+        if (row < rows && c * VE<G> < cols) st_chunk(out + row * ld, c * VE<G>, cols, v);
+    }
+}
+
 // Forward: for a wavefront's vocabulary rows the largest logit of each token and the sum of the exponentials over it; the
 // target's logit.
 template <typename I> struct Stats {
+    static constexpr bool ROWS = false;
     f32x2 *parts;                   // [part][tokens]
     float *hit;                     // [tokens]
     const I *targets;
@@ -237,23 +302,27 @@ template <typename I> struct Stats {
         return !__syncthreads_or(any);
     }
     template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int part) const
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int part, char *) const
     {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int t = n + 32 * j, target = target_of(targets, t, tokens, vocab) - first;
-            const int room = end_ - first - m, want = target - m;
-            float top = -INFINITY, at = 0;
-            bool mine = false;
+            const int t = n + 32 * j, want = target_of(targets, t, tokens, vocab) - first - m, room = end_ - first - m;
+            float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+            for (int i = 0; i < FM; ++i) {
+                if (room < 32 * i + 16) {                   // past the vocabulary
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (32 * i + r >= room) acc[i][j][r] = -INFINITY;
-                    top = fmaxf(top, acc[i][j][r]);
-                    if (32 * i + r == want) at = acc[i][j][r], mine = true;
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = 32 * i + r >= room ? -INFINITY : acc[i][j][r];
                 }
-            if (mine) hit[t] = at;
+                if ((uint32_t)(want - 32 * i) < 16) {
+                    float at = 0;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) at = 32 * i + r == want ? acc[i][j][r] : at;
+                    hit[t] = at;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+            }
             top = fmaxf(top, __shfl_xor(top, 32));
             const float base = top == -INFINITY ? 0.0f : top;
             float sum = 0;
@@ -265,11 +334,31 @@ template <typename I> struct Stats {
             if ((threadIdx.x & 32) == 0 && t < tokens) parts[(int64_t)(part0 + part) * tokens + t] = f32x2{top, sum};
         }
     }
+    __device__ __forceinline__ void few(f32x4 z, int v, int t, int part) const
+    {
+        const int want = target_of(targets, t, tokens, vocab) - first - v, room = end_ - first - v;
+        float top = -INFINITY, sum = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (r == want) hit[t] = z[r];
+            z[r] = r < room ? z[r] : -INFINITY;
+            top = fmaxf(top, z[r]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((z[r] - base) * LOG2E);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (threadIdx.x % 64 < 16 && t < tokens) parts[(int64_t)(part0 + part) * tokens + t] = f32x2{top, sum};
+    }
 };
 
 // Backward: dz of a piece of the vocabulary, rows of tokens `ld` apart; columns past the vocabulary and rows of tokens that take
 // no part are zeros.
 template <typename T, typename I> struct Slope {
+    static constexpr bool ROWS = true;
     T *dz;
     int64_t ld;
     const float *lse, *dloss;
@@ -283,87 +372,184 @@ template <typename T, typename I> struct Slope {
         return any == 0;
     }
     template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int) const
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int, char *scratch) const
     {
+        const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int t = n + 32 * j;
-            if (t >= tokens) continue;
-            const int target = target_of(targets, t, tokens, vocab) - first;
-            const float up = dloss[t], base = lse[t];
-            const bool on = live[t >> 6] >> (t & 63) & 1;
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                if (m + 32 * i >= ld) continue;
-                float f[16];
+            const int t = n + 32 * j, first_t = t - l;
+            if (first_t >= tokens) continue;
+            const int at = min(t, tokens - 1), target = target_of(targets, at, tokens, vocab) - first, room = end_ - first;
+            const float up = dloss[at], base = lse[at];
+            const bool on = live[at >> 6] >> (at & 63) & 1;
+            store_rows<FM>(scratch, dz + first_t * ld + m0, ld, tokens - first_t, (int)ld - m0, [&](int i, float *f) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int v = m + 32 * i + r;
                     const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E) - (v == target ? 1.0f : 0.0f);
-                    f[r] = on && v < end_ - first ? p * up : 0.0f;
+                    f[r] = on && v < room ? p * up : 0.0f;
                 }
-                T *row = dz + t * ld + m + 32 * i;
+            });
+        }
+    }
+    __device__ __forceinline__ void few(f32x4 z, int v, int t, int) const
+    {
+        if (t >= tokens || v >= ld) return;
+        const int want = target_of(targets, t, tokens, vocab) - first - v, room = end_ - first - v;
+        const bool on = live[t >> 6] >> (t & 63) & 1;
+        const float up = dloss[t], base = lse[t];
+        T f[4];
 #pragma unroll
-                for (int c = 0; c < 16; c += VE<T>) st16(row + c, narrow<T>(f + c));
+        for (int r = 0; r < 4; ++r) {
+            const float p = __builtin_amdgcn_exp2f((z[r] - base) * LOG2E) - (r == want ? 1.0f : 0.0f);
+            f[r] = (T)(on && r < room ? p * up : 0.0f);
+        }
+        T *row = dz + t * ld + v;
+        if constexpr (sizeof(T) == 2) *(u32x2 *)row = __builtin_bit_cast(u32x2, f);
+        else *(u32x4 *)row = __builtin_bit_cast(u32x4, f);
+    }
+};
+
+// Whether none of the rows [n0, n0 + count) takes part; null: all do.
+__device__ __forceinline__ bool all_dead(const uint64_t *live, int n0, int count, int rows)
+{
+    if (!live) return false;
+    uint64_t any = 0;
+    for (int i = 0; i < count && n0 + i < rows; i += 64) any |= ((Words)(uintptr_t)live)[(n0 + i) >> 6];
+    return any == 0;
+}
+
+// Sums that the next piece of the vocabulary goes on with, as the lanes hold them: nobody else reads them.
+template <int FM, int FN> __device__ __forceinline__ int64_t carried()
+{
+    return (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / 64) + wave_id()) * (FM * FN * 1024) + (threadIdx.x & 63) * 4;
+}
+template <int FM, int FN> __device__ __forceinline__ void resume(const float *sums, f32x16 (&acc)[FM][FN])
+{
+    const float *p = sums + carried<FM, FN>();
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const u32x4 v = *(const u32x4 *)(p + ((i * FN + j) * 4 + c) * 256);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][4 * c + r] = as_f(v[r]);
             }
+}
+struct Carry {
+    static constexpr bool ROWS = false;
+    float *sums;
+    bool first;
+    const uint64_t *live;           // of the rows, or null: all
+    int rows;
+    __device__ __forceinline__ bool skip(int n0, int count) const { return all_dead(live, n0, count, rows); }
+    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int, int) const
+    {
+        if (!first) resume(sums, acc);
+    }
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int, int, int, char *) const
+    {
+        float *p = sums + carried<FM, FN>();
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    u32x4 v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = as_u(acc[i][j][4 * c + r]);
+                    *(u32x4 *)(p + ((i * FN + j) * 4 + c) * 256) = v;
+                }
+    }
+};
+
+// The result, or (G = float, pieces of k) the sums of a piece.
+template <typename G> struct Result {
+    static constexpr bool ROWS = true;
+    G *out;
+    int64_t ld, apart;              // rows; matrices of the pieces of k
+    const float *sums;              // what Carry left, or null
+    const uint64_t *live;           // rows that are not zeros, or null: all
+    int rows, cols;
+    __device__ __forceinline__ bool skip(int n0, int count) const { return all_dead(live, n0, count, rows); }
+    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int, int) const
+    {
+        if (sums) resume(sums, acc);
+    }
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int, char *scratch) const
+    {
+        const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int row = n + 32 * j, first = row - l;
+            if (first >= rows || m0 >= cols) continue;
+            const int at = min(row, rows - 1);
+            const bool on = !live || (live[at >> 6] >> (at & 63) & 1);
+            store_rows<FM>(scratch, out + blockIdx.y * apart + first * ld + m0, ld, rows - first, cols - m0, [&](int i, float *f) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) f[r] = on ? acc[i][j][r] : 0.0f;
+            });
         }
     }
 };
 
-// A sum in binary32 (pieces of k: one matrix for each), or the result.  `sums` rows are `lds` apart, a multiple of 16, and whole.
-template <typename G> struct Result {
-    G *out;                         // float: the sums themselves
-    int64_t ld, apart;              // rows; matrices of the pieces of k
-    const float *start;             // what the sums start from, or null; rows `lds` apart
-    int64_t lds;
-    const uint64_t *live;           // rows that are not zeros, or null: all
-    int rows, cols;                 // cols of the sums: up to a multiple of 16
-    __device__ __forceinline__ bool skip(int n0, int count) const
-    {
-        if (!live) return false;
-        uint64_t any = 0;
-        for (int i = 0; i < count && n0 + i < rows; i += 64) any |= ((Words)(uintptr_t)live)[(n0 + i) >> 6];
-        return any == 0;
+// ---- logits of few tokens --------------------------------------------------------------
+//
+// Up to 32 tokens are bound by the weight's bytes: a wavefront takes 16 rows of it from memory into fragments, 64 bytes of each row a load and AHEAD
+// loads on their way, with no LDS and no wait for others.  D = 16 x 16: lane l holds row (A) or token (B) l % 16, k = V (l / 16) + 0.. of 4 V, and of D the
+// token l % 16 of rows 4 (l / 16) + 0..3.
+constexpr int FEW_AHEAD = 8;
+
+__device__ __forceinline__ void multiply16(f32x4 &d, u32x4 a, u32x4 b, bf16)
+{
+    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply16(f32x4 &d, u32x4 a, u32x4 b, float)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) d = __builtin_amdgcn_mfma_f32_16x16x4f32(as_f(a[j]), as_f(b[j]), d, 0, 0, 0);
+}
+
+// GROUPS of 16 tokens.  E::few(z, rows from, token, part): four logits of one token.
+template <typename T, int GROUPS, typename E>
+__global__ __launch_bounds__(256) void kt_xent_few_kernel(const T *w, int64_t ldw, int rows, const T *x, int64_t ldx, int tokens, int width, E e)
+{
+    constexpr int V = VE<T>, STEP_ = 4 * V;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, part = blockIdx.x * 4 + wave_id(), v0 = part * 16;
+    if (v0 >= rows) return;
+    const T *a = w + min(v0 + l, rows - 1) * ldw + g * V, *b[GROUPS];
+    f32x4 z[GROUPS];
+#pragma unroll
+    for (int t = 0; t < GROUPS; ++t) {
+        b[t] = x + min(16 * t + l, tokens - 1) * ldx + g * V;
+        z[t] = f32x4{0, 0, 0, 0};
     }
-    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int m, int n) const
-    {
-        if (!start) return;
+    int k = 0;
+    for (; k + FEW_AHEAD * STEP_ <= width; k += FEW_AHEAD * STEP_) {
+        u32x4 ra[FEW_AHEAD], rb[FEW_AHEAD][GROUPS];
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int u = 0; u < FEW_AHEAD; ++u) {
+            ra[u] = ld16<true>(a + k + u * STEP_);
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                if (n + 32 * j >= rows || m + 32 * i >= cols) continue;
-                const float *p = start + blockIdx.y * apart + (n + 32 * j) * lds + m + 32 * i;
-#pragma unroll
-                for (int c = 0; c < 16; c += 4) {
-                    const u32x4 v = *(const u32x4 *)(p + c);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][c + r] = as_f(v[r]);
-                }
-            }
-    }
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int) const
-    {
-        G *to = out + blockIdx.y * apart;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int row = n + 32 * j;
-            if (row >= rows) continue;
-            const bool on = !live || (live[row >> 6] >> (row & 63) & 1);
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const int c0 = m + 32 * i;
-                float f[16];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) f[r] = on ? acc[i][j][r] : 0.0f;
-#pragma unroll
-                for (int c = 0; c < 16; c += VE<G>) {
-                    if (c0 + c < cols) st_chunk(to + row * ld, c0 + c, cols, narrow<G>(f + c));
-                }
-            }
+            for (int t = 0; t < GROUPS; ++t) rb[u][t] = ld16(b[t] + k + u * STEP_);
         }
+#pragma unroll
+        for (int u = 0; u < FEW_AHEAD; ++u)
+#pragma unroll
+            for (int t = 0; t < GROUPS; ++t) multiply16(z[t], ra[u], rb[u][t], T());
     }
-};
+    for (; k < width; k += STEP_) {
+        const int left = width - k - g * V;
+        const u32x4 ra = ld_chunk(a + k, 0, left);
+#pragma unroll
+        for (int t = 0; t < GROUPS; ++t) multiply16(z[t], ra, ld_chunk(b[t] + k, 0, left), T());
+    }
+#pragma unroll
+    for (int t = 0; t < GROUPS; ++t) e.few(z[t], v0 + 4 * g, 16 * t + l, part);
+}
 
 // ---- the small kernels beside them ---------------------------------------------------
 
@@ -379,13 +565,13 @@ __global__ __launch_bounds__(256) void kt_xent_align_kernel(const T *x, int64_t 
     }
 }
 
-// lse and loss from the parts' largest values and sums: 256 / TOKENS lanes for a token, each a stretch of the parts.
+// lse and loss from the parts' largest values and sums: 256 / TOKENS lanes for a token, each a stretch of the parts or (one token) every 256th.
 template <typename I, int TOKENS>
 __global__ __launch_bounds__(256) void kt_xent_join_kernel(const f32x2 *parts, int count, const float *hit, const I *targets, int tokens,
                                                            int vocab, float *loss, float *lse)
 {
-    constexpr int EACH = 256 / TOKENS;
-    __shared__ f32x2 of[EACH][TOKENS];
+    constexpr int EACH = 256 / TOKENS, LEFT = TOKENS == 1 ? 4 : EACH;
+    __shared__ f32x2 of[LEFT][TOKENS];
     const int i = threadIdx.x % TOKENS, w = threadIdx.x / TOKENS;
     const int64_t t = (int64_t)blockIdx.x * TOKENS + i;
     const bool on = t < tokens && target_of(targets, (int)min(t, (int64_t)INT32_MAX), tokens, vocab) >= 0;
@@ -400,10 +586,16 @@ __global__ __launch_bounds__(256) void kt_xent_join_kernel(const f32x2 *parts, i
 #pragma unroll 8
         for (int k = a; k < b; k += TOKENS == 1 ? EACH : 1) add(parts[(int64_t)k * tokens + t]);
     }
-    of[w][i] = f32x2{top, sum};
+    if constexpr (TOKENS == 1) {
+#pragma unroll
+        for (int d = 32; d; d /= 2) add(f32x2{__shfl_xor(top, d), __shfl_xor(sum, d)});
+        if ((threadIdx.x & 63) == 0) of[threadIdx.x / 64][0] = f32x2{top, sum};
+    } else {
+        of[w][i] = f32x2{top, sum};
+    }
     __syncthreads();
     if (w || t >= tokens) return;
-    for (int k = 1; k < EACH; ++k) add(of[k][i]);
+    for (int k = 1; k < LEFT; ++k) add(of[k][i]);
     const float all = top + __builtin_amdgcn_logf(sum) * LN2;
     loss[t] = on ? all - hit[t] : 0.0f;
     if (lse) lse[t] = on ? all : 0.0f;
@@ -471,6 +663,8 @@ template <typename T> bool plain(const T *p, int64_t ld, int64_t width)
 
 // What a call needs of the workspace, and its cut.  Other matrices are copied to rows of a multiple of 16 bytes first (the weight up to 32 MiB of it
 // at a time), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
+constexpr int64_t FEW = 32;         // tokens whose logits kt_xent_few_kernel makes
+
 struct Plan {
     int64_t es, wide;               // bytes of an element; elements to a row of a copy
     int64_t copy;                   // rows of the weight copied at a time
@@ -505,19 +699,21 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
         p.bytes += up(bytes, 256);
         return from;
     };
-    p.x = take(tokens * p.wide * p.es);
-    p.w = take(p.piece * p.wide * p.es);
+    const bool few = tokens <= FEW;
+    p.x = take(!bwd && few ? 0 : tokens * p.wide * p.es);
+    p.w = take(!bwd && few ? 0 : p.piece * p.wide * p.es);
     if (!bwd) {
-        p.parts = take(over(vocab, p.side) * 2 * tokens * 8);
+        p.parts = take((few ? over(vocab, 16) : over(vocab, p.side) * 2) * tokens * 8);
         p.hit = take(tokens * 4);
         return p;
     }
     p.live = take(over(tokens, 64) * 8);
     p.dz = take(tokens * p.most * p.es);
     p.kx = pieces_of(dt, width, tokens, at_most(p.most, vocab));
-    if (p.kx.count > 1 || p.piece < vocab) p.acc = take(p.kx.count * tokens * p.ldp * 4);
-    // the weight's gradient, cut over the tokens: whichever of the two pieces takes more
-    int64_t most = 0;
+    const int64_t side = side_of(dt, width, tokens);
+    if (p.piece < vocab) p.acc = take(p.kx.count * over(width, side) * over(tokens, side) * side * side * 4);
+    // dx cut over the vocabulary, and the weight's gradient cut over the tokens: whichever takes more
+    int64_t most = p.kx.count > 1 ? p.kx.count * tokens : 0;
     for (int64_t rows : {at_most(p.most, vocab), at_most(p.piece, vocab), vocab % p.most, vocab % p.piece}) {
         if (rows == 0) continue;
         const Pieces k = pieces_of(dt, width, rows, tokens);
@@ -530,7 +726,7 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
 template <typename T, typename S, bool AA, bool BA, typename E>
 int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Pieces &k, const uint64_t *live, const E &e, hipStream_t s)
 {
-    constexpr int LDS = 2 * (S::BM + S::BN) * 128;
+    constexpr int LDS = S::SLOTS * (S::BM + S::BN) * ROW;
     const auto kernel = kt_xent_product_kernel<T, S, AA, BA, E>;
     if (LDS > 65536) {
         const hipError_t e1 = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
@@ -558,6 +754,14 @@ int product(int side, const Operand<T> &a, int64_t m, const Operand<T> &b, int64
         if (go_) return go_;           \
     } while (0)
 
+template <typename T, typename E> int few(const T *w, int64_t ldw, int64_t rows, const T *x, int64_t ldx, int64_t tokens, int64_t width, const E &e, hipStream_t s)
+{
+    const unsigned blocks = (unsigned)over(rows, 64);
+    if (tokens <= 16) kt_xent_few_kernel<T, 1, E><<<blocks, 256, 0, s>>>(w, ldw, (int)rows, x, ldx, (int)tokens, (int)width, e);
+    else kt_xent_few_kernel<T, 2, E><<<blocks, 256, 0, s>>>(w, ldw, (int)rows, x, ldx, (int)tokens, (int)width, e);
+    return (int)hipGetLastError();
+}
+
 // x or rows of w as the products take them: as they are, or copied.
 template <typename T> int aligned_rows(bool as_is, const T *x, int64_t ldx, int64_t width, int64_t rows, T *copy, int64_t wide, Operand<T> *to, hipStream_t s)
 {
@@ -584,14 +788,20 @@ int fwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, i
     float *hit = (float *)(ws + p.hit);
     const bool w_as_is = plain(w, ldw, width);
     Operand<T> a, b;
-    KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
-    for (int64_t v = 0, rows; v < vocab; v += rows) {
+    int count = (int)over(vocab, p.side) * 2;
+    if (tokens <= FEW) {
+        const Stats<I> e{parts, hit, targets, (int)tokens, (int)vocab, 0, (int)vocab, 0};
+        KT_GO(few(w, ldw, vocab, x, ldx, tokens, width, e, s));
+        count = (int)over(vocab, 16);
+    } else {
+        KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
+    }
+    for (int64_t v = tokens <= FEW ? vocab : 0, rows; v < vocab; v += rows) {
         rows = at_most(w_as_is ? p.most : p.piece, vocab - v);
         KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
         const Stats<I> e{parts, hit, targets, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / (p.side / 2))};
         KT_GO((product<T, true, true>(p.side, a, rows, b, tokens, width, Pieces{1, (int)up(width, 64)}, nullptr, e, s)));
     }
-    const int count = (int)over(vocab, p.side) * 2;
     if (tokens >= 512) kt_xent_join_kernel<I, 32><<<(unsigned)over(tokens, 32), 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
     else kt_xent_join_kernel<I, 1><<<(unsigned)tokens, 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
     return (int)hipGetLastError();
@@ -626,20 +836,25 @@ int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *
         if (tokens) {
             KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
             const Slope<T, I> e{dz, p.most, lse, dloss, targets, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
-            KT_GO((product<T, true, true>(side_of(dt, rows, tokens), a, rows, b, tokens, width, Pieces{1, (int)up(width, 64)}, nullptr, e, s)));
+            if (tokens <= FEW) KT_GO(few(w + v * ldw, ldw, rows, x, ldx, tokens, width, e, s));
+            else KT_GO((product<T, true, true>(side_of(dt, rows, tokens), a, rows, b, tokens, width, Pieces{1, (int)up(width, 64)}, nullptr, e, s)));
         }
         if (dx && tokens) {
             const Operand<T> wide{a.p, a.ld, (int)cols}, slope{dz, p.most, (int)tokens};
             const bool first = v == 0, last = v + rows == vocab;
-            const int64_t apart = tokens * p.ldp;
             const int side = side_of(dt, width, tokens);
-            if (last && p.kx.count == 1) {
-                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, p.ldp, live, (int)tokens, (int)width};
-                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, p.kx, nullptr, e, s)));
+            const Pieces k{p.kx.count, (int)up(over(rows, p.kx.count), 64)};
+            if (!last) {
+                const Carry e{acc, first, live, (int)tokens};
+                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, k, nullptr, e, s)));
+            } else if (k.count == 1) {
+                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, live, (int)tokens, (int)width};
+                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, k, nullptr, e, s)));
             } else {
-                const Result<float> e{acc, p.ldp, apart, first ? nullptr : acc, p.ldp, live, (int)tokens, (int)p.ldp};
-                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, p.kx, nullptr, e, s)));
-                if (last) KT_GO(sum(acc, p.kx, apart, p.ldp, tokens, width, dx, lddx, s));
+                const int64_t apart = tokens * p.ldp;
+                const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, live, (int)tokens, (int)p.ldp};
+                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, k, nullptr, e, s)));
+                KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, s));
             }
         }
         if (dw) {
@@ -647,10 +862,10 @@ int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *
             const Pieces k = pieces_of(dt, width, rows, tokens);
             const int side = side_of(dt, width, rows);
             if (k.count == 1) {
-                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, 0, nullptr, (int)rows, (int)width};
+                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, (int)rows, (int)width};
                 KT_GO((product<T, false, false>(side, wide, width, slope, rows, tokens, k, live, e, s)));
             } else {
-                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, 0, nullptr, (int)rows, (int)p.ldp};
+                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, (int)rows, (int)p.ldp};
                 KT_GO((product<T, false, false>(side, wide, width, slope, rows, tokens, k, live, e, s)));
                 KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, s));
             }
