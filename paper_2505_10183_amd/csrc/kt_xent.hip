@@ -104,12 +104,11 @@ template <typename T, int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct Bring
 template <typename T> struct Part;
 template <> struct Part<bf16> { typedef bf16x8 type; };
 template <> struct Part<float> { typedef f32x4 type; };
-__device__ __forceinline__ void multiply(f32x16 &d, bf16x8 a, bf16x8 b) { mma(d, a, b); }
-__device__ __forceinline__ void multiply(f32x16 &d, f32x4 a, f32x4 b)
-{
-#pragma unroll
-    for (int j = 0; j < 4; ++j) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], d, 0, 0, 0);
-}
+// Part j of PARTS of a product of two fragments: f32 takes four instructions, each with one k of both halves.  Those that follow each other should
+// add to different sums: the next one to the same waits until this one is through.
+template <typename T> constexpr int PARTS = sizeof(T) == 2 ? 1 : 4;
+template <int J> __device__ __forceinline__ void multiply(f32x16 &d, bf16x8 a, bf16x8 b) { mma(d, a, b); }
+template <int J> __device__ __forceinline__ void multiply(f32x16 &d, f32x4 a, f32x4 b) { d = __builtin_amdgcn_mfma_f32_32x32x2f32(a[J], b[J], d, 0, 0, 0); }
 
 // Fragment of 32 m or n from `first` on, chunk c of the step.
 template <typename T, int SIDE, bool ALONG, bool SPREAD>
@@ -199,7 +198,7 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
             if constexpr (u < BringA::N) from_a.load(u);
             else from_b.load(u - BringA::N);
         };
-        constexpr int PER = S::FM * S::FN, CHUNKS = ROW / 32, READS = S::FM + S::FN;
+        constexpr int PER = S::FM * S::FN, ALL = PER * PARTS<T>, CHUNKS = ROW / 32, READS = S::FM + S::FN;
         static_assert(CHUNKS % 2 == 0, "two sets of fragments take turns");
         F fa[2][S::FM], fb[2][S::FN];
         // fragment number r of a chunk, in the order in which the products need them
@@ -222,21 +221,21 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
             const int after = slot + 1 == SLOTS ? 0 : slot + 1;
             char *const now = lds + slot * SLOT, *const then = lds + after * SLOT;
             const bool more = k < k1;
-            span<0, CHUNKS * PER>([&](auto n1) {
-                constexpr int n = n1, c = n / PER, i = n % PER;
-                if constexpr (c == CHUNKS - 1 && i == 0) {
+            span<0, CHUNKS * ALL>([&](auto n1) {
+                constexpr int n = n1 % ALL, c = n1 / ALL, i = n % PER;
+                if constexpr (c == CHUNKS - 1 && n == 0) {
                     if (ahead == SLOTS) meet<(SLOTS - 2) * LOADS>();
                     else meet<0>();
                     if (more) aim(now, k);
                 }
-                multiply(acc[i / S::FN][i % S::FN], fa[c % 2][i / S::FN], fb[c % 2][i % S::FN]);
+                multiply<n / PER>(acc[i / S::FN][i % S::FN], fa[c % 2][i / S::FN], fb[c % 2][i % S::FN]);
                 // beside each product from the first on, so that the last ones are there for the next chunk's first products
-                constexpr int RATE = (READS + PER - 1) / PER;
-                span<(i * RATE < READS ? i * RATE : READS), ((i + 1) * RATE < READS ? (i + 1) * RATE : READS)>([&](auto r) {
+                constexpr int RATE = (READS + ALL - 1) / ALL;
+                span<(n * RATE < READS ? n * RATE : READS), ((n + 1) * RATE < READS ? (n + 1) * RATE : READS)>([&](auto r) {
                     read(c + 1 < CHUNKS ? now : then, std::integral_constant<int, (c + 1) % CHUNKS>(), r);
                 });
                 if constexpr (c == CHUNKS - 1) {
-                    if (more) span<i * LOADS / PER, (i + 1) * LOADS / PER>(load);
+                    if (more) span<n * LOADS / ALL, (n + 1) * LOADS / ALL>(load);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
@@ -633,27 +632,35 @@ __global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, in
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t over(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
-// The tile's side for a product of m x n: the largest that makes 192 tiles.
-int side_of(kt_dtype dt, int64_t m, int64_t n)
-{
-    auto tiles = [&](int64_t s) { return over(m, s) * over(n, s); };
-    return dt == KT_BF16 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
-}
-// Pieces of k where the tiles are fewer than the CUs: 256 steps of k in a piece at least, 16 pieces at most.
-struct Pieces {
-    int count, piece;
+// How a product of m x n over k is cut: the tile's side, and pieces of k (at most `most`), whose sums a second kernel adds.
+struct Cut {
+    int side, pieces, piece;
 };
-Pieces pieces_of(kt_dtype dt, int64_t m, int64_t n, int64_t k)
+// The least time of a model in us: a CU makes one workgroup's tile after the other, elements times steps of k at a rate that depends on the side (and a
+// start and an end worth 128 steps); pieces cost a launch and their sums' way through memory.  Rates are what full chips reached (16384 x 8192 x 2048 in its three orders: tiles of 256 511
+// to 555 us, of 128 600 to 650, of 64 850 to 1060; f32 4096 x 32768 x 768: 128 1578 to 1684, 64 1639 to 1829).  Both sides of a choice, us: f32
+// 768 x 4096 over 32768 in 2 pieces (384 workgroups) 2024, in 4 (768) 1578; bf16 2048 x 1152 over 16384 in tiles of 64 206, of 128 in 3 pieces 122.
+Cut cut_of(kt_dtype dt, int64_t m, int64_t n, int64_t k, int64_t most)
 {
-    const int s = side_of(dt, m, n), step = dt == KT_F32 ? 32 : 64;
-    const int64_t tiles = over(m, s) * over(n, s);
-    int64_t p = tiles > 0 && tiles < 256 ? 512 / tiles : 1;
-    if (p > k / 256) p = k / 256;
-    if (p > 16) p = 16;
-    if (p < 2) return Pieces{1, (int)up(k < 1 ? 1 : k, 64)};
-    const int64_t piece = up(over(k, p), 64 > step ? 64 : step);
-    return Pieces{(int)over(k, piece), (int)piece};
+    Cut best{64, 1, (int)up(k < 1 ? 1 : k, 64)};
+    double least = 1e300;
+    for (int side : {256, 128, 64}) {
+        if (side == 256 && dt == KT_F32) continue;
+        const double rate = dt == KT_F32 ? (side == 128 ? 2.5e5 : 2.3e5) : side == 256 ? 2.0e6 : side == 128 ? 1.75e6 : 1.15e6;
+        const int64_t tiles = over(m, side) * over(n, side);
+        for (int64_t p = 1; p <= most && (p == 1 || p * 128 <= k); ++p) {
+            const int64_t piece = up(over(k < 1 ? 1 : k, p), 64), count = over(k < 1 ? 1 : k, piece);
+            if (count != p) continue;
+            const double t = (double)over(tiles * p, 256) * side * side * (double)(piece + 128) / rate + (p > 1 ? 4 + (double)m * n * 8 * p / 5.5e6 : 0);
+            if (t < least) {
+                least = t;
+                best = Cut{side, (int)p, (int)piece};
+            }
+        }
+    }
+    return best;
 }
+constexpr int64_t MOST_PIECES = 16;
 
 // Whether loads of 16 bytes can take a matrix as it is: rows at multiples of 16 bytes, offsets within a tile of 31 bits.
 template <typename T> bool plain(const T *p, int64_t ld, int64_t width)
@@ -669,9 +676,9 @@ struct Plan {
     int64_t es, wide;               // bytes of an element; elements to a row of a copy
     int64_t copy;                   // rows of the weight copied at a time
     int64_t most, piece;            // rows of the vocabulary in a piece: with the weight as it is; with copies
-    int side;                       // forward
+    int side;                       // of the forward pass's tiles
     int64_t ldp;                    // backward: elements to a row of sums
-    Pieces kx;                      // of the vocabulary's pieces, for dx
+    Cut kx;                         // of dx over a piece of the vocabulary
     int64_t x, w, parts, hit, dz, live, acc, sums, bytes;       // where in the workspace
 };
 int64_t at_most(int64_t a, int64_t b) { return a < b ? a : b; }
@@ -692,7 +699,7 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
     p.most = rows_in(bwd ? 1ll << 27 : 1ll << 36, tokens, vocab);
     if (bwd) p.most = at_most(p.most, 1 << 18);
     p.piece = at_most(p.most, p.copy);
-    p.side = side_of(dt, vocab, tokens);
+    p.side = cut_of(dt, vocab, tokens, width, 1).side;
     p.ldp = up(width, 16);
     auto take = [&](int64_t bytes) {
         const int64_t from = p.bytes;
@@ -709,22 +716,22 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
     }
     p.live = take(over(tokens, 64) * 8);
     p.dz = take(tokens * p.most * p.es);
-    p.kx = pieces_of(dt, width, tokens, at_most(p.most, vocab));
-    const int64_t side = side_of(dt, width, tokens);
-    if (p.piece < vocab) p.acc = take(p.kx.count * over(width, side) * over(tokens, side) * side * side * 4);
+    p.kx = cut_of(dt, width, tokens, at_most(p.most, vocab), MOST_PIECES);
+    const int64_t side = p.kx.side;
+    if (p.piece < vocab) p.acc = take(p.kx.pieces * over(width, side) * over(tokens, side) * side * side * 4);
     // dx cut over the vocabulary, and the weight's gradient cut over the tokens: whichever takes more
-    int64_t most = p.kx.count > 1 ? p.kx.count * tokens : 0;
+    int64_t most = p.kx.pieces > 1 ? p.kx.pieces * tokens : 0;
     for (int64_t rows : {at_most(p.most, vocab), at_most(p.piece, vocab), vocab % p.most, vocab % p.piece}) {
         if (rows == 0) continue;
-        const Pieces k = pieces_of(dt, width, rows, tokens);
-        if (k.count > 1 && k.count * rows > most) most = k.count * rows;
+        const Cut k = cut_of(dt, width, rows, tokens, MOST_PIECES);
+        if (k.pieces > 1 && k.pieces * rows > most) most = k.pieces * rows;
     }
     p.sums = take(most * p.ldp * 4);
     return p;
 }
 
 template <typename T, typename S, bool AA, bool BA, typename E>
-int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Pieces &k, const uint64_t *live, const E &e, hipStream_t s)
+int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Cut &k, const uint64_t *live, const E &e, hipStream_t s)
 {
     constexpr int LDS = S::SLOTS * (S::BM + S::BN) * ROW;
     const auto kernel = kt_xent_product_kernel<T, S, AA, BA, E>;
@@ -733,18 +740,17 @@ int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n,
         if (e1 != hipSuccess) return (int)e1;
     }
     const int64_t mt = over(m, S::BM), nt = over(n, S::BN);
-    kernel<<<dim3((unsigned)(mt * nt), (unsigned)k.count), S::BLOCK, LDS, s>>>(a, b, (int)steps, k.piece, live, (int)mt, (int)nt, e);
+    kernel<<<dim3((unsigned)(mt * nt), (unsigned)k.pieces), S::BLOCK, LDS, s>>>(a, b, (int)steps, k.piece, live, (int)mt, (int)nt, e);
     return (int)hipGetLastError();
 }
-// The product of A [m x steps] and B [n x steps] in tiles of `side`.
+// The product of A [m x steps] and B [n x steps].
 template <typename T, bool AA, bool BA, typename E>
-int product(int side, const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Pieces &k, const uint64_t *live, const E &e,
-            hipStream_t s)
+int product(const Cut &k, const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const uint64_t *live, const E &e, hipStream_t s)
 {
     if constexpr (sizeof(T) == 2) {
-        if (side == 256) return launch_tiles<T, Big, AA, BA>(a, m, b, n, steps, k, live, e, s);
+        if (k.side == 256) return launch_tiles<T, Big, AA, BA>(a, m, b, n, steps, k, live, e, s);
     }
-    if (side == 128) return launch_tiles<T, Mid, AA, BA>(a, m, b, n, steps, k, live, e, s);
+    if (k.side == 128) return launch_tiles<T, Mid, AA, BA>(a, m, b, n, steps, k, live, e, s);
     return launch_tiles<T, Small, AA, BA>(a, m, b, n, steps, k, live, e, s);
 }
 
@@ -800,17 +806,17 @@ int fwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, i
         rows = at_most(w_as_is ? p.most : p.piece, vocab - v);
         KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
         const Stats<I> e{parts, hit, targets, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / (p.side / 2))};
-        KT_GO((product<T, true, true>(p.side, a, rows, b, tokens, width, Pieces{1, (int)up(width, 64)}, nullptr, e, s)));
+        KT_GO((product<T, true, true>(Cut{p.side, 1, (int)up(width, 64)}, a, rows, b, tokens, width, nullptr, e, s)));
     }
     if (tokens >= 512) kt_xent_join_kernel<I, 32><<<(unsigned)over(tokens, 32), 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
     else kt_xent_join_kernel<I, 1><<<(unsigned)tokens, 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
     return (int)hipGetLastError();
 }
 
-template <typename G> int sum(const float *parts, const Pieces &k, int64_t apart, int64_t ldp, int64_t rows, int64_t cols, G *out, int64_t ld, hipStream_t s)
+template <typename G> int sum(const float *parts, const Cut &k, int64_t apart, int64_t ldp, int64_t rows, int64_t cols, G *out, int64_t ld, hipStream_t s)
 {
     const int64_t blocks = over(rows * over(cols, 4), 256);
-    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.count, apart, (int)ldp, (int)rows, (int)cols, out, ld);
+    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.pieces, apart, (int)ldp, (int)rows, (int)cols, out, ld);
     return (int)hipGetLastError();
 }
 
@@ -837,36 +843,34 @@ int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *
             KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
             const Slope<T, I> e{dz, p.most, lse, dloss, targets, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
             if (tokens <= FEW) KT_GO(few(w + v * ldw, ldw, rows, x, ldx, tokens, width, e, s));
-            else KT_GO((product<T, true, true>(side_of(dt, rows, tokens), a, rows, b, tokens, width, Pieces{1, (int)up(width, 64)}, nullptr, e, s)));
+            else KT_GO((product<T, true, true>(cut_of(dt, rows, tokens, width, 1), a, rows, b, tokens, width, nullptr, e, s)));
         }
         if (dx && tokens) {
             const Operand<T> wide{a.p, a.ld, (int)cols}, slope{dz, p.most, (int)tokens};
             const bool first = v == 0, last = v + rows == vocab;
-            const int side = side_of(dt, width, tokens);
-            const Pieces k{p.kx.count, (int)up(over(rows, p.kx.count), 64)};
+            const Cut k{p.kx.side, p.kx.pieces, (int)up(over(rows, p.kx.pieces), 64)};
             if (!last) {
                 const Carry e{acc, first, live, (int)tokens};
-                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, k, nullptr, e, s)));
-            } else if (k.count == 1) {
+                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, nullptr, e, s)));
+            } else if (k.pieces == 1) {
                 const Result<T> e{dx, lddx, 0, first ? nullptr : acc, live, (int)tokens, (int)width};
-                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, k, nullptr, e, s)));
+                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, nullptr, e, s)));
             } else {
                 const int64_t apart = tokens * p.ldp;
                 const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, live, (int)tokens, (int)p.ldp};
-                KT_GO((product<T, false, true>(side, wide, width, slope, tokens, rows, k, nullptr, e, s)));
+                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, nullptr, e, s)));
                 KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, s));
             }
         }
         if (dw) {
             const Operand<T> wide{b.p, b.ld, (int)cols}, slope{dz, p.most, (int)up(rows, VE<T>)};
-            const Pieces k = pieces_of(dt, width, rows, tokens);
-            const int side = side_of(dt, width, rows);
-            if (k.count == 1) {
+            const Cut k = cut_of(dt, width, rows, tokens, MOST_PIECES);
+            if (k.pieces == 1) {
                 const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, (int)rows, (int)width};
-                KT_GO((product<T, false, false>(side, wide, width, slope, rows, tokens, k, live, e, s)));
+                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, live, e, s)));
             } else {
                 const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, (int)rows, (int)p.ldp};
-                KT_GO((product<T, false, false>(side, wide, width, slope, rows, tokens, k, live, e, s)));
+                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, live, e, s)));
                 KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, s));
             }
         }
