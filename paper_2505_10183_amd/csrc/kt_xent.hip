@@ -226,7 +226,12 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
                 if constexpr (c == CHUNKS - 1 && n == 0) {
                     if (ahead == SLOTS) meet<(SLOTS - 2) * LOADS>();
                     else meet<0>();
-                    if (more) aim(now, k);
+                    if (more) {
+                        aim(now, k);
+                        // bf16: all loads at once (spread over the products that follow the decoder's backward pass takes 9.87 ms instead of 9.47); f32, whose
+                        // products take eight times as long: spread (4096 x 50304 x 768 7.55 ms instead of 8.10)
+                        if constexpr (PARTS<T> == 1) span<0, LOADS>(load);
+                    }
                 }
                 multiply<n / PER>(acc[i / S::FN][i % S::FN], fa[c % 2][i / S::FN], fb[c % 2][i % S::FN]);
                 // beside each product from the first on, so that the last ones are there for the next chunk's first products
@@ -234,7 +239,7 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
                 span<(n * RATE < READS ? n * RATE : READS), ((n + 1) * RATE < READS ? (n + 1) * RATE : READS)>([&](auto r) {
                     read(c + 1 < CHUNKS ? now : then, std::integral_constant<int, (c + 1) % CHUNKS>(), r);
                 });
-                if constexpr (c == CHUNKS - 1) {
+                if constexpr (c == CHUNKS - 1 && PARTS<T> > 1) {
                     if (more) span<n * LOADS / ALL, (n + 1) * LOADS / ALL>(load);
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -526,20 +531,38 @@ __global__ __launch_bounds__(256) void kt_xent_few_kernel(const T *w, int64_t ld
         b[t] = x + min(16 * t + l, tokens - 1) * ldx + g * V;
         z[t] = f32x4{0, 0, 0, 0};
     }
-    int k = 0;
-    for (; k + FEW_AHEAD * STEP_ <= width; k += FEW_AHEAD * STEP_) {
-        u32x4 ra[FEW_AHEAD], rb[FEW_AHEAD][GROUPS];
+    // two sets of loads take turns: one is on its way while the other is used
+    u32x4 ra[2][FEW_AHEAD], rb[2][FEW_AHEAD][GROUPS];
+    auto load = [&](auto set0, int k) __attribute__((always_inline)) {
+        constexpr int set = set0;
 #pragma unroll
         for (int u = 0; u < FEW_AHEAD; ++u) {
-            ra[u] = ld16<true>(a + k + u * STEP_);
+            ra[set][u] = ld16(a + k + u * STEP_);
 #pragma unroll
-            for (int t = 0; t < GROUPS; ++t) rb[u][t] = ld16(b[t] + k + u * STEP_);
+            for (int t = 0; t < GROUPS; ++t) rb[set][u][t] = ld16(b[t] + k + u * STEP_);
         }
+    };
+    auto use = [&](auto set0) __attribute__((always_inline)) {
+        constexpr int set = set0;
 #pragma unroll
         for (int u = 0; u < FEW_AHEAD; ++u)
 #pragma unroll
-            for (int t = 0; t < GROUPS; ++t) multiply16(z[t], ra[u], rb[u][t], T());
+            for (int t = 0; t < GROUPS; ++t) multiply16(z[t], ra[set][u], rb[set][u][t], T());
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+    constexpr int SET = FEW_AHEAD * STEP_;
+    const int whole = width / SET * SET;
+    int k = 0;
+    if (whole) load(first, 0);
+    for (; k < whole; k += 2 * SET) {
+        if (k + SET < whole) load(second, k + SET);
+        use(first);
+        if (k + SET >= whole) break;
+        if (k + 2 * SET < whole) load(first, k + 2 * SET);
+        use(second);
     }
+    k = whole;
     for (; k < width; k += STEP_) {
         const int left = width - k - g * V;
         const u32x4 ra = ld_chunk(a + k, 0, left);
