@@ -240,7 +240,7 @@ __global__ __launch_bounds__(FEW_LANES) void kt_embedding_sort_few_kernel(const 
 }
 
 // More tokens: a workgroup has a stretch of them; a pass over one digit is two kernels, the first of which counts.
-constexpr int LANES = 256, WAVES = LANES / 64, MOST_BITS = 10, MOST_BINS = 1 << MOST_BITS;
+constexpr int LANES = 1024, WAVES = LANES / 64, STRETCH = 2 * LANES, MOST_BITS = 9, MOST_BINS = 1 << MOST_BITS;
 
 // What a pass reads: the ids as they are, or what the last pass left.
 template <typename I, bool FIRST> struct Source {
@@ -285,39 +285,31 @@ __global__ __launch_bounds__(LANES) void kt_embedding_place_kernel(Source<I, FIR
         fill(zeros, blockIdx.x - stretches, gridDim.x - stretches, LANES);
         return;
     }
-    __shared__ int next[WAVES][MOST_BINS], total[MOST_BINS], carry[16];
+    __shared__ int next[WAVES][MOST_BINS], total[MOST_BINS], before[MOST_BINS], carry[16];
     const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63, bins = 1 << bits;
-    for (int i = tid; i < bins; i += LANES)
-        for (int w = 0; w < WAVES; ++w) next[w][i] = 0;
+    for (int i = tid; i < bins; i += LANES) total[i] = before[i] = 0;
+    for (int i = lane; i < bins; i += 64) next[wave][i] = 0;
     __syncthreads();
     // a wavefront's elements are neighbours
     const int64_t each = stretch / WAVES, n0 = min((int64_t)tokens, (int64_t)blockIdx.x * stretch + wave * each), n1 = min((int64_t)tokens, n0 + each);
     for (int64_t n = n0 + lane; n < n1; n += 64) atomicAdd(&next[wave][from.key(n, vocab) >> shift & (bins - 1)], 1);
-    int before[MOST_BINS / LANES];              // of each digit, in the stretches before this one
-#pragma unroll
-    for (int u = 0; u < MOST_BINS / LANES; ++u) {
-        const int i = tid + u * LANES;
-        before[u] = 0;
-        if (i >= bins) break;
-        int all = 0;
-#pragma unroll 8
-        for (int b = 0; b < stretches; ++b) {
-            const int n = counts[b * bins + i];
-            all += n;
-            before[u] += b < (int)blockIdx.x ? n : 0;
-        }
-        total[i] = all;
+    // of each digit: all of them, and those in the stretches before this one
+    int all = 0, mine = 0;
+#pragma unroll 4
+    for (int b = tid >> bits; b < stretches; b += LANES >> bits) {
+        const int n = counts[b * bins + (tid & (bins - 1))];
+        all += n;
+        mine += b < (int)blockIdx.x ? n : 0;
     }
+    atomicAdd(&total[tid & (bins - 1)], all);
+    atomicAdd(&before[tid & (bins - 1)], mine);
     __syncthreads();
     exclusive_sums(total, bins, carry);
-#pragma unroll
-    for (int u = 0; u < MOST_BINS / LANES; ++u) {
-        const int i = tid + u * LANES;
-        if (i >= bins) break;
-        int s = total[i] + before[u];
+    if (tid < bins) {
+        int s = total[tid] + before[tid];
         for (int w = 0; w < WAVES; ++w) {
-            const int n = next[w][i];
-            next[w][i] = s;
+            const int n = next[w][tid];
+            next[w][tid] = s;
             s += n;
         }
     }
@@ -418,55 +410,81 @@ __global__ __launch_bounds__(256) void kt_embedding_sum_kernel(const int *keys, 
     if (now >= 0) end(now == behind);
 }
 
-// A run that begins in piece p and goes on behind it: the partial sums in their order, each wavefront a stretch of them.
-constexpr int JOIN = 512;
+// A run that begins in piece p and goes on behind it: the partial sums in their order.  Each wavefront has a piece, and adds what its run left if that
+// is up to SHORT partial sums; all of them add a longer one together, each a stretch of it.
+constexpr int JOIN = 512, JOIN_WAVES = JOIN / 64, SHORT = 16;
 
 template <typename W, bool ADD>
 __global__ __launch_bounds__(JOIN) void kt_embedding_join_kernel(const int *keys, const float *parts, int ldp, W *dw, int64_t lddw, float scale,
                                                                  int vocab, int width, int piece, int pieces)
 {
-    __shared__ __align__(16) float sums[JOIN / 64][256];
-    const int p = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const int i0 = p * piece, i1 = i0 + piece;          // not the last piece: there are tokens behind it
-    const int key = keys[i1 - 1];
-    if (key >= vocab || keys[i1] != key || (i0 && keys[i0 - 1] == key)) return;
-    int q = p + 1;                                      // the first piece that does not begin with the key
-    for (;;) {
-        const int at = q + lane;
-        const uint64_t other = __ballot(at >= pieces || keys[(int64_t)at * piece] != key);
-        if (other) {
-            q += __builtin_ctzll(other);
-            break;
+    __shared__ int run[JOIN_WAVES], key_of_run[JOIN_WAVES];                     // pieces behind the one that it begins in
+    __shared__ __align__(16) float sums[JOIN_WAVES][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, p0 = blockIdx.x * JOIN_WAVES, p = p0 + wave;
+    int n = 0, key = -1;
+    if (p < pieces - 1) {                               // not the last piece: there are tokens behind it
+        const int i0 = p * piece, i1 = i0 + piece;
+        key = keys[i1 - 1];
+        if (key < vocab && keys[i1] == key && !(i0 && keys[i0 - 1] == key)) {
+            int q = p + 1;                              // to the first piece that does not begin with the key
+            for (;;) {
+                const int at = q + lane;
+                const uint64_t other = __ballot(at >= pieces || keys[(int64_t)at * piece] != key);
+                if (other) {
+                    q += __builtin_ctzll(other);
+                    break;
+                }
+                q += 64;
+            }
+            n = q - p - 1;
         }
-        q += 64;
     }
-    const int n = q - p - 1, each = (n + JOIN / 64 - 1) / (JOIN / 64), a = p + 1 + wave * each, b = min(q, a + each);
+    if (lane == 0) {
+        run[wave] = n;
+        key_of_run[wave] = key;
+    }
+    __syncthreads();
+    auto add = [&](float (&s)[4], const float *row) {
+        const u32x4 r = *(const u32x4 *)row;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += as_f(r[j]);
+    };
+    auto put4 = [&](int k, int c, const float (&s)[4]) {
+        W *row = dw + (int64_t)k * lddw;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < width) row[c + j] = (W)(s[j] * scale + (ADD ? (float)row[c + j] : 0.0f));
+    };
     for (int c0 = blockIdx.y * 256; c0 < width; c0 += gridDim.y * 256) {
         const int c = c0 + lane * 4;
-        float s[4] = {0, 0, 0, 0};
-        auto add = [&](const float *row) {
-            const u32x4 r = *(const u32x4 *)(row + c);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[j] += as_f(r[j]);
-        };
-        if (c < width) {
-            if (wave == 0) add(parts + ((int64_t)p * 2 + 1) * ldp);
+        if (n > 0 && n <= SHORT && c < width) {
+            float s[4] = {0, 0, 0, 0};
+            add(s, parts + ((int64_t)p * 2 + 1) * ldp + c);
+#pragma unroll 4
+            for (int k = p + 1; k <= p + n; ++k) add(s, parts + (int64_t)k * 2 * ldp + c);
+            put4(key, c, s);
+        }
+        for (int r = 0; r < JOIN_WAVES; ++r) {
+            const int m = run[r];
+            if (m <= SHORT) continue;
+            const int each = (m + JOIN_WAVES - 1) / JOIN_WAVES, a = p0 + r + 1 + wave * each, b = min(p0 + r + 1 + m, a + each);
+            float s[4] = {0, 0, 0, 0};
+            if (c < width) {
+                if (wave == 0) add(s, parts + ((int64_t)(p0 + r) * 2 + 1) * ldp + c);
 #pragma unroll 16
-            for (int k = a; k < b; ++k) add(parts + (int64_t)k * 2 * ldp);
+                for (int k = a; k < b; ++k) add(s, parts + (int64_t)k * 2 * ldp + c);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sums[wave][lane * 4 + j] = s[j];
+            __syncthreads();
+            if (wave == 0 && c < width) {
+                for (int w = 1; w < JOIN_WAVES; ++w)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[j] += sums[w][lane * 4 + j];
+                put4(key_of_run[r], c, s);
+            }
+            __syncthreads();
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sums[wave][lane * 4 + j] = s[j];
-        __syncthreads();
-        if (wave == 0 && c < width) {
-            for (int w = 1; w < JOIN / 64; ++w)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] += sums[w][lane * 4 + j];
-            W *row = dw + (int64_t)key * lddw;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + j < width) row[c + j] = (W)(s[j] * scale + (ADD ? (float)row[c + j] : 0.0f));
-        }
-        __syncthreads();
     }
 }
 
@@ -496,7 +514,7 @@ Cut cut(int64_t tokens, int64_t vocab, int64_t width)
     c.passes = (all + MOST_BITS - 1) / MOST_BITS;
     c.bits = (all + c.passes - 1) / c.passes;
     c.stretch = (int)up((tokens + 511) / 512, LANES);
-    if (c.stretch < 8 * LANES) c.stretch = 8 * LANES;
+    if (c.stretch < STRETCH) c.stretch = STRETCH;
     c.stretches = (int)((tokens + c.stretch - 1) / c.stretch);
     c.lists = up(tokens * 4, 256);
     c.counts = tokens <= FEW ? 0 : up((int64_t)c.stretches * 4 << c.bits, 256);
@@ -509,8 +527,8 @@ int pass(const Cut &c, const Source<I, FIRST> &from, int *counts, int *keys, int
          const Fill &f2, hipStream_t s)
 {
     auto blocks = [&](const Fill &f) {
-        const int64_t n = (f.to - f.from + 15) / 16;
-        return (unsigned)(c.stretches + (n < 2048 ? n : 2048));
+        const int64_t n = (f.to - f.from + 63) / 64;
+        return (unsigned)(c.stretches + (n < 512 ? n : 512));
     };
     kt_embedding_count_kernel<I, FIRST><<<blocks(f1), LANES, 0, s>>>(from, counts, tokens, vocab, c.stretch, c.stretches, shift, c.bits, f1);
     kt_embedding_place_kernel<I, FIRST><<<blocks(f2), LANES, 0, s>>>(from, counts, keys, order, tokens, vocab, c.stretch, c.stretches, shift, c.bits, f2);
@@ -527,7 +545,7 @@ int sums(const Cut &c, const int *keys, const int *order, const T *dy, int64_t l
     kt_embedding_sum_kernel<T, W, ADD><<<(unsigned)((waves + 3) / 4), 256, 0, s>>>(keys, order, dy, lddy, dw, lddw, parts, c.ldp, scale, tokens, vocab, width, c.piece, c.pieces, spans);
     if (c.pieces > 1) {
         const int across = (width + 255) / 256;
-        kt_embedding_join_kernel<W, ADD><<<dim3(c.pieces - 1, across < 64 ? across : 64), JOIN, 0, s>>>(keys, parts, c.ldp, dw, lddw, scale, vocab, width, c.piece, c.pieces);
+        kt_embedding_join_kernel<W, ADD><<<dim3((c.pieces - 1 + JOIN_WAVES - 1) / JOIN_WAVES, across < 64 ? across : 64), JOIN, 0, s>>>(keys, parts, c.ldp, dw, lddw, scale, vocab, width, c.piece, c.pieces);
     }
     return (int)hipGetLastError();
 }
