@@ -13,6 +13,8 @@ namespace {
 
 constexpr int64_t MOST_BLOCKS = 1 << 20;        // of a launch; what is more is taken in turns
 
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+
 template <typename I> __device__ __forceinline__ int key_of(I id, int vocab)
 {
     return id >= 0 && id < (I)vocab ? (int)id : vocab;      // sorted behind all others
@@ -86,6 +88,17 @@ int fwd(int64_t tokens, int vocab, int width, const I *ids, const W *w, int64_t 
 
 // ---- zeros beside the sort ---------------------------------------------------------
 
+// The part-th 4 KiB of a row of `bytes` bytes, by a wavefront.
+__device__ __forceinline__ void fill_part(char *row, int64_t part, int64_t bytes, int lane)
+{
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const int64_t at = part * 4096 + s * 1024 + lane * 16;
+        if (at + 16 <= bytes) st16(row + at, u32x4{0, 0, 0, 0});
+        else
+            for (int64_t b = at; b < bytes; b += 2) *(uint16_t *)(row + b) = 0;
+    }
+}
 // A share of a matrix to fill with zeros: items [from, to) of 4 KiB of a row each.
 struct Fill {
     char *p;
@@ -96,15 +109,7 @@ __device__ __forceinline__ void fill(const Fill &f, int block, int blocks, int l
 {
     const int lane = threadIdx.x & 63, waves = lanes / 64;
     for (int64_t n = f.from + (int64_t)block * waves + threadIdx.x / 64; n < f.to; n += (int64_t)blocks * waves) {
-        char *row = f.p + n / f.parts * f.ld;
-        const int64_t c = n % f.parts * 4096 + lane * 16;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int64_t at = c + s * 1024;
-            if (at + 16 <= f.row) st16(row + at, u32x4{0, 0, 0, 0});
-            else
-                for (int64_t b = at; b < f.row; b += 2) *(uint16_t *)(row + b) = 0;
-        }
+        fill_part(f.p + n / f.parts * f.ld, n % f.parts, f.row, lane);
     }
 }
 
@@ -344,6 +349,19 @@ template <typename W, int E, bool ADD> __device__ __forceinline__ void put(W *ro
     store_e<W, E>(row, c, width, f);
 }
 
+// E columns for each lane of a wavefront, from column c0 on.  A lane whose columns end past the row takes the row's last E instead, some of them as its neighbour
+// does: both write the same numbers, with one instruction.  (Not the first lane: its neighbour is another wavefront.)  Lanes past the row
+// read what the first one does.
+template <int E> struct Columns {
+    bool whole;                 // E columns from `from` on are there in every lane
+    int c, from;
+    __device__ __forceinline__ Columns(int c0, int lane, int width) : whole(c0 + E <= width), c(c0 + lane * E)
+    {
+        if (whole && c < width) c = min(c, width - E);
+        from = c < width ? c : c0;
+    }
+};
+
 constexpr int AHEAD = 8;        // rows on their way at once
 
 // A wavefront adds the rows of a piece of the sorted list, 64 * E columns of them.  parts[piece][0]: the sum of what a run that began
@@ -355,9 +373,11 @@ __global__ __launch_bounds__(256) void kt_embedding_sum_kernel(const int *keys, 
 {
     constexpr int E = EACH<T, W>, R = E / VE<T>;
     const int lane = threadIdx.x & 63;
-    const int64_t n = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t n = (int64_t)blockIdx.x * 4 + wave_of();
     if (n >= (int64_t)pieces * spans) return;
-    const int p = (int)(n / spans), c = (int)(n % spans) * (64 * E) + lane * E;
+    const int p = (int)(n / spans), c0 = (int)(n % spans) * (64 * E);
+    const Columns<E> at(c0, lane, width);
+    const int c = at.c;
     const int i0 = p * piece, i1 = min(tokens, i0 + piece);
     const int before = i0 ? keys[i0 - 1] : -1, behind = i1 < tokens ? keys[i1] : -1;
     float sum[E];
@@ -370,7 +390,7 @@ __global__ __launch_bounds__(256) void kt_embedding_sum_kernel(const int *keys, 
             float *to = parts + ((int64_t)p * 2 + (begun ? 0 : 1)) * ldp;
             if (c < width) {
 #pragma unroll
-                for (int j = 0; j < E; j += 4) *(u32x4 *)(to + c + j) = u32x4{as_u(sum[j]), as_u(sum[j + 1]), as_u(sum[j + 2]), as_u(sum[j + 3])};
+                for (int j = 0; j < E; j += 4) *(u32x4_any *)(to + c + j) = u32x4{as_u(sum[j]), as_u(sum[j + 1]), as_u(sum[j + 2]), as_u(sum[j + 3])};
             }
         } else {
             put<W, E, ADD>(dw + now * lddw, c, width, scale, sum);
@@ -378,15 +398,25 @@ __global__ __launch_bounds__(256) void kt_embedding_sum_kernel(const int *keys, 
     };
     for (int i = i0; i < i1; i += 64) {
         const int mine = min(i + lane, i1 - 1), key = keys[mine], pos = order[mine], count = min(64, i1 - i);
-        for (int a = 0; a < count; a += AHEAD) {
-            u32x4 r[AHEAD][R];
+        auto load = [&](u32x4 (&r)[AHEAD][R], int a) __attribute__((always_inline)) {
+            if (at.whole && a + AHEAD <= count && __builtin_amdgcn_readlane(key, a + AHEAD - 1) < vocab) {
+                // without a branch, so that the loads leave together
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int l = min(a + u, count - 1);
-                const bool there = a + u < count && __builtin_amdgcn_readlane(key, l) < vocab;
-                const T *row = dy + (int64_t)__builtin_amdgcn_readlane(pos, l) * lddy;
-                if (there) load_e<T, E>(row, c, width, r[u]);
+                for (int u = 0; u < AHEAD; ++u) {
+                    const T *row = dy + (int64_t)__builtin_amdgcn_readlane(pos, a + u) * lddy + at.from;
+#pragma unroll
+                    for (int k = 0; k < R; ++k) r[u][k] = ld16<true>(row + k * VE<T>);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int l = min(a + u, count - 1);
+                    const T *row = dy + (int64_t)__builtin_amdgcn_readlane(pos, l) * lddy;
+                    if (a + u < count && __builtin_amdgcn_readlane(key, l) < vocab) load_e<T, E>(row, c, width, r[u]);
+                }
             }
+        };
+        auto use = [&](const u32x4 (&r)[AHEAD][R], int a) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 if (a + u >= count) break;
@@ -405,6 +435,14 @@ __global__ __launch_bounds__(256) void kt_embedding_sum_kernel(const int *keys, 
                     for (int j = 0; j < E; ++j) sum[j] += f[j];
                 }
             }
+        };
+        u32x4 r0[AHEAD][R], r1[AHEAD][R];       // one is on its way while the other is added
+        load(r0, 0);
+        for (int a = 0; a < count; a += 2 * AHEAD) {
+            if (a + AHEAD < count) load(r1, a + AHEAD);
+            use(r0, a);
+            if (a + 2 * AHEAD < count) load(r0, a + 2 * AHEAD);
+            if (a + AHEAD < count) use(r1, a + AHEAD);
         }
     }
     if (now >= 0) end(now == behind);
@@ -444,24 +482,43 @@ __global__ __launch_bounds__(JOIN) void kt_embedding_join_kernel(const int *keys
         key_of_run[wave] = key;
     }
     __syncthreads();
-    auto add = [&](float (&s)[4], const float *row) {
-        const u32x4 r = *(const u32x4 *)row;
+    auto add = [&](float (&s)[4], u32x4 r) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] += as_f(r[j]);
     };
-    auto put4 = [&](int k, int c, const float (&s)[4]) {
-        W *row = dw + (int64_t)k * lddw;
+    // the first partial sums of pieces a to b - 1, LOADS of them on their way at once
+    auto add_all = [&](float (&s)[4], int a, int b, int c) {
+        constexpr int LOADS = 16;
+        for (; a < b; a += LOADS) {
+            u32x4 r[LOADS];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c + j < width) row[c + j] = (W)(s[j] * scale + (ADD ? (float)row[c + j] : 0.0f));
+            for (int u = 0; u < LOADS; ++u) r[u] = *(const u32x4 *)(parts + (int64_t)min(a + u, b - 1) * 2 * ldp + c);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u)
+                if (a + u < b) add(s, r[u]);
+        }
+    };
+    auto put4 = [&](int k, int c, const float (&s)[4]) {
+        typedef W W4 __attribute__((ext_vector_type(4)));
+        typedef W4 W4_any __attribute__((aligned(sizeof(W))));
+        W *row = dw + (int64_t)k * lddw + c;
+        if (c + 4 <= width) {
+            W4 v;
+            if (ADD) v = *(const W4_any *)row;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = (W)(s[j] * scale + (ADD ? (float)v[j] : 0.0f));
+            *(W4_any *)row = v;
+        } else {
+            for (int j = 0; j < width - c; ++j) row[j] = (W)(s[j] * scale + (ADD ? (float)row[j] : 0.0f));
+        }
     };
     for (int c0 = blockIdx.y * 256; c0 < width; c0 += gridDim.y * 256) {
         const int c = c0 + lane * 4;
         if (n > 0 && n <= SHORT && c < width) {
             float s[4] = {0, 0, 0, 0};
-            add(s, parts + ((int64_t)p * 2 + 1) * ldp + c);
-#pragma unroll 4
-            for (int k = p + 1; k <= p + n; ++k) add(s, parts + (int64_t)k * 2 * ldp + c);
+            add(s, *(const u32x4 *)(parts + ((int64_t)p * 2 + 1) * ldp + c));
+            add_all(s, p + 1, p + 1 + n, c);
             put4(key, c, s);
         }
         for (int r = 0; r < JOIN_WAVES; ++r) {
@@ -470,9 +527,8 @@ __global__ __launch_bounds__(JOIN) void kt_embedding_join_kernel(const int *keys
             const int each = (m + JOIN_WAVES - 1) / JOIN_WAVES, a = p0 + r + 1 + wave * each, b = min(p0 + r + 1 + m, a + each);
             float s[4] = {0, 0, 0, 0};
             if (c < width) {
-                if (wave == 0) add(s, parts + ((int64_t)(p0 + r) * 2 + 1) * ldp + c);
-#pragma unroll 16
-                for (int k = a; k < b; ++k) add(s, parts + (int64_t)k * 2 * ldp + c);
+                if (wave == 0) add(s, *(const u32x4 *)(parts + ((int64_t)(p0 + r) * 2 + 1) * ldp + c));
+                add_all(s, a, b, c);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) sums[wave][lane * 4 + j] = s[j];
@@ -485,6 +541,86 @@ __global__ __launch_bounds__(JOIN) void kt_embedding_join_kernel(const int *keys
             }
             __syncthreads();
         }
+    }
+}
+
+// ---- a handful of tokens -------------------------------------------------------------
+//
+// Up to HANDFUL tokens need no order: every wavefront has all ids in four registers.  That of a token's first occurrence adds its rows, those of the
+// other occurrences have nothing to do; the wavefronts behind them write zeros into the rows whose number is not among the ids.  One launch
+// instead of three: 197 tokens of 1000 x 768 f32 14.4 -> 6.4 us.
+constexpr int HANDFUL = 256;
+
+template <typename T, typename W, typename I, bool ADD>
+__global__ __launch_bounds__(256) void kt_embedding_handful_kernel(const I *ids, const T *dy, int64_t lddy, W *dw, int64_t lddw, float scale, int tokens,
+                                                                   int vocab, int width, int spans)
+{
+    constexpr int E = EACH<T, W>, R = E / VE<T>, WORDS = HANDFUL / 64;
+    const int lane = threadIdx.x & 63;
+    int key[WORDS];
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) key[w] = w * 64 + lane < tokens ? key_of(ids[w * 64 + lane], vocab) : vocab;
+    const int64_t waves = (int64_t)gridDim.x * 4, sums = (int64_t)tokens * spans;
+    int64_t n = (int64_t)blockIdx.x * 4 + wave_of();
+    if (n < sums) {
+        const int t = (int)(n / spans), c0 = (int)(n % spans) * (64 * E);
+        int mine = vocab;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w)
+            if (w == t / 64) mine = __builtin_amdgcn_readlane(key[w], t % 64);
+        uint64_t same[WORDS];
+        bool first = mine < vocab;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            same[w] = __ballot(key[w] == mine);
+            if (w < t / 64 ? same[w] != 0 : w == t / 64 && (same[w] & ((1ull << t % 64) - 1))) first = false;
+        }
+        if (first) {
+            const Columns<E> at(c0, lane, width);
+            float sum[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) sum[j] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                uint64_t left = same[w];
+                while (left) {
+                    u32x4 r[AHEAD][R];
+                    const int there = min(AHEAD, __popcll(left));
+                    int l = 0;
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        if (left) l = __builtin_ctzll(left);            // else the last one again
+                        left &= left - 1;
+                        const T *row = dy + (int64_t)(w * 64 + l) * lddy;
+                        if (at.whole) {
+#pragma unroll
+                            for (int k = 0; k < R; ++k) r[u][k] = ld16<true>(row + at.from + k * VE<T>);
+                        } else {
+                            load_e<T, E>(row, at.c, width, r[u]);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        if (u >= there) break;
+                        float f[E];
+                        widen_e<T, E>(r[u], f);
+#pragma unroll
+                        for (int j = 0; j < E; ++j) sum[j] += f[j];
+                    }
+                }
+            }
+            put<W, E, ADD>(dw + (int64_t)mine * lddw, at.c, width, scale, sum);
+        }
+        return;
+    }
+    if (ADD) return;
+    const int64_t row_bytes = width * (int64_t)sizeof(W), parts = (row_bytes + 4095) / 4096;
+    for (n -= sums; n < vocab * parts; n += waves - sums) {
+        const int64_t v = n / parts;
+        bool named = false;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) named |= key[w] == (int)v;
+        if (__ballot(named) == 0) fill_part((char *)(dw + v * lddw), n % parts, row_bytes, lane);
     }
 }
 
@@ -502,11 +638,14 @@ int bits_of(int64_t n)
     while (n >> b) ++b;
     return b;
 }
-// 8 rows to a piece, and 2 048 pieces at most.
+// 8 rows to a piece, and at most 2^20 / width pieces within 512 to 2 048.  More make more partial sums, fewer too few wavefronts: 65536 tokens of 50304 x 2048
+// bf16, half of them one, 115 us in 512, 120 in 1 024, 134 in 2 048; 60000 of 131072 x 768 bf16 into f32 126, 116 and 119.
 Cut cut(int64_t tokens, int64_t vocab, int64_t width)
 {
     Cut c{};
-    c.piece = (int)((tokens + 2047) / 2048);
+    int64_t most = (1 << 20) / width;
+    most = most < 512 ? 512 : most > 2048 ? 2048 : most;
+    c.piece = (int)((tokens + most - 1) / most);
     if (c.piece < 8) c.piece = 8;
     c.pieces = (int)((tokens + c.piece - 1) / c.piece);
     c.ldp = (int)up(width, 8);
@@ -518,7 +657,7 @@ Cut cut(int64_t tokens, int64_t vocab, int64_t width)
     c.stretches = (int)((tokens + c.stretch - 1) / c.stretch);
     c.lists = up(tokens * 4, 256);
     c.counts = tokens <= FEW ? 0 : up((int64_t)c.stretches * 4 << c.bits, 256);
-    c.bytes = tokens == 0 ? 0 : (tokens <= FEW ? 2 : 4) * c.lists + c.counts + (c.pieces > 1 ? (int64_t)c.pieces * 2 * c.ldp * 4 : 0);
+    c.bytes = tokens <= HANDFUL ? 0 : (tokens <= FEW ? 2 : 4) * c.lists + c.counts + (c.pieces > 1 ? (int64_t)c.pieces * 2 * c.ldp * 4 : 0);
     return c;
 }
 
@@ -554,6 +693,17 @@ template <typename T, typename W, typename I>
 int bwd(int64_t tokens, int vocab, int width, const I *ids, const T *dy, int64_t lddy, float scale, W *dw, int64_t lddw, bool add, char *ws,
         hipStream_t s)
 {
+    if (tokens <= HANDFUL) {
+        const int span = 64 * EACH<T, W>, spans = (width + span - 1) / span;
+        const int64_t zeros = add ? 0 : vocab * ((width * (int64_t)sizeof(W) + 4095) / 4096);
+        const int64_t waves = tokens * spans + (zeros < 16384 ? zeros : 16384);
+        if (waves == 0) return 0;
+        // (a wavefront of zeros at least, whatever the last workgroup leaves of them)
+        const unsigned blocks = (unsigned)((waves + 3) / 4);
+        if (add) kt_embedding_handful_kernel<T, W, I, true><<<blocks, 256, 0, s>>>(ids, dy, lddy, dw, lddw, scale, (int)tokens, vocab, width, spans);
+        else kt_embedding_handful_kernel<T, W, I, false><<<blocks, 256, 0, s>>>(ids, dy, lddy, dw, lddw, scale, (int)tokens, vocab, width, spans);
+        return (int)hipGetLastError();
+    }
     const Cut c = cut(tokens, vocab, width);
     // zeros: a share of them beside every kernel of the sort
     Fill all{(char *)dw, lddw * (int64_t)sizeof(W), width * (int64_t)sizeof(W), 1, 0, 0};
@@ -589,7 +739,6 @@ int bwd(int64_t tokens, int vocab, int width, const I *ids, const T *dy, int64_t
                      share(2 * k + 1, of), s);
         if (e) return e;
     }
-    if (tokens == 0) return 0;
     float *parts = (float *)(ws + (tokens <= FEW ? 2 : 4) * c.lists + c.counts);
     if (add) return sums<T, W, true>(c, keys, order, dy, lddy, dw, lddw, parts, scale, (int)tokens, vocab, width, s);
     return sums<T, W, false>(c, keys, order, dy, lddy, dw, lddw, parts, scale, (int)tokens, vocab, width, s);
