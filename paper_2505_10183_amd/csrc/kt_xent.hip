@@ -7,8 +7,8 @@
 // dz is rounded to bf16 as an operand of bf16 products, as attention's probabilities are: its error, 2^-9 of an element's size, is below
 // that of the result's own rounding once some elements of either sign are added.
 //
-// Tokens without a target (or with dloss 0) take no part: their rows are made zeros where they are read, whatever they hold, tiles and steps
-// that hold no others are left out.
+// Tokens without a target (or with dloss 0) take no part: the backward pass, and the forward pass where it is long, list the others and copy their rows
+// of x one after another, so that the products are made of those alone, and what the rows of the others hold reaches nothing.
 #include "kt_mfma.h"
 
 namespace {
@@ -42,14 +42,8 @@ template <typename T> struct Operand {
     int count;                      // of m or n; a multiple of 16 bytes where those are adjacent
 };
 
-typedef const uint64_t __attribute__((address_space(4))) *Words;
-// Which of the tokens of the step at k take part, a bit each; null: all of them.
-template <typename T> __device__ __forceinline__ uint64_t live_of(Words live, int k)
-{
-    if (!live) return ~0ull;
-    if constexpr (STEP<T> == 64) return live[k >> 6];
-    else return live[k >> 6] >> (k & 63) & 0xffffffffu;
-}
+// A number that a kernel before has written, the same for all.
+__device__ __forceinline__ int scalar(const int *p) { return *(const int __attribute__((address_space(4))) *)(uintptr_t)p; }
 
 // Tiles of one operand on their way from memory to LDS, SIDE of m or n by STEP of k.
 template <typename T, int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct Bring {
@@ -73,12 +67,10 @@ template <typename T, int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct Bring
             at[u] = (ALONG ? row : c) < count ? (row * (int)ld + c) * (int)sizeof(T) : INT32_MIN;
         }
     }
-    // The steps from k on, `left` of them until the end, into `tile`, as N loads one by one.  What lies past an end is zeros and is not read, and so
-    // are steps whose bit of `live` is 0 (across only).
+    // The steps from k on, `left` of them until the end, into `tile`, as N loads one by one.  What lies past an end is zeros and is not read.
     u32x4 rs;
     uint32_t to;
-    uint64_t live;
-    __device__ __forceinline__ void aim(char *tile, int k, int left, uint64_t live_)
+    __device__ __forceinline__ void aim(char *tile, int k, int left)
     {
         const int up = (min(left, K) + V - 1) / V * V;
         if (ALONG && left < K) {
@@ -90,14 +82,12 @@ template <typename T, int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct Bring
         const int bytes = (ALONG ? (count - 1) * (int)ld + up : (min(left, K) - 1) * (int)ld + count) * (int)sizeof(T);
         rs = u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
         to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
-        live = live_;
     }
     __device__ __forceinline__ void load(int u) const
     {
-        const int off = ALONG || (live >> row_of(u) & 1) ? at[u] : INT32_MIN;
         // as Feed::bring
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     :: "s"(to + u * BLOCK * 16), "v"(off), "s"(rs) : "memory");
+                     :: "s"(to + u * BLOCK * 16), "v"(at[u]), "s"(rs) : "memory");
     }
 };
 
@@ -157,9 +147,10 @@ template <int LATER> __device__ __forceinline__ void meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LATER) : "memory");
 }
 
+// live: how many of n (B along k) or of the steps (B across) there are, or null: all.
 // E: what becomes of the tile.  E::skip(n0, count): nothing to multiply;  E::begin(acc, ...) the sums' start;  E::end(acc, ...).
 template <typename T, typename S, bool AA, bool BA, typename E>
-__global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a, Operand<T> b, int steps, int piece, const uint64_t *live_, int mt, int nt, E e)
+__global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a, Operand<T> b, int steps, int piece, const int *live, int mt, int nt, E e)
 {
     constexpr int K = STEP<T>;
     typedef Bring<T, S::BM, S::BLOCK, AA, true> BringA;
@@ -168,8 +159,17 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
     constexpr int ABYTES = S::BM * ROW, SLOT = (S::BM + S::BN) * ROW, LOADS = BringA::N + BringB::N, SLOTS = S::SLOTS;
     extern __shared__ __align__(16) char lds[];             // SLOTS slots
 
-    const Words live = (Words)(uintptr_t)live_;
     const int wave = wave_id(), lane = threadIdx.x & 63;
+    if (live) {
+        const int n = scalar(live);
+        if constexpr (BA) {
+            nt = (n + S::BN - 1) / S::BN;
+            if ((int)blockIdx.x >= mt * nt) return;
+        } else {
+            steps = n;
+            piece = ((n + (int)gridDim.y - 1) / (int)gridDim.y + 63) / 64 * 64;
+        }
+    }
     const Place at = place(blockIdx.x, mt, nt);
     const int m0 = at.m * S::BM, n0 = at.n * S::BN, wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
     const int k0 = blockIdx.y * piece, k1 = min(steps, k0 + piece);
@@ -182,16 +182,9 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
     if (!e.skip(n0, S::BN)) {
         BringA from_a(a, m0);
         BringB from_b(b, n0);
-        // the next step that has a live token
-        auto next = [&](int k) {
-            if constexpr (!AA && !BA)
-                while (k < k1 && live_of<T>(live, k) == 0) k += K;
-            return k;
-        };
         auto aim = [&](char *to, int k) __attribute__((always_inline)) {
-            const uint64_t bits = !AA && !BA ? live_of<T>(live, k) : ~0ull;
-            from_a.aim(to, k, k1 - k, bits);
-            from_b.aim(to + ABYTES, k, k1 - k, bits);
+            from_a.aim(to, k, k1 - k);
+            from_b.aim(to + ABYTES, k, k1 - k);
         };
         auto load = [&](auto u0) __attribute__((always_inline)) {
             constexpr int u = u0;
@@ -208,8 +201,8 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
             else if constexpr (r <= S::FN) fb[c % 2][r - 1] = fragment<T, S::BN, BA, false>(slot + ABYTES, wn + 32 * (r - 1), c);
             else fa[c % 2][r - S::FN] = fragment<T, S::BM, AA, true>(slot, wm + 32 * (r - S::FN), c);
         };
-        int k = next(k0), ahead = 0;            // the next step to bring; steps brought and not done
-        for (; ahead < SLOTS && k < k1; ++ahead, k = next(k + K)) {
+        int k = k0, ahead = 0;            // the next step to bring; steps brought and not done
+        for (; ahead < SLOTS && k < k1; ++ahead, k += K) {
             aim(lds + ahead * SLOT, k);
             span<0, LOADS>(load);
         }
@@ -244,7 +237,7 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
-            if (more) k = next(k + K);
+            if (more) k += K;
             else --ahead;
             slot = after;
         }
@@ -266,8 +259,9 @@ template <typename I> __device__ __forceinline__ int target_of(const I *targets,
 
 // 32 rows (lanes) of FM * 32 columns to memory in whole lines: each lane's 16 neighbouring columns go into this wavefront's part of LDS and
 // come back a row after the other.  The chunks of a row are exchanged, so that lanes of different rows use different banks.
-// f(i, values): the 16 values of column 32 i + 16 h on;  out: the matrix at the first row and column;  rows, cols: what of it is there.
-template <int FM, typename G, typename F> __device__ __forceinline__ void store_rows(char *scratch, G *out, int64_t ld, int rows, int cols, F f)
+// f(i, values): the 16 values of column 32 i + 16 h on;  out: the matrix at its first row and this first column;  first, rows, cols: the first row, and what
+// of them is there;  map: where a row goes, or null.
+template <int FM, typename G, typename F> __device__ __forceinline__ void store_rows(char *scratch, G *out, int64_t ld, int first, int rows, int cols, const int *map, F f)
 {
     constexpr int CHUNKS = FM * 32 / VE<G>;
     static_assert((CHUNKS & (CHUNKS - 1)) == 0, "chunks of a row are exchanged among a power of two");
@@ -286,7 +280,7 @@ template <int FM, typename G, typename F> __device__ __forceinline__ void store_
     for (int u = 0; u < 32 * CHUNKS / 64; ++u) {
         const int n = u * 64 + lane, row = n / CHUNKS, c = n % CHUNKS;
         const u32x4 v = to[row * CHUNKS + (c ^ (row & (CHUNKS - 1)))];
-        if (row < rows && c * VE<G> < cols) st_chunk(out + row * ld, c * VE<G>, cols, v);
+        if (row < rows && c * VE<G> < cols) st_chunk(out + (map ? map[first + row] : first + row) * ld, c * VE<G>, cols, v);
     }
 }
 
@@ -297,20 +291,24 @@ template <typename I> struct Stats {
     f32x2 *parts;                   // [part][tokens]
     float *hit;                     // [tokens]
     const I *targets;
+    const int *map, *live;          // the token of each row of x and their number, or null: all tokens
     int tokens, vocab, first, end_;         // the piece of the vocabulary: rows [first, end)
     int part0;
     __device__ __forceinline__ bool skip(int n0, int count) const
     {
-        bool any = false;
-        for (int i = threadIdx.x; i < count; i += blockDim.x) any |= target_of(targets, n0 + i, tokens, vocab) >= 0;
-        return !__syncthreads_or(any);
+        if (live) return false;
+        bool any = false;       // every wavefront for itself
+        for (int i = threadIdx.x & 63; i < count; i += 64) any |= target_of(targets, n0 + i, tokens, vocab) >= 0;
+        return __ballot(any) == 0;
     }
     template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
     template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int part, char *) const
     {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int t = n + 32 * j, want = target_of(targets, t, tokens, vocab) - first - m, room = end_ - first - m;
+            int t = n + 32 * j;
+            if (live) t = t < scalar(live) ? map[t] : tokens;
+            const int want = target_of(targets, t, tokens, vocab) - first - m, room = end_ - first - m;
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
@@ -359,69 +357,52 @@ template <typename I> struct Stats {
     }
 };
 
-// Backward: dz of a piece of the vocabulary, rows of tokens `ld` apart; columns past the vocabulary and rows of tokens that take
-// no part are zeros.
+// Backward: dz of a piece of the vocabulary, rows of tokens `ld` apart; columns past the vocabulary are zeros.
 template <typename T, typename I> struct Slope {
     static constexpr bool ROWS = true;
     T *dz;
     int64_t ld;
     const float *lse, *dloss;
     const I *targets;
-    const uint64_t *live;
+    const int *map, *live;          // the token of each row, and their number
     int tokens, vocab, first, end_;
-    __device__ __forceinline__ bool skip(int n0, int count) const
-    {
-        uint64_t any = 0;
-        for (int i = 0; i < count && n0 + i < tokens; i += 64) any |= ((Words)(uintptr_t)live)[(n0 + i) >> 6];
-        return any == 0;
-    }
+    __device__ __forceinline__ bool skip(int, int) const { return false; }
     template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
     template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int, char *scratch) const
     {
         const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int t = n + 32 * j, first_t = t - l;
-            if (first_t >= tokens) continue;
-            const int at = min(t, tokens - 1), target = target_of(targets, at, tokens, vocab) - first, room = end_ - first;
+            const int row = n + 32 * j, first_row = row - l, rows = scalar(live);
+            if (first_row >= rows) continue;
+            const int at = map[min(row, rows - 1)], target = (int)targets[at] - first, room = end_ - first;
             const float up = dloss[at], base = lse[at];
-            const bool on = live[at >> 6] >> (at & 63) & 1;
-            store_rows<FM>(scratch, dz + first_t * ld + m0, ld, tokens - first_t, (int)ld - m0, [&](int i, float *f) {
+            store_rows<FM>(scratch, dz + m0, ld, first_row, rows - first_row, (int)ld - m0, nullptr, [&](int i, float *f) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int v = m + 32 * i + r;
                     const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E) - (v == target ? 1.0f : 0.0f);
-                    f[r] = on && v < room ? p * up : 0.0f;
+                    f[r] = v < room ? p * up : 0.0f;
                 }
             });
         }
     }
     __device__ __forceinline__ void few(f32x4 z, int v, int t, int) const
     {
-        if (t >= tokens || v >= ld) return;
-        const int want = target_of(targets, t, tokens, vocab) - first - v, room = end_ - first - v;
-        const bool on = live[t >> 6] >> (t & 63) & 1;
-        const float up = dloss[t], base = lse[t];
+        if (t >= scalar(live) || v >= ld) return;
+        const int at = map[t], want = (int)targets[at] - first - v, room = end_ - first - v;
+        const float up = dloss[at], base = lse[at];
         T f[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const float p = __builtin_amdgcn_exp2f((z[r] - base) * LOG2E) - (r == want ? 1.0f : 0.0f);
-            f[r] = (T)(on && r < room ? p * up : 0.0f);
+            f[r] = (T)(r < room ? p * up : 0.0f);
         }
         T *row = dz + t * ld + v;
         if constexpr (sizeof(T) == 2) *(u32x2 *)row = __builtin_bit_cast(u32x2, f);
         else *(u32x4 *)row = __builtin_bit_cast(u32x4, f);
     }
 };
-
-// Whether none of the rows [n0, n0 + count) takes part; null: all do.
-__device__ __forceinline__ bool all_dead(const uint64_t *live, int n0, int count, int rows)
-{
-    if (!live) return false;
-    uint64_t any = 0;
-    for (int i = 0; i < count && n0 + i < rows; i += 64) any |= ((Words)(uintptr_t)live)[(n0 + i) >> 6];
-    return any == 0;
-}
 
 // Sums that the next piece of the vocabulary goes on with, as the lanes hold them: nobody else reads them.
 template <int FM, int FN> __device__ __forceinline__ int64_t carried()
@@ -446,9 +427,7 @@ struct Carry {
     static constexpr bool ROWS = false;
     float *sums;
     bool first;
-    const uint64_t *live;           // of the rows, or null: all
-    int rows;
-    __device__ __forceinline__ bool skip(int n0, int count) const { return all_dead(live, n0, count, rows); }
+    __device__ __forceinline__ bool skip(int, int) const { return false; }
     template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int, int) const
     {
         if (!first) resume(sums, acc);
@@ -476,9 +455,9 @@ template <typename G> struct Result {
     G *out;
     int64_t ld, apart;              // rows; matrices of the pieces of k
     const float *sums;              // what Carry left, or null
-    const uint64_t *live;           // rows that are not zeros, or null: all
+    const int *map, *live;          // where a row goes, and how many there are, or null
     int rows, cols;
-    __device__ __forceinline__ bool skip(int n0, int count) const { return all_dead(live, n0, count, rows); }
+    __device__ __forceinline__ bool skip(int, int) const { return false; }
     template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int, int) const
     {
         if (sums) resume(sums, acc);
@@ -488,13 +467,11 @@ template <typename G> struct Result {
         const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int row = n + 32 * j, first = row - l;
-            if (first >= rows || m0 >= cols) continue;
-            const int at = min(row, rows - 1);
-            const bool on = !live || (live[at >> 6] >> (at & 63) & 1);
-            store_rows<FM>(scratch, out + blockIdx.y * apart + first * ld + m0, ld, rows - first, cols - m0, [&](int i, float *f) {
+            const int first = n + 32 * j - l, end = live ? scalar(live) : rows;
+            if (first >= end || m0 >= cols) continue;
+            store_rows<FM>(scratch, out + blockIdx.y * apart + m0, ld, first, end - first, cols - m0, map, [&](int i, float *f) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) f[r] = on ? acc[i][j][r] : 0.0f;
+                for (int r = 0; r < 16; ++r) f[r] = acc[i][j][r];
             });
         }
     }
@@ -623,30 +600,64 @@ __global__ __launch_bounds__(256) void kt_xent_join_kernel(const f32x2 *parts, i
     if (lse) lse[t] = on ? all : 0.0f;
 }
 
-// A bit for every token that takes part.
+// The tokens that take part, in their order, and their number.  A workgroup counts those before its own by itself, which takes one launch.
 template <typename I>
-__global__ __launch_bounds__(256) void kt_xent_live_kernel(const I *targets, const float *dloss, int tokens, int vocab, uint64_t *live)
+__global__ __launch_bounds__(1024) void kt_xent_list_kernel(const I *targets, const float *dloss, int tokens, int vocab, int *map, int *live)
 {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const bool on = t < tokens && target_of(targets, (int)min(t, (int64_t)INT32_MAX), tokens, vocab) >= 0 && dloss[t] != 0.0f;
+    __shared__ int before[16], mine[16];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, first = blockIdx.x * 1024, t = first + threadIdx.x;
+    auto takes_part = [&](int t) { return target_of(targets, t, tokens, vocab) >= 0 && (!dloss || dloss[t] != 0.0f); };
+    int n = 0;
+#pragma unroll 4
+    for (int at = threadIdx.x; at < first; at += 1024) n += takes_part(at);
+    for (int d = 32; d; d /= 2) n += __shfl_xor(n, d);
+    const bool on = takes_part(t);
     const uint64_t word = __ballot(on);
-    if ((threadIdx.x & 63) == 0 && t < tokens) live[t >> 6] = word;
+    if (lane == 0) {
+        before[wave] = n;
+        mine[wave] = __popcll(word);
+    }
+    __syncthreads();
+    int at = 0, all = 0;
+    for (int w = 0; w < 16; ++w) {
+        at += before[w] + (w < wave ? mine[w] : 0);
+        all += before[w] + mine[w];
+    }
+    if (on) map[at + __popcll(word & ((1ull << lane) - 1))] = t;
+    if (threadIdx.x == 0 && blockIdx.x == gridDim.x - 1) *live = all;
 }
 
-// The sum of pieces of k, in their order; rows of the pieces `ldp` apart.
+// Their rows of x one after another, zeros up to `ld`; where dx is given, zeros into its rows of the other tokens.
+template <typename T, typename I>
+__global__ __launch_bounds__(256) void kt_xent_gather_kernel(const T *x, int64_t ldx, int cols, T *y, int64_t ld, const int *map, const int *live,
+                                                             const I *targets, const float *dloss, int tokens, int vocab, T *dx, int64_t lddx)
+{
+    const int parts = (int)((ld + 64 * VE<T> - 1) / (64 * VE<T>)), count = *live;
+    for (int64_t n = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; n < (int64_t)tokens * parts; n += (int64_t)gridDim.x * 4) {
+        const int t = (int)(n / parts), c = (int)(n % parts) * 64 * VE<T> + (threadIdx.x & 63) * VE<T>;
+        if (c >= ld) continue;
+        if (t < count) *(u32x4 *)(y + t * ld + c) = ld_chunk(x + map[t] * ldx, c, cols);
+        if (dx && c < cols && !(target_of(targets, t, tokens, vocab) >= 0 && dloss[t] != 0.0f)) st_chunk(dx + t * lddx, c, cols, u32x4{0, 0, 0, 0});
+    }
+}
+
+// The sum of pieces of k, in their order; rows of the pieces `ldp` apart.  map, live: as Result has them.
 template <typename G>
-__global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, int pieces, int64_t apart, int ldp, int rows, int cols, G *out, int64_t ld)
+__global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, int pieces, int64_t apart, int ldp, int rows, int cols, G *out, int64_t ld, const int *map,
+                                                           const int *live)
 {
     const int across = (cols + 3) / 4;
+    if (live) rows = *live;
     for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < (int64_t)rows * across; n += (int64_t)gridDim.x * 256) {
         const int64_t row = n / across;
         const int c = (int)(n % across) * 4;
         const float *p = parts + row * ldp + c;
+        const int64_t to = (map ? map[row] : row) * ld;
         f32x4 s = *(const f32x4 *)p;
         for (int k = 1; k < pieces; ++k) s += *(const f32x4 *)(p + k * apart);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (c + j < cols) out[row * ld + c + j] = (G)s[j];
+            if (c + j < cols) out[to + c + j] = (G)s[j];
     }
 }
 
@@ -702,7 +713,8 @@ struct Plan {
     int side;                       // of the forward pass's tiles
     int64_t ldp;                    // backward: elements to a row of sums
     Cut kx;                         // of dx over a piece of the vocabulary
-    int64_t x, w, parts, hit, dz, live, acc, sums, bytes;       // where in the workspace
+    bool list;                      // whether the tokens that take part are listed
+    int64_t x, w, parts, hit, dz, map, live, acc, sums, bytes;  // where in the workspace
 };
 int64_t at_most(int64_t a, int64_t b) { return a < b ? a : b; }
 // Rows of a multiple of 256 that keep rows * of below `most`.
@@ -732,12 +744,15 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
     const bool few = tokens <= FEW;
     p.x = take(!bwd && few ? 0 : tokens * p.wide * p.es);
     p.w = take(!bwd && few ? 0 : p.piece * p.wide * p.es);
+    // a list and a copy of x cost some 6 us and its bytes twice: worth while for the forward pass from some 100 us on
+    p.list = bwd || (double)tokens * vocab * width * (dt == KT_F32 ? 8 : 1) > 5e10;
+    p.map = take(p.list ? tokens * 4 : 0);
+    p.live = take(p.list ? 4 : 0);
     if (!bwd) {
         p.parts = take((few ? over(vocab, 16) : over(vocab, p.side) * 2) * tokens * 8);
         p.hit = take(tokens * 4);
         return p;
     }
-    p.live = take(over(tokens, 64) * 8);
     p.dz = take(tokens * p.most * p.es);
     p.kx = cut_of(dt, width, tokens, at_most(p.most, vocab), MOST_PIECES);
     const int64_t side = p.kx.side;
@@ -754,7 +769,7 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
 }
 
 template <typename T, typename S, bool AA, bool BA, typename E>
-int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Cut &k, const uint64_t *live, const E &e, hipStream_t s)
+int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const Cut &k, const int *live, const E &e, hipStream_t s)
 {
     constexpr int LDS = S::SLOTS * (S::BM + S::BN) * ROW;
     const auto kernel = kt_xent_product_kernel<T, S, AA, BA, E>;
@@ -768,7 +783,7 @@ int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n,
 }
 // The product of A [m x steps] and B [n x steps].
 template <typename T, bool AA, bool BA, typename E>
-int product(const Cut &k, const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const uint64_t *live, const E &e, hipStream_t s)
+int product(const Cut &k, const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const int *live, const E &e, hipStream_t s)
 {
     if constexpr (sizeof(T) == 2) {
         if (k.side == 256) return launch_tiles<T, Big, AA, BA>(a, m, b, n, steps, k, live, e, s);
@@ -808,38 +823,55 @@ template <typename T> int aligned_rows(bool as_is, const T *x, int64_t ldx, int6
     return (int)hipGetLastError();
 }
 
+// The list of the tokens that take part and their rows of x; zeros in dx's rows of the others.
+template <typename T, typename I>
+int list(const T *x, int64_t ldx, int64_t width, const I *targets, const float *dloss, int64_t tokens, int64_t vocab, T *copy, int64_t wide, int *map,
+         int *live, T *dx, int64_t lddx, hipStream_t s)
+{
+    kt_xent_list_kernel<I><<<(unsigned)over(tokens, 1024), 1024, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, map, live);
+    KT_GO((int)hipGetLastError());
+    const int64_t blocks = over(tokens * over(wide, 64 * VE<T>), 4);
+    kt_xent_gather_kernel<T, I><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, map, live, targets, dloss, (int)tokens, (int)vocab, dx, lddx);
+    return (int)hipGetLastError();
+}
+
 template <typename T, typename I>
 int fwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, int64_t ldx, const T *w, int64_t ldw, const I *targets, float *loss,
         float *lse, char *ws, hipStream_t s)
 {
     const Plan p = plan_of(dt, tokens, vocab, width, false);
     f32x2 *parts = (f32x2 *)(ws + p.parts);
+    int *const map = p.list ? (int *)(ws + p.map) : nullptr, *const live = p.list ? (int *)(ws + p.live) : nullptr;
     float *hit = (float *)(ws + p.hit);
     const bool w_as_is = plain(w, ldw, width);
     Operand<T> a, b;
     int count = (int)over(vocab, p.side) * 2;
     if (tokens <= FEW) {
-        const Stats<I> e{parts, hit, targets, (int)tokens, (int)vocab, 0, (int)vocab, 0};
+        const Stats<I> e{parts, hit, targets, nullptr, nullptr, (int)tokens, (int)vocab, 0, (int)vocab, 0};
         KT_GO(few(w, ldw, vocab, x, ldx, tokens, width, e, s));
         count = (int)over(vocab, 16);
+    } else if (p.list) {
+        KT_GO((list<T, I>(x, ldx, width, targets, nullptr, tokens, vocab, (T *)(ws + p.x), p.wide, map, live, nullptr, 0, s)));
+        b = Operand<T>{(T *)(ws + p.x), p.wide, (int)tokens};
     } else {
         KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
     }
     for (int64_t v = tokens <= FEW ? vocab : 0, rows; v < vocab; v += rows) {
         rows = at_most(w_as_is ? p.most : p.piece, vocab - v);
         KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
-        const Stats<I> e{parts, hit, targets, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / (p.side / 2))};
-        KT_GO((product<T, true, true>(Cut{p.side, 1, (int)up(width, 64)}, a, rows, b, tokens, width, nullptr, e, s)));
+        const Stats<I> e{parts, hit, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / (p.side / 2))};
+        KT_GO((product<T, true, true>(Cut{p.side, 1, (int)up(width, 64)}, a, rows, b, tokens, width, live, e, s)));
     }
     if (tokens >= 512) kt_xent_join_kernel<I, 32><<<(unsigned)over(tokens, 32), 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
     else kt_xent_join_kernel<I, 1><<<(unsigned)tokens, 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
     return (int)hipGetLastError();
 }
 
-template <typename G> int sum(const float *parts, const Cut &k, int64_t apart, int64_t ldp, int64_t rows, int64_t cols, G *out, int64_t ld, hipStream_t s)
+template <typename G> int sum(const float *parts, const Cut &k, int64_t apart, int64_t ldp, int64_t rows, int64_t cols, G *out, int64_t ld, const int *map, const int *live,
+                              hipStream_t s)
 {
     const int64_t blocks = over(rows * over(cols, 4), 256);
-    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.pieces, apart, (int)ldp, (int)rows, (int)cols, out, ld);
+    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.pieces, apart, (int)ldp, (int)rows, (int)cols, out, ld, map, live);
     return (int)hipGetLastError();
 }
 
@@ -848,53 +880,51 @@ int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *
         const I *targets, const float *lse, T *dx, int64_t lddx, T *dw, int64_t lddw, char *ws, hipStream_t s)
 {
     const Plan p = plan_of(dt, tokens, vocab, width, true);
-    uint64_t *live = (uint64_t *)(ws + p.live);
+    int *const map = (int *)(ws + p.map), *const live = (int *)(ws + p.live);
     T *dz = (T *)(ws + p.dz);
     float *acc = (float *)(ws + p.acc), *sums = (float *)(ws + p.sums);
     const bool w_as_is = plain(w, ldw, width);
     const int64_t cols = up(width, VE<T>);              // of an operand: what a copy has past the width is zeros
     const int64_t piece = w_as_is ? p.most : p.piece;
-    Operand<T> a, b;
-    KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
-    if (tokens) {
-        kt_xent_live_kernel<I><<<(unsigned)over(tokens, 256), 256, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, live);
-        KT_GO((int)hipGetLastError());
-    }
+    T *const copy = (T *)(ws + p.x);
+    Operand<T> a;
+    const Operand<T> b{copy, p.wide, (int)tokens};
+    if (tokens) KT_GO((list<T, I>(x, ldx, width, targets, dloss, tokens, vocab, copy, p.wide, map, live, dx, lddx, s)));
     for (int64_t v = 0, rows; v < vocab; v += rows) {
         rows = at_most(piece, vocab - v);
         if (tokens) {
             KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
-            const Slope<T, I> e{dz, p.most, lse, dloss, targets, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
-            if (tokens <= FEW) KT_GO(few(w + v * ldw, ldw, rows, x, ldx, tokens, width, e, s));
-            else KT_GO((product<T, true, true>(cut_of(dt, rows, tokens, width, 1), a, rows, b, tokens, width, nullptr, e, s)));
+            const Slope<T, I> e{dz, p.most, lse, dloss, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
+            if (tokens <= FEW) KT_GO(few(w + v * ldw, ldw, rows, (const T *)copy, p.wide, tokens, width, e, s));
+            else KT_GO((product<T, true, true>(cut_of(dt, rows, tokens, width, 1), a, rows, b, tokens, width, live, e, s)));
         }
         if (dx && tokens) {
             const Operand<T> wide{a.p, a.ld, (int)cols}, slope{dz, p.most, (int)tokens};
             const bool first = v == 0, last = v + rows == vocab;
             const Cut k{p.kx.side, p.kx.pieces, (int)up(over(rows, p.kx.pieces), 64)};
             if (!last) {
-                const Carry e{acc, first, live, (int)tokens};
-                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, nullptr, e, s)));
+                const Carry e{acc, first};
+                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else if (k.pieces == 1) {
-                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, live, (int)tokens, (int)width};
-                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, nullptr, e, s)));
+                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, map, live, (int)tokens, (int)width};
+                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else {
                 const int64_t apart = tokens * p.ldp;
-                const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, live, (int)tokens, (int)p.ldp};
-                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, nullptr, e, s)));
-                KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, s));
+                const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, nullptr, live, (int)tokens, (int)p.ldp};
+                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
+                KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, map, live, s));
             }
         }
         if (dw) {
             const Operand<T> wide{b.p, b.ld, (int)cols}, slope{dz, p.most, (int)up(rows, VE<T>)};
             const Cut k = cut_of(dt, width, rows, tokens, MOST_PIECES);
             if (k.pieces == 1) {
-                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, (int)rows, (int)width};
-                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, live, e, s)));
+                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, nullptr, (int)rows, (int)width};
+                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
             } else {
-                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, (int)rows, (int)p.ldp};
-                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, live, e, s)));
-                KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, s));
+                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, nullptr, (int)rows, (int)p.ldp};
+                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
+                KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, nullptr, nullptr, s));
             }
         }
     }
