@@ -1,8 +1,10 @@
 /*
- * kt operators -- the parts of a transformer block's training pass that make
- * the gradients which kt.h packs, reduces and applies: layer norm with its
- * backward pass, activation checkpoints in 8 bits with the weight gradient of
- * a linear layer from them, and attention with its backward pass.
+ * kt operators -- the parts of a language model's training pass that make the
+ * gradients which kt.h packs, reduces and applies.  In a transformer block: layer norm
+ * with its backward pass, activation checkpoints in 8 bits with the weight gradient of
+ * a linear layer from them, and attention with its backward pass.  At the model's two
+ * ends: the embedding lookup with the gradient of its table, and the cross entropy
+ * of a linear layer over the vocabulary with its gradients.
  *
  * The conventions of kt.h hold: status codes, kt_last_error(), device pointers
  * owned by the caller, asynchronous calls on `stream`.  Beyond them:
@@ -15,9 +17,9 @@
  *  - Weight gradients may be written where a bucket keeps them: any address
  *    that is a multiple of the element size will do.
  *  - Sums, softmax statistics and products are held in binary32; a result is
- *    rounded to bf16 once, to nearest-even.  bf16 attention rounds more on the
- *    way, as it says below.  Results depend on the arguments alone: no atomics,
- *    every sum has a fixed order.
+ *    rounded to bf16 once, to nearest-even.  bf16 attention and cross entropy round
+ *    more on the way, as they say below.  Results depend on the arguments alone: no
+ *    sum is made by atomics, every one has a fixed order.
  *  - A matrix [rows, cols] has adjacent columns and rows `ld` elements apart
  *    (ld >= cols).  Rows may be 0: then weight gradients are written as 0.
  *  - Outputs must not overlap inputs or each other, except where a call says so.
@@ -236,7 +238,7 @@ KT_API kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it,
  * Logits are products of dt pairs summed in binary32, and not rounded.  Where one is not
  * finite the token's loss is not either.  x and w may have any stride and start; rows that are
  * not multiples of 16 bytes, or do not begin at one, are copied into the workspace first.
- * KT_EUNSUPPORTED: more than 2^24 tokens or rows of w, 2^20 columns, 2^38 elements of x.
+ * KT_EUNSUPPORTED: more than 2^24 tokens or rows of w, 2^20 columns, 2^36 elements of x or w.
  */
 KT_API int64_t kt_linear_xent_fwd_workspace(kt_dtype dt, int64_t tokens,
                                             int64_t vocab, int64_t width);

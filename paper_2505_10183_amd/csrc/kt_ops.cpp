@@ -489,13 +489,14 @@ extern "C" kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it, in
 namespace {
 
 // 31-bit numbers in the kernels, launches of fewer than 2^32 lanes, offsets within a tile of a copy of 31 bits
-const int64_t MOST_ROWS = 1 << 24, MOST_XENT_WIDTH = 1 << 20, MOST_X = 1ll << 38;
+const int64_t MOST_ROWS = 1 << 24, MOST_XENT_WIDTH = 1 << 20, MOST_X = 1ll << 36;
 
 bool xent_sizes(int64_t tokens, int64_t vocab, int64_t width)
 {
-    return tokens >= 0 && vocab >= 1 && width >= 1 && tokens <= MOST_ROWS && vocab <= MOST_ROWS && width <= MOST_XENT_WIDTH && tokens * width <= MOST_X;
+    return tokens >= 0 && vocab >= 1 && width >= 1 && tokens <= MOST_ROWS && vocab <= MOST_ROWS && width <= MOST_XENT_WIDTH && tokens * width <= MOST_X &&
+           vocab * width <= MOST_X;
 }
-const char *const XENT_SIZES = "more than 2^24 tokens or rows of w, 2^20 columns, or 2^38 elements of x";
+const char *const XENT_SIZES = "more than 2^24 tokens or rows of w, 2^20 columns, or 2^36 elements of x or w";
 
 }  // namespace
 

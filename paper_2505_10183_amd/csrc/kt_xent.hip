@@ -694,7 +694,7 @@ Cut cut_of(kt_dtype dt, int64_t m, int64_t n, int64_t k, int64_t most)
     }
     return best;
 }
-constexpr int64_t MOST_PIECES = 16;
+constexpr int64_t MOST_PIECES = 64;
 
 // Whether loads of 16 bytes can take a matrix as it is: rows at multiples of 16 bytes, offsets within a tile of 31 bits.
 template <typename T> bool plain(const T *p, int64_t ld, int64_t width)
@@ -702,7 +702,7 @@ template <typename T> bool plain(const T *p, int64_t ld, int64_t width)
     return rows_of_16(p, ld) && width % VE<T> == 0 && ld * (int64_t)sizeof(T) <= 1 << 22;
 }
 
-// What a call needs of the workspace, and its cut.  Other matrices are copied to rows of a multiple of 16 bytes first (the weight up to 32 MiB of it
+// What a call needs of the workspace, and its cut.  Other matrices are copied to rows of a multiple of 16 bytes first (the weight up to 128 MiB of it
 // at a time), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
 constexpr int64_t FEW = 32;         // tokens whose logits kt_xent_few_kernel makes
 
@@ -729,7 +729,7 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
     Plan p{};
     p.es = dt == KT_F32 ? 4 : 2;
     p.wide = up(width, 64);
-    p.copy = rows_in(32 << 20, p.wide * p.es, vocab);
+    p.copy = rows_in(128 << 20, p.wide * p.es, vocab);
     // backward: dz of up to 2^27 elements, 256 MiB of bf16, what the last-level cache holds; forward: a launch of up to 2^20 tiles of 256
     p.most = rows_in(bwd ? 1ll << 27 : 1ll << 36, tokens, vocab);
     if (bwd) p.most = at_most(p.most, 1 << 18);
@@ -895,7 +895,7 @@ int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *
         if (tokens) {
             KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
             const Slope<T, I> e{dz, p.most, lse, dloss, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
-            if (tokens <= FEW) KT_GO(few(w + v * ldw, ldw, rows, (const T *)copy, p.wide, tokens, width, e, s));
+            if (tokens <= FEW) KT_GO(few(a.p, a.ld, rows, (const T *)copy, p.wide, tokens, width, e, s));
             else KT_GO((product<T, true, true>(cut_of(dt, rows, tokens, width, 1), a, rows, b, tokens, width, live, e, s)));
         }
         if (dx && tokens) {

@@ -114,7 +114,7 @@ def test_tiles_and_pieces(dtype, tokens, vocab, width):
 
 
 # more vocabulary than a piece of dz takes; more of a weight at odd addresses than is copied at a time
-@pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 20000, 7003, 72), ("f32", 20000, 6657, 40), ("f32", 70, 2500, 8191), ("bf16", 5, 5001, 8191)])
+@pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 20000, 7003, 72), ("f32", 20000, 6657, 40), ("f32", 70, 9500, 8191), ("bf16", 5, 9001, 16383)])
 def test_pieces_of_the_vocabulary(dtype, tokens, vocab, width):
     c = Case(tokens, vocab, width, DT[dtype]).forward()
     c.check_forward()

@@ -23,7 +23,8 @@ BOTH = [
 
 @pytest.mark.parametrize("changes,status,word", BOTH + [
     (dict(width=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21), EUNSUPPORTED, "2^20"),
-    (dict(tokens=1 << 24, width=1 << 15, ldx=1 << 15, ldw=1 << 15), EUNSUPPORTED, "2^38"),
+    (dict(tokens=1 << 24, width=1 << 13, ldx=1 << 13, ldw=1 << 13), EUNSUPPORTED, "2^36"),
+    (dict(vocab=1 << 24, width=1 << 13, ldx=1 << 13, ldw=1 << 13), EUNSUPPORTED, "2^36"),
     (dict(loss=0), EINVAL, "NULL"), (dict(loss=at(3) + 1), EALIGN, "loss"), (dict(ws=at(5) + 8), EALIGN, "ws"), (dict(loss=at(4)), EINVAL, "overlaps"),
     (dict(loss=at(0) + 4 * 4095), EINVAL, "overlaps"), (dict(lse=at(1)), EINVAL, "overlaps"), (dict(lse=at(2)), EINVAL, "overlaps"),
     (dict(loss=at(5)), EINVAL, "overlaps")])
@@ -47,9 +48,9 @@ def test_workspace():
     for f in (L.kt_linear_xent_fwd_workspace, L.kt_linear_xent_bwd_workspace):
         assert f(F32, 0, 100, 64) == 0 and f(2, 5, 100, 64) == 0 and f(F32, -1, 100, 64) == 0 and f(F32, 5, 100, 1 << 21) == 0
         assert f(F32, 1, 1, 1) > 0
-    # dz in 2^27 elements, sums and a copy of x, 32 MiB of the weight, whatever the vocabulary, and what the last piece of it is cut into
+    # dz in 2^27 elements, sums and a copy of x, 128 MiB of the weight, whatever the vocabulary, and what the last piece of it is cut into
     for v in (50304, 1 << 20, 1 << 24):
-        assert L.kt_linear_xent_bwd_workspace(BF16, 16384, v, 2048) < 2 * (1 << 27) + 16384 * 2048 * (2 + 4) + (32 << 20) + 16 * 8192 * 2048 * 4
+        assert L.kt_linear_xent_bwd_workspace(BF16, 16384, v, 2048) < 2 * (1 << 27) + 16384 * 2048 * (2 + 4) + (128 << 20) + 64 * 8192 * 2048 * 4
 
 
 def test_binding_refuses():
