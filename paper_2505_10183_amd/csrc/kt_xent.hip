@@ -479,7 +479,7 @@ template <typename G> struct Result {
 
 // ---- logits of few tokens --------------------------------------------------------------
 //
-// Up to 32 tokens are bound by the weight's bytes: a wavefront takes 16 rows of it from memory into fragments, 64 bytes of each row a load and AHEAD
+// Few tokens are bound by the weight's bytes: a wavefront takes 16 rows of it from memory into fragments, 64 bytes of each row a load and AHEAD
 // loads on their way, with no LDS and no wait for others.  D = 16 x 16: lane l holds row (A) or token (B) l % 16, k = V (l / 16) + 0.. of 4 V, and of D the
 // token l % 16 of rows 4 (l / 16) + 0..3.
 constexpr int FEW_AHEAD = 8;
@@ -496,11 +496,10 @@ __device__ __forceinline__ void multiply16(f32x4 &d, u32x4 a, u32x4 b, float)
 
 // GROUPS of 16 tokens.  E::few(z, rows from, token, part): four logits of one token.
 template <typename T, int GROUPS, typename E>
-__global__ __launch_bounds__(256) void kt_xent_few_kernel(const T *w, int64_t ldw, int rows, const T *x, int64_t ldx, int tokens, int width, E e)
+__global__ __launch_bounds__(64) void kt_xent_few_kernel(const T *w, int64_t ldw, int rows, const T *x, int64_t ldx, int tokens, int width, E e)
 {
     constexpr int V = VE<T>, STEP_ = 4 * V;
-    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, part = blockIdx.x * 4 + wave_id(), v0 = part * 16;
-    if (v0 >= rows) return;
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, part = blockIdx.x, v0 = part * 16;
     const T *a = w + min(v0 + l, rows - 1) * ldw + g * V, *b[GROUPS];
     f32x4 z[GROUPS];
 #pragma unroll
@@ -704,7 +703,12 @@ template <typename T> bool plain(const T *p, int64_t ld, int64_t width)
 
 // What a call needs of the workspace, and its cut.  Other matrices are copied to rows of a multiple of 16 bytes first (the weight up to 128 MiB of it
 // at a time), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
-constexpr int64_t FEW = 32;         // tokens whose logits kt_xent_few_kernel makes
+// Whether kt_xent_few_kernel makes the logits: up to 16 tokens, and up to 32 where tiles would need a copy of the weight or have little to do.  us, forward
+// pass: 30 tokens of 50304 x 2048 bf16 85, in tiles 55; of 50304 x 1001 f32 93 and 150; of 5003 x 768 bf16 9.9 and 11.9; 12 of 50304 x 2048 56 and 53.
+bool few_tokens(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
+{
+    return tokens <= 16 || (tokens <= 32 && (width * (dt == KT_F32 ? 4 : 2) % 16 || vocab * width < 1 << 25));
+}
 
 struct Plan {
     int64_t es, wide;               // bytes of an element; elements to a row of a copy
@@ -741,7 +745,7 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
         p.bytes += up(bytes, 256);
         return from;
     };
-    const bool few = tokens <= FEW;
+    const bool few = few_tokens(dt, tokens, vocab, width);
     p.x = take(!bwd && few ? 0 : tokens * p.wide * p.es);
     p.w = take(!bwd && few ? 0 : p.piece * p.wide * p.es);
     // a list and a copy of x cost some 6 us and its bytes twice: worth while for the forward pass from some 100 us on
@@ -800,9 +804,9 @@ int product(const Cut &k, const Operand<T> &a, int64_t m, const Operand<T> &b, i
 
 template <typename T, typename E> int few(const T *w, int64_t ldw, int64_t rows, const T *x, int64_t ldx, int64_t tokens, int64_t width, const E &e, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)over(rows, 64);
-    if (tokens <= 16) kt_xent_few_kernel<T, 1, E><<<blocks, 256, 0, s>>>(w, ldw, (int)rows, x, ldx, (int)tokens, (int)width, e);
-    else kt_xent_few_kernel<T, 2, E><<<blocks, 256, 0, s>>>(w, ldw, (int)rows, x, ldx, (int)tokens, (int)width, e);
+    const unsigned blocks = (unsigned)over(rows, 16);
+    if (tokens <= 16) kt_xent_few_kernel<T, 1, E><<<blocks, 64, 0, s>>>(w, ldw, (int)rows, x, ldx, (int)tokens, (int)width, e);
+    else kt_xent_few_kernel<T, 2, E><<<blocks, 64, 0, s>>>(w, ldw, (int)rows, x, ldx, (int)tokens, (int)width, e);
     return (int)hipGetLastError();
 }
 
@@ -846,7 +850,7 @@ int fwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, i
     const bool w_as_is = plain(w, ldw, width);
     Operand<T> a, b;
     int count = (int)over(vocab, p.side) * 2;
-    if (tokens <= FEW) {
+    if (few_tokens(dt, tokens, vocab, width)) {
         const Stats<I> e{parts, hit, targets, nullptr, nullptr, (int)tokens, (int)vocab, 0, (int)vocab, 0};
         KT_GO(few(w, ldw, vocab, x, ldx, tokens, width, e, s));
         count = (int)over(vocab, 16);
@@ -856,7 +860,7 @@ int fwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, i
     } else {
         KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
     }
-    for (int64_t v = tokens <= FEW ? vocab : 0, rows; v < vocab; v += rows) {
+    for (int64_t v = few_tokens(dt, tokens, vocab, width) ? vocab : 0, rows; v < vocab; v += rows) {
         rows = at_most(w_as_is ? p.most : p.piece, vocab - v);
         KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
         const Stats<I> e{parts, hit, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / (p.side / 2))};
@@ -895,7 +899,7 @@ int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *
         if (tokens) {
             KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
             const Slope<T, I> e{dz, p.most, lse, dloss, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
-            if (tokens <= FEW) KT_GO(few(a.p, a.ld, rows, (const T *)copy, p.wide, tokens, width, e, s));
+            if (few_tokens(dt, tokens, vocab, width)) KT_GO(few(a.p, a.ld, rows, (const T *)copy, p.wide, tokens, width, e, s));
             else KT_GO((product<T, true, true>(cut_of(dt, rows, tokens, width, 1), a, rows, b, tokens, width, live, e, s)));
         }
         if (dx && tokens) {

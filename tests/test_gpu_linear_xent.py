@@ -91,7 +91,7 @@ class Case:
 
 
 SHAPES = [(1, 1, 1), (1, 7, 8), (2, 300, 64), (3, 1000, 100), (63, 65, 63), (64, 64, 64), (65, 129, 1001), (130, 500, 257), (257, 1023, 768),
-          (300, 5003, 200), (1, 50304, 256), (33, 4099, 2048)]
+          (300, 5003, 200), (1, 50304, 256), (33, 4099, 2048), (16, 4099, 72), (17, 4099, 72), (30, 17000, 2048), (30, 4099, 1001)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
