@@ -236,7 +236,10 @@ KT_API kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it,
  *   lse      for the backward pass; NULL: not wanted.
  *   ws       kt_linear_xent_fwd_workspace(...) bytes.
  * Logits are products of dt pairs summed in binary32, and not rounded.  Where one is not
- * finite the token's loss is not either.  x and w may have any stride and start; rows that are
+ * finite the token's loss is not either.  Large f32 products are made of three bf16 parts
+ * of each number, copied into the workspace, as near as those of the numbers themselves;
+ * bits of a number that lie under 2^-133 are lost then, and a sum that an infinite one
+ * takes part in is NaN.  x and w may have any stride and start; rows that are
  * not multiples of 16 bytes, or do not begin at one, are copied into the workspace first.
  * KT_EUNSUPPORTED: more than 2^24 tokens or rows of w, 2^20 columns, 2^36 elements of x or w.
  */
@@ -259,7 +262,7 @@ KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
  *   ws       kt_linear_xent_bwd_workspace(...) bytes: up to 2^27 elements of dz, a row of
  *            binary32 sums for each token, and copies as in the forward pass.
  * Rounding in bf16: dz is rounded to bf16 as an operand of both products.  f32 has no
- * rounding but that of its own arithmetic.
+ * rounding but that of its own arithmetic, and the parts of large products as above.
  */
 KT_API int64_t kt_linear_xent_bwd_workspace(kt_dtype dt, int64_t tokens,
                                             int64_t vocab, int64_t width);

@@ -42,6 +42,37 @@ template <typename T> struct Operand {
     int count;                      // of m or n; a multiple of 16 bytes where those are adjacent
 };
 
+// A binary32 number as three bf16 that add up to it: 8 bits of its significand each, nearest first.  A product of two such numbers is six products of bf16 pairs,
+// exact and summed in binary32, and what is left out (of the 2nd and the 3rd part, and of the 3rd ones) is below 2^-24 of it, half a step of binary32: for the
+// matrix cores six bf16 products cost six sixteenths of an f32 one.  As the sums have fewer steps, they are nearer: the log-sum-exp of 5003 logits of 4096
+// products each is off by 2.3e-6 on the average, with f32 instructions by 3.0e-6.  Of a number below 2^-110 bits under 2^-133 are lost; an infinite one times
+// a part that is 0 is NaN, so its sums are.  Rows of such numbers are groups of 32, a group the 64 bytes of each part one after another.
+struct Three {
+    uint16_t part[3];
+};
+constexpr int PLANES = 3, GROUP = 32;
+static_assert(sizeof(Three) * GROUP == 64 * PLANES, "pointers to Three count elements, a group at a time");
+
+// 8 numbers of a group, from column c % 32 = 0, 8, 16 or 24 on.  A number that is not finite is its first part, and one that would round to infinity is
+// cut off instead.
+__device__ __forceinline__ void put_three(Three *group, int c, const float *f)
+{
+    bf16x8 part[PLANES];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t bits = as_u(f[j]);
+        const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+        float first = (float)(bf16)f[j];
+        if (finite && (as_u(first) & 0x7f800000u) == 0x7f800000u) first = as_f(bits & 0xffff0000u);
+        const float left = finite ? f[j] - first : 0.0f, second = (float)(bf16)left;
+        part[0][j] = (bf16)first;
+        part[1][j] = (bf16)second;
+        part[2][j] = (bf16)(left - second);
+    }
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) *(u32x4 *)((char *)group + p * 64 + c * 2) = __builtin_bit_cast(u32x4, part[p]);
+}
+
 // A number that a kernel before has written, the same for all.
 __device__ __forceinline__ int scalar(const int *p) { return *(const int __attribute__((address_space(4))) *)(uintptr_t)p; }
 
@@ -173,6 +204,7 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
     const Place at = place(blockIdx.x, mt, nt);
     const int m0 = at.m * S::BM, n0 = at.n * S::BN, wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
     const int k0 = blockIdx.y * piece, k1 = min(steps, k0 + piece);
+    const int64_t holder = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (S::WM * S::WN) + wave;
 
     f32x16 acc[S::FM][S::FN];
 #pragma unroll
@@ -206,7 +238,7 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
             aim(lds + ahead * SLOT, k);
             span<0, LOADS>(load);
         }
-        e.begin(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31));
+        e.begin(acc, holder);
         meet<0>();
         span<0, READS>([&](auto r) { read(lds, std::integral_constant<int, 0>(), r); });
         __builtin_amdgcn_sched_barrier(0);
@@ -243,7 +275,133 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
         }
     }
     if constexpr (E::ROWS) __syncthreads();                 // LDS is read: the epilogue takes it
-    e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), wave / S::WN + S::WM * at.m, lds + wave * (32 * S::FM * 32 * 4));
+    e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), holder, wave / S::WN + S::WM * at.m, lds + wave * (S::FM * 4096));
+}
+
+// The same product of numbers in three parts: tiles of 256 x 128, 32 of k a step, each part a tile of its own in LDS (144 KiB of two slots).
+template <int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct BringThree {
+    static constexpr int K = GROUP, PART = SIDE * K / 8, N = PLANES * PART / BLOCK;       // 16-byte chunks of a part; a lane's
+    static_assert(PLANES * PART % BLOCK == 0, "a chunk for every lane");
+    typedef Tile<bf16, SIDE> Across;
+    const Three *p;
+    int64_t ld;
+    int count, at[N];
+    u32x4 rs;
+    uint32_t to;
+    // rows of 64 bytes, four of which fill the banks: 16 lanes that read the same chunk of 16 rows read all of them
+    __device__ __forceinline__ static int along(int row, int chunk) { return row * 64 + (chunk ^ (row >> 2 & 3)) * 16; }
+    __device__ __forceinline__ BringThree(const Operand<Three> &o, int first) : p(ALONG ? o.p + first * o.ld : o.p + first), ld(o.ld), count(min(SIDE, o.count - first))
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int n = threadIdx.x + u * BLOCK, part = n / PART, m = n % PART;
+            if (ALONG) {
+                const int r = m / 4, row = SPREAD ? (r & ~31) + spread_of(r & 31) : r;
+                at[u] = row < count ? row * (int)ld * (int)sizeof(Three) + part * 64 + (m % 4 ^ (r >> 2 & 3)) * 16 : INT32_MIN;
+            } else {
+                const int r = m / (SIDE / 8), c = (m % (SIDE / 8) ^ Across::swizzle(r)) * 8;
+                at[u] = c < count ? (r * (int)ld + c / GROUP * GROUP) * (int)sizeof(Three) + part * 64 + c % GROUP * 2 : INT32_MIN;
+            }
+        }
+    }
+    __device__ __forceinline__ void aim(char *tile, int k, int left)
+    {
+        const uint64_t base = (uint64_t)(ALONG ? p + k : p + k * ld);
+        const int bytes = (ALONG ? (count - 1) * (int)ld + K : (min(left, K) - 1) * (int)ld + count) * (int)sizeof(Three);
+        rs = u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)bytes, 0x00020000u};
+        to = (uint32_t)(uintptr_t)(KT_LDS char *)tile + wave_id() * 1024;
+    }
+    __device__ __forceinline__ void load(int u) const
+    {
+        // as Feed::bring
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :: "s"(to + u * BLOCK * 16), "v"(at[u]), "s"(rs) : "memory");
+    }
+    // 32 m or n from `first` on, 16 of k from 16 c on
+    static __device__ __forceinline__ bf16x8 read(const char *tile, int part, int first, int c)
+    {
+        const char *const t = tile + part * SIDE * 64;
+        if constexpr (ALONG) return *(const bf16x8 *)(t + along(first + (threadIdx.x & 31), 2 * c + (threadIdx.x >> 5 & 1)));
+        else return fragment<bf16, SIDE, false, SPREAD>(t, first, c);
+    }
+};
+
+struct Split {
+    static constexpr int WM = 4, WN = 2, FM = 2, FN = 2, BM = WM * FM * 32, BN = WN * FN * 32, BLOCK = WM * WN * 64, SLOT = (BM + BN) * 64 * PLANES;
+};
+template <bool AA, bool BA, typename E>
+__global__ __launch_bounds__(Split::BLOCK) void kt_xent_three_kernel(Operand<Three> a, Operand<Three> b, int steps, int piece, const int *live, int mt, int nt, E e)
+{
+    typedef Split S;
+    typedef BringThree<S::BM, S::BLOCK, AA, true> BringA;
+    typedef BringThree<S::BN, S::BLOCK, BA, false> BringB;
+    constexpr int K = GROUP, ABYTES = S::BM * 64 * PLANES, LA = BringA::N, LB = BringB::N;
+    extern __shared__ __align__(16) char lds[];             // two slots
+
+    const int wave = wave_id(), lane = threadIdx.x & 63;
+    if (live) {
+        const int n = scalar(live);
+        if constexpr (BA) {
+            nt = (n + S::BN - 1) / S::BN;
+            if ((int)blockIdx.x >= mt * nt) return;
+        } else {
+            steps = n;
+            piece = ((n + (int)gridDim.y - 1) / (int)gridDim.y + 63) / 64 * 64;
+        }
+    }
+    const Place at = place(blockIdx.x, mt, nt);
+    const int m0 = at.m * S::BM, n0 = at.n * S::BN, wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
+    const int k0 = blockIdx.y * piece, k1 = min(steps, k0 + piece);
+
+    f32x16 acc[S::FM][S::FN];
+#pragma unroll
+    for (int m = 0; m < S::FM; ++m)
+#pragma unroll
+        for (int n = 0; n < S::FN; ++n) acc[m][n] = f32x16{0};
+    BringA from_a(a, m0);
+    BringB from_b(b, n0);
+    auto bring = [&](char *to, int k) __attribute__((always_inline)) {
+        from_a.aim(to, k, k1 - k);
+        from_b.aim(to + ABYTES, k, k1 - k);
+        span<0, LA>([&](auto u) { from_a.load(u); });
+        span<0, LB>([&](auto u) { from_b.load(u); });
+    };
+    // the products of two numbers' parts, least first
+    constexpr int PER = S::FM * S::FN, PAIRS = 6, ALL = PER * PAIRS, READS = (S::FM + S::FN) * PLANES;
+    constexpr int PA[PAIRS] = {2, 1, 0, 1, 0, 0}, PB[PAIRS] = {0, 1, 2, 0, 1, 0};
+    bf16x8 fa[2][PLANES][S::FM], fb[2][PLANES][S::FN];
+    // fragment number r of a chunk, in the order in which the products need them: parts 2 of A and 0 of B first
+    auto read = [&](const char *slot, auto c0, auto r0) __attribute__((always_inline)) {
+        constexpr int c = c0, r = r0, group = r / 2, i = r % 2, part = group / 2;
+        static_assert(S::FM == 2 && S::FN == 2, "two fragments of each part");
+        if constexpr (group % 2 == 0) fa[c][PLANES - 1 - part][i] = BringA::read(slot, PLANES - 1 - part, wm + 32 * i, c);
+        else fb[c][part][i] = BringB::read(slot + ABYTES, part, wn + 32 * i, c);
+    };
+    int k = k0, ahead = 0;
+    for (; ahead < 2 && k < k1; ++ahead, k += K) bring(lds + ahead * S::SLOT, k);
+    const int64_t holder = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (S::WM * S::WN) + wave;
+    e.begin(acc, holder);
+    meet<0>();
+    span<0, READS>([&](auto r) { read(lds, std::integral_constant<int, 0>(), r); });
+    __builtin_amdgcn_sched_barrier(0);
+    for (int slot = 0; ahead > 0; slot ^= 1) {
+        char *const now = lds + slot * S::SLOT, *const then = lds + (slot ^ 1) * S::SLOT;
+        const bool more = k < k1;
+        span<0, 2 * ALL>([&](auto n1) {
+            constexpr int c = n1 / ALL, n = n1 % ALL, pair = n / PER, i = n % PER / S::FN, j = n % S::FN;
+            if constexpr (c == 1 && n == 0) {
+                meet<0>();
+                if (more) bring(now, k);
+            }
+            mma(acc[i][j], fa[c][PA[pair]][i], fb[c][PB[pair]][j]);
+            if constexpr (n < READS) read(c == 0 ? now : then, std::integral_constant<int, 1 - c>(), std::integral_constant<int, n>());
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (more) k += K;
+        else --ahead;
+    }
+    if constexpr (E::ROWS) __syncthreads();                 // LDS is read: the epilogue takes it
+    e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), holder, wave / S::WN + S::WM * at.m, lds + wave * (S::FM * 4096));
 }
 
 // ---- what becomes of a tile ----------------------------------------------------------
@@ -301,8 +459,8 @@ template <typename I> struct Stats {
         for (int i = threadIdx.x & 63; i < count; i += 64) any |= target_of(targets, n0 + i, tokens, vocab) >= 0;
         return __ballot(any) == 0;
     }
-    template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int part, char *) const
+    template <typename A> __device__ __forceinline__ void begin(A &, int64_t) const {}
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int64_t, int part, char *) const
     {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
@@ -367,8 +525,8 @@ template <typename T, typename I> struct Slope {
     const int *map, *live;          // the token of each row, and their number
     int tokens, vocab, first, end_;
     __device__ __forceinline__ bool skip(int, int) const { return false; }
-    template <typename A> __device__ __forceinline__ void begin(A &, int, int) const {}
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int, char *scratch) const
+    template <typename A> __device__ __forceinline__ void begin(A &, int64_t) const {}
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int64_t, int, char *scratch) const
     {
         const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
 #pragma unroll
@@ -377,14 +535,27 @@ template <typename T, typename I> struct Slope {
             if (first_row >= rows) continue;
             const int at = map[min(row, rows - 1)], target = (int)targets[at] - first, room = end_ - first;
             const float up = dloss[at], base = lse[at];
-            store_rows<FM>(scratch, dz + m0, ld, first_row, rows - first_row, (int)ld - m0, nullptr, [&](int i, float *f) {
+            auto values = [&](int i, float *f) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int v = m + 32 * i + r;
                     const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E) - (v == target ? 1.0f : 0.0f);
                     f[r] = v < room ? p * up : 0.0f;
                 }
-            });
+            };
+            if constexpr (std::is_same_v<T, Three>) {
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    float f[16];
+                    values(i, f);
+                    if (row >= rows || m0 + 32 * i >= ld) continue;
+                    Three *group = dz + row * ld + m0 + 32 * i;
+                    put_three(group, 16 * h, f);
+                    put_three(group, 16 * h + 8, f + 8);
+                }
+            } else {
+                store_rows<FM>(scratch, dz + m0, ld, first_row, rows - first_row, (int)ld - m0, nullptr, values);
+            }
         }
     }
     __device__ __forceinline__ void few(f32x4 z, int v, int t, int) const
@@ -404,14 +575,10 @@ template <typename T, typename I> struct Slope {
     }
 };
 
-// Sums that the next piece of the vocabulary goes on with, as the lanes hold them: nobody else reads them.
-template <int FM, int FN> __device__ __forceinline__ int64_t carried()
+// Sums that the next piece of the vocabulary goes on with, as the lanes hold them: nobody else reads them.  `holder`: the wavefront's number.
+template <int FM, int FN> __device__ __forceinline__ void resume(const float *sums, int64_t holder, f32x16 (&acc)[FM][FN])
 {
-    return (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / 64) + wave_id()) * (FM * FN * 1024) + (threadIdx.x & 63) * 4;
-}
-template <int FM, int FN> __device__ __forceinline__ void resume(const float *sums, f32x16 (&acc)[FM][FN])
-{
-    const float *p = sums + carried<FM, FN>();
+    const float *p = sums + holder * (FM * FN * 1024) + (threadIdx.x & 63) * 4;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -428,13 +595,13 @@ struct Carry {
     float *sums;
     bool first;
     __device__ __forceinline__ bool skip(int, int) const { return false; }
-    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int, int) const
+    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int64_t holder) const
     {
-        if (!first) resume(sums, acc);
+        if (!first) resume(sums, holder, acc);
     }
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int, int, int, char *) const
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int, int, int64_t holder, int, char *) const
     {
-        float *p = sums + carried<FM, FN>();
+        float *p = sums + holder * (FM * FN * 1024) + (threadIdx.x & 63) * 4;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -458,11 +625,11 @@ template <typename G> struct Result {
     const int *map, *live;          // where a row goes, and how many there are, or null
     int rows, cols;
     __device__ __forceinline__ bool skip(int, int) const { return false; }
-    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int, int) const
+    template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int64_t holder) const
     {
-        if (sums) resume(sums, acc);
+        if (sums) resume(sums, holder, acc);
     }
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int, char *scratch) const
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int64_t, int, char *scratch) const
     {
         const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
 #pragma unroll
@@ -551,15 +718,29 @@ __global__ __launch_bounds__(64) void kt_xent_few_kernel(const T *w, int64_t ldw
 
 // ---- the small kernels beside them ---------------------------------------------------
 
-// Rows at multiples of 16 bytes for tensors that have none: zeros up to `ld`.
-template <typename T>
-__global__ __launch_bounds__(256) void kt_xent_align_kernel(const T *x, int64_t ldx, int cols, T *y, int64_t ld, int64_t rows)
+// EACH neighbouring elements of a row from column c on as an operand has them; zeros from `cols` on.
+template <typename X> constexpr int EACH = std::is_same_v<X, Three> ? 8 : 16 / (int)sizeof(X);
+template <typename X, typename T> __device__ __forceinline__ void copy_chunk(const T *row, int c, int cols, X *to)
 {
-    const int parts = (int)((ld + 64 * VE<T> - 1) / (64 * VE<T>));
+    if constexpr (std::is_same_v<X, Three>) {
+        float f[8];
+        widen<float>(ld_chunk(row, c, cols), f);
+        widen<float>(ld_chunk(row, c + 4, cols), f + 4);
+        put_three(to + c / GROUP * GROUP, c % GROUP, f);
+    } else {
+        *(u32x4 *)(to + c) = ld_chunk(row, c, cols);
+    }
+}
+
+// Rows at multiples of 16 bytes for tensors that have none, or in three parts: zeros up to `ld`.
+template <typename X, typename T>
+__global__ __launch_bounds__(256) void kt_xent_align_kernel(const T *x, int64_t ldx, int cols, X *y, int64_t ld, int64_t rows)
+{
+    const int parts = (int)((ld + 64 * EACH<X> - 1) / (64 * EACH<X>));
     for (int64_t n = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; n < rows * parts; n += (int64_t)gridDim.x * 4) {
         const int64_t row = n / parts;
-        const int c = (int)(n % parts) * 64 * VE<T> + (threadIdx.x & 63) * VE<T>;
-        if (c < ld) *(u32x4 *)(y + row * ld + c) = ld_chunk(x + row * ldx, c, cols);
+        const int c = (int)(n % parts) * 64 * EACH<X> + (threadIdx.x & 63) * EACH<X>;
+        if (c < ld) copy_chunk(x + row * ldx, c, cols, y + row * ld);
     }
 }
 
@@ -627,16 +808,20 @@ __global__ __launch_bounds__(1024) void kt_xent_list_kernel(const I *targets, co
 }
 
 // Their rows of x one after another, zeros up to `ld`; where dx is given, zeros into its rows of the other tokens.
-template <typename T, typename I>
-__global__ __launch_bounds__(256) void kt_xent_gather_kernel(const T *x, int64_t ldx, int cols, T *y, int64_t ld, const int *map, const int *live,
+template <typename X, typename T, typename I>
+__global__ __launch_bounds__(256) void kt_xent_gather_kernel(const T *x, int64_t ldx, int cols, X *y, int64_t ld, const int *map, const int *live,
                                                              const I *targets, const float *dloss, int tokens, int vocab, T *dx, int64_t lddx)
 {
-    const int parts = (int)((ld + 64 * VE<T> - 1) / (64 * VE<T>)), count = *live;
+    const int parts = (int)((ld + 64 * EACH<X> - 1) / (64 * EACH<X>)), count = *live;
     for (int64_t n = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; n < (int64_t)tokens * parts; n += (int64_t)gridDim.x * 4) {
-        const int t = (int)(n / parts), c = (int)(n % parts) * 64 * VE<T> + (threadIdx.x & 63) * VE<T>;
+        const int t = (int)(n / parts), c = (int)(n % parts) * 64 * EACH<X> + (threadIdx.x & 63) * EACH<X>;
         if (c >= ld) continue;
-        if (t < count) *(u32x4 *)(y + t * ld + c) = ld_chunk(x + map[t] * ldx, c, cols);
-        if (dx && c < cols && !(target_of(targets, t, tokens, vocab) >= 0 && dloss[t] != 0.0f)) st_chunk(dx + t * lddx, c, cols, u32x4{0, 0, 0, 0});
+        if (t < count) copy_chunk(x + map[t] * ldx, c, cols, y + t * ld);
+        if (dx && !(target_of(targets, t, tokens, vocab) >= 0 && dloss[t] != 0.0f)) {
+#pragma unroll
+            for (int k = 0; k < EACH<X>; k += VE<T>)
+                if (c + k < cols) st_chunk(dx + t * lddx, c + k, cols, u32x4{0, 0, 0, 0});
+        }
     }
 }
 
@@ -667,24 +852,28 @@ int64_t over(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
 // How a product of m x n over k is cut: the tile's side, and pieces of k (at most `most`), whose sums a second kernel adds.
 struct Cut {
-    int side, pieces, piece;
+    int side, pieces, piece;        // side 0: tiles of numbers in three parts
+    int64_t m() const { return side ? side : Split::BM; }
+    int64_t n() const { return side ? side : Split::BN; }
+    int64_t part() const { return side ? side / 2 : Split::FM * 32; }       // rows of m that a wavefront has
 };
 // The least time of a model in us: a CU makes one workgroup's tile after the other, elements times steps of k at a rate that depends on the side (and a
 // start and an end worth 128 steps); pieces cost a launch and their sums' way through memory.  Rates are what full chips reached (16384 x 8192 x 2048 in its three orders: tiles of 256 511
 // to 555 us, of 128 600 to 650, of 64 850 to 1060; f32 4096 x 32768 x 768: 128 1578 to 1684, 64 1639 to 1829).  Both sides of a choice, us: f32
 // 768 x 4096 over 32768 in 2 pieces (384 workgroups) 2024, in 4 (768) 1578; bf16 2048 x 1152 over 16384 in tiles of 64 206, of 128 in 3 pieces 122.
-Cut cut_of(kt_dtype dt, int64_t m, int64_t n, int64_t k, int64_t most)
+Cut cut_of(kt_dtype dt, bool three, int64_t m, int64_t n, int64_t k, int64_t most)
 {
-    Cut best{64, 1, (int)up(k < 1 ? 1 : k, 64)};
+    Cut best{three ? 0 : 64, 1, (int)up(k < 1 ? 1 : k, 64)};
     double least = 1e300;
-    for (int side : {256, 128, 64}) {
-        if (side == 256 && dt == KT_F32) continue;
-        const double rate = dt == KT_F32 ? (side == 128 ? 2.5e5 : 2.3e5) : side == 256 ? 2.0e6 : side == 128 ? 1.75e6 : 1.15e6;
-        const int64_t tiles = over(m, side) * over(n, side);
+    for (int side : {0, 256, 128, 64}) {
+        if (three != (side == 0) || (side == 256 && dt == KT_F32)) continue;
+        const double rate = three ? 4.0e5 : dt == KT_F32 ? (side == 128 ? 2.5e5 : 2.3e5) : side == 256 ? 2.0e6 : side == 128 ? 1.75e6 : 1.15e6;
+        const Cut c{side, 1, 0};
+        const int64_t tiles = over(m, c.m()) * over(n, c.n());
         for (int64_t p = 1; p <= most && (p == 1 || p * 128 <= k); ++p) {
             const int64_t piece = up(over(k < 1 ? 1 : k, p), 64), count = over(k < 1 ? 1 : k, piece);
             if (count != p) continue;
-            const double t = (double)over(tiles * p, 256) * side * side * (double)(piece + 128) / rate + (p > 1 ? 4 + (double)m * n * 8 * p / 5.5e6 : 0);
+            const double t = (double)over(tiles * p, 256) * c.m() * c.n() * (double)(piece + 128) / rate + (p > 1 ? 4 + (double)m * n * 8 * p / 5.5e6 : 0);
             if (t < least) {
                 least = t;
                 best = Cut{side, (int)p, (int)piece};
@@ -701,8 +890,6 @@ template <typename T> bool plain(const T *p, int64_t ld, int64_t width)
     return rows_of_16(p, ld) && width % VE<T> == 0 && ld * (int64_t)sizeof(T) <= 1 << 22;
 }
 
-// What a call needs of the workspace, and its cut.  Other matrices are copied to rows of a multiple of 16 bytes first (the weight up to 128 MiB of it
-// at a time), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
 // Whether kt_xent_few_kernel makes the logits: up to 16 tokens, and up to 32 where tiles would need a copy of the weight or have little to do.  us, forward
 // pass: 30 tokens of 50304 x 2048 bf16 85, in tiles 55; of 50304 x 1001 f32 93 and 150; of 5003 x 768 bf16 9.9 and 11.9; 12 of 50304 x 2048 56 and 53.
 bool few_tokens(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
@@ -710,11 +897,22 @@ bool few_tokens(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
     return tokens <= 16 || (tokens <= 32 && (width * (dt == KT_F32 ? 4 : 2) % 16 || vocab * width < 1 << 25));
 }
 
+// Whether f32 products are made of numbers in three parts: where the copies into parts cost little beside them and tiles of 256 x 128 keep the chip busy.
+// us, f32 instructions and parts: forward 8192 tokens of 50304 x 768 4810 and 3020, 1024 of 5003 x 1001 118 and 90, but 512 of 5003 x 1024 65 and 87;
+// backward 4096 of 50304 x 768 7520 and 5160, 512 of 5003 x 1024 204 and 171, but 100 of 50304 x 768 343 and 375, 1024 of 1000 x 768 92 and 116.
+bool in_three(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd)
+{
+    return dt == KT_F32 && width >= 128 && tokens >= (bwd ? 256 : 512) && over(vocab, Split::BM) * over(tokens, Split::BN) >= (bwd ? 64 : 144);
+}
+
+// What a call needs of the workspace, and its cut.  Matrices that loads of 16 bytes cannot take as they are are copied to rows of a multiple of 16 bytes first
+// (the weight up to 128 MiB of it at a time), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
 struct Plan {
-    int64_t es, wide;               // bytes of an element; elements to a row of a copy
+    bool three;                     // operands in three parts
+    int64_t es, wide;               // bytes of an operand's element; elements to a row of a copy
     int64_t copy;                   // rows of the weight copied at a time
     int64_t most, piece;            // rows of the vocabulary in a piece: with the weight as it is; with copies
-    int side;                       // of the forward pass's tiles
+    Cut z;                          // of the forward pass
     int64_t ldp;                    // backward: elements to a row of sums
     Cut kx;                         // of dx over a piece of the vocabulary
     bool list;                      // whether the tokens that take part are listed
@@ -731,14 +929,15 @@ int64_t rows_in(int64_t most, int64_t of, int64_t vocab)
 Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd)
 {
     Plan p{};
-    p.es = dt == KT_F32 ? 4 : 2;
+    p.three = in_three(dt, tokens, vocab, width, bwd);
+    p.es = p.three ? sizeof(Three) : dt == KT_F32 ? 4 : 2;
     p.wide = up(width, 64);
     p.copy = rows_in(128 << 20, p.wide * p.es, vocab);
     // backward: dz of up to 2^27 elements, 256 MiB of bf16, what the last-level cache holds; forward: a launch of up to 2^20 tiles of 256
-    p.most = rows_in(bwd ? 1ll << 27 : 1ll << 36, tokens, vocab);
+    p.most = rows_in(bwd ? 1ll << (p.three ? 26 : 27) : 1ll << 36, tokens, vocab);
     if (bwd) p.most = at_most(p.most, 1 << 18);
     p.piece = at_most(p.most, p.copy);
-    p.side = cut_of(dt, vocab, tokens, width, 1).side;
+    p.z = cut_of(dt, p.three, vocab, tokens, width, 1);
     p.ldp = up(width, 16);
     auto take = [&](int64_t bytes) {
         const int64_t from = p.bytes;
@@ -749,23 +948,22 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
     p.x = take(!bwd && few ? 0 : tokens * p.wide * p.es);
     p.w = take(!bwd && few ? 0 : p.piece * p.wide * p.es);
     // a list and a copy of x cost some 6 us and its bytes twice: worth while for the forward pass from some 100 us on
-    p.list = bwd || (double)tokens * vocab * width * (dt == KT_F32 ? 8 : 1) > 5e10;
+    p.list = bwd || p.three || (double)tokens * vocab * width * (dt == KT_F32 ? 8 : 1) > 5e10;
     p.map = take(p.list ? tokens * 4 : 0);
     p.live = take(p.list ? 4 : 0);
     if (!bwd) {
-        p.parts = take((few ? over(vocab, 16) : over(vocab, p.side) * 2) * tokens * 8);
+        p.parts = take((few ? over(vocab, 16) : over(vocab, p.z.m()) * (p.z.m() / p.z.part())) * tokens * 8);
         p.hit = take(tokens * 4);
         return p;
     }
     p.dz = take(tokens * p.most * p.es);
-    p.kx = cut_of(dt, width, tokens, at_most(p.most, vocab), MOST_PIECES);
-    const int64_t side = p.kx.side;
-    if (p.piece < vocab) p.acc = take(p.kx.pieces * over(width, side) * over(tokens, side) * side * side * 4);
+    p.kx = cut_of(dt, p.three, width, tokens, at_most(p.most, vocab), MOST_PIECES);
+    if (p.piece < vocab) p.acc = take(p.kx.pieces * over(width, p.kx.m()) * over(tokens, p.kx.n()) * p.kx.m() * p.kx.n() * 4);
     // dx cut over the vocabulary, and the weight's gradient cut over the tokens: whichever takes more
     int64_t most = p.kx.pieces > 1 ? p.kx.pieces * tokens : 0;
     for (int64_t rows : {at_most(p.most, vocab), at_most(p.piece, vocab), vocab % p.most, vocab % p.piece}) {
         if (rows == 0) continue;
-        const Cut k = cut_of(dt, width, rows, tokens, MOST_PIECES);
+        const Cut k = cut_of(dt, p.three, width, rows, tokens, MOST_PIECES);
         if (k.pieces > 1 && k.pieces * rows > most) most = k.pieces * rows;
     }
     p.sums = take(most * p.ldp * 4);
@@ -789,11 +987,21 @@ int launch_tiles(const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n,
 template <typename T, bool AA, bool BA, typename E>
 int product(const Cut &k, const Operand<T> &a, int64_t m, const Operand<T> &b, int64_t n, int64_t steps, const int *live, const E &e, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2) {
-        if (k.side == 256) return launch_tiles<T, Big, AA, BA>(a, m, b, n, steps, k, live, e, s);
+    if constexpr (std::is_same_v<T, Three>) {
+        constexpr int LDS = 2 * Split::SLOT;
+        const auto kernel = kt_xent_three_kernel<AA, BA, E>;
+        const hipError_t e1 = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        if (e1 != hipSuccess) return (int)e1;
+        const int64_t mt = over(m, Split::BM), nt = over(n, Split::BN);
+        kernel<<<dim3((unsigned)(mt * nt), (unsigned)k.pieces), Split::BLOCK, LDS, s>>>(a, b, (int)steps, k.piece, live, (int)mt, (int)nt, e);
+        return (int)hipGetLastError();
+    } else {
+        if constexpr (sizeof(T) == 2) {
+            if (k.side == 256) return launch_tiles<T, Big, AA, BA>(a, m, b, n, steps, k, live, e, s);
+        }
+        if (k.side == 128) return launch_tiles<T, Mid, AA, BA>(a, m, b, n, steps, k, live, e, s);
+        return launch_tiles<T, Small, AA, BA>(a, m, b, n, steps, k, live, e, s);
     }
-    if (k.side == 128) return launch_tiles<T, Mid, AA, BA>(a, m, b, n, steps, k, live, e, s);
-    return launch_tiles<T, Small, AA, BA>(a, m, b, n, steps, k, live, e, s);
 }
 
 #define KT_GO(call)                    \
@@ -811,60 +1019,64 @@ template <typename T, typename E> int few(const T *w, int64_t ldw, int64_t rows,
 }
 
 // x or rows of w as the products take them: as they are, or copied.
-template <typename T> int aligned_rows(bool as_is, const T *x, int64_t ldx, int64_t width, int64_t rows, T *copy, int64_t wide, Operand<T> *to, hipStream_t s)
+template <typename X, typename T>
+int aligned_rows(bool as_is, const T *x, int64_t ldx, int64_t width, int64_t rows, X *copy, int64_t wide, Operand<X> *to, hipStream_t s)
 {
     to->count = (int)rows;
-    if (as_is) {
-        to->p = x;
-        to->ld = ldx;
-        return 0;
+    if constexpr (std::is_same_v<X, T>) {
+        if (as_is) {
+            to->p = x;
+            to->ld = ldx;
+            return 0;
+        }
     }
     to->p = copy;
     to->ld = wide;
     if (rows == 0) return 0;
-    const int64_t blocks = over(rows * over(wide, 64 * VE<T>), 4);
-    kt_xent_align_kernel<T><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, rows);
+    const int64_t blocks = over(rows * over(wide, 64 * EACH<X>), 4);
+    kt_xent_align_kernel<X, T><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, rows);
     return (int)hipGetLastError();
 }
 
 // The list of the tokens that take part and their rows of x; zeros in dx's rows of the others.
-template <typename T, typename I>
-int list(const T *x, int64_t ldx, int64_t width, const I *targets, const float *dloss, int64_t tokens, int64_t vocab, T *copy, int64_t wide, int *map,
+template <typename X, typename T, typename I>
+int list(const T *x, int64_t ldx, int64_t width, const I *targets, const float *dloss, int64_t tokens, int64_t vocab, X *copy, int64_t wide, int *map,
          int *live, T *dx, int64_t lddx, hipStream_t s)
 {
     kt_xent_list_kernel<I><<<(unsigned)over(tokens, 1024), 1024, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, map, live);
     KT_GO((int)hipGetLastError());
-    const int64_t blocks = over(tokens * over(wide, 64 * VE<T>), 4);
-    kt_xent_gather_kernel<T, I><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, map, live, targets, dloss, (int)tokens, (int)vocab, dx, lddx);
+    const int64_t blocks = over(tokens * over(wide, 64 * EACH<X>), 4);
+    kt_xent_gather_kernel<X, T, I><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, map, live, targets, dloss, (int)tokens, (int)vocab, dx, lddx);
     return (int)hipGetLastError();
 }
 
-template <typename T, typename I>
-int fwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, int64_t ldx, const T *w, int64_t ldw, const I *targets, float *loss,
+// X: the operands' type.
+template <typename X, typename T, typename I>
+int fwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const T *x, int64_t ldx, const T *w, int64_t ldw, const I *targets, float *loss,
         float *lse, char *ws, hipStream_t s)
 {
-    const Plan p = plan_of(dt, tokens, vocab, width, false);
     f32x2 *parts = (f32x2 *)(ws + p.parts);
     int *const map = p.list ? (int *)(ws + p.map) : nullptr, *const live = p.list ? (int *)(ws + p.live) : nullptr;
     float *hit = (float *)(ws + p.hit);
-    const bool w_as_is = plain(w, ldw, width);
-    Operand<T> a, b;
-    int count = (int)over(vocab, p.side) * 2;
-    if (few_tokens(dt, tokens, vocab, width)) {
+    const bool w_as_is = std::is_same_v<X, T> && plain(w, ldw, width), by_few = few_tokens(dt, tokens, vocab, width);
+    X *const copy = (X *)(ws + p.x);
+    Operand<X> a, b;
+    int count = (int)(over(vocab, p.z.m()) * (p.z.m() / p.z.part()));
+    if (by_few) {
         const Stats<I> e{parts, hit, targets, nullptr, nullptr, (int)tokens, (int)vocab, 0, (int)vocab, 0};
         KT_GO(few(w, ldw, vocab, x, ldx, tokens, width, e, s));
         count = (int)over(vocab, 16);
     } else if (p.list) {
-        KT_GO((list<T, I>(x, ldx, width, targets, nullptr, tokens, vocab, (T *)(ws + p.x), p.wide, map, live, nullptr, 0, s)));
-        b = Operand<T>{(T *)(ws + p.x), p.wide, (int)tokens};
+        KT_GO((list<X, T, I>(x, ldx, width, targets, nullptr, tokens, vocab, copy, p.wide, map, live, nullptr, 0, s)));
+        b = Operand<X>{copy, p.wide, (int)tokens};
     } else {
-        KT_GO(aligned_rows(plain(x, ldx, width), x, ldx, width, tokens, (T *)(ws + p.x), p.wide, &b, s));
+        KT_GO((aligned_rows<X, T>(plain(x, ldx, width), x, ldx, width, tokens, copy, p.wide, &b, s)));
     }
-    for (int64_t v = few_tokens(dt, tokens, vocab, width) ? vocab : 0, rows; v < vocab; v += rows) {
+    for (int64_t v = by_few ? vocab : 0, rows; v < vocab; v += rows) {
         rows = at_most(w_as_is ? p.most : p.piece, vocab - v);
-        KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
-        const Stats<I> e{parts, hit, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / (p.side / 2))};
-        KT_GO((product<T, true, true>(Cut{p.side, 1, (int)up(width, 64)}, a, rows, b, tokens, width, live, e, s)));
+        KT_GO((aligned_rows<X, T>(w_as_is, w + v * ldw, ldw, width, rows, (X *)(ws + p.w), p.wide, &a, s)));
+        const Stats<I> e{parts, hit, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)(v / p.z.part())};
+        KT_GO((product<X, true, true>(p.z, a, rows, b, tokens, width, live, e, s)));
     }
     if (tokens >= 512) kt_xent_join_kernel<I, 32><<<(unsigned)over(tokens, 32), 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
     else kt_xent_join_kernel<I, 1><<<(unsigned)tokens, 256, 0, s>>>(parts, count, hit, targets, (int)tokens, (int)vocab, loss, lse);
@@ -879,55 +1091,59 @@ template <typename G> int sum(const float *parts, const Cut &k, int64_t apart, i
     return (int)hipGetLastError();
 }
 
-template <typename T, typename I>
-int bwd(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *dloss, const T *x, int64_t ldx, const T *w, int64_t ldw,
+template <typename X, typename T, typename I>
+int bwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, const float *dloss, const T *x, int64_t ldx, const T *w, int64_t ldw,
         const I *targets, const float *lse, T *dx, int64_t lddx, T *dw, int64_t lddw, char *ws, hipStream_t s)
 {
-    const Plan p = plan_of(dt, tokens, vocab, width, true);
     int *const map = (int *)(ws + p.map), *const live = (int *)(ws + p.live);
-    T *dz = (T *)(ws + p.dz);
+    X *dz = (X *)(ws + p.dz);
     float *acc = (float *)(ws + p.acc), *sums = (float *)(ws + p.sums);
-    const bool w_as_is = plain(w, ldw, width);
-    const int64_t cols = up(width, VE<T>);              // of an operand: what a copy has past the width is zeros
+    const bool w_as_is = std::is_same_v<X, T> && plain(w, ldw, width);
+    constexpr int UNIT = std::is_same_v<X, Three> ? GROUP : VE<T>;
+    const int64_t cols = up(width, UNIT);               // of an operand: what a copy has past the width is zeros
     const int64_t piece = w_as_is ? p.most : p.piece;
-    T *const copy = (T *)(ws + p.x);
-    Operand<T> a;
-    const Operand<T> b{copy, p.wide, (int)tokens};
-    if (tokens) KT_GO((list<T, I>(x, ldx, width, targets, dloss, tokens, vocab, copy, p.wide, map, live, dx, lddx, s)));
+    X *const copy = (X *)(ws + p.x);
+    Operand<X> a;
+    const Operand<X> b{copy, p.wide, (int)tokens};
+    if (tokens) KT_GO((list<X, T, I>(x, ldx, width, targets, dloss, tokens, vocab, copy, p.wide, map, live, dx, lddx, s)));
     for (int64_t v = 0, rows; v < vocab; v += rows) {
         rows = at_most(piece, vocab - v);
         if (tokens) {
-            KT_GO(aligned_rows(w_as_is, w + v * ldw, ldw, width, rows, (T *)(ws + p.w), p.wide, &a, s));
-            const Slope<T, I> e{dz, p.most, lse, dloss, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
-            if (few_tokens(dt, tokens, vocab, width)) KT_GO(few(a.p, a.ld, rows, (const T *)copy, p.wide, tokens, width, e, s));
-            else KT_GO((product<T, true, true>(cut_of(dt, rows, tokens, width, 1), a, rows, b, tokens, width, live, e, s)));
+            KT_GO((aligned_rows<X, T>(w_as_is, w + v * ldw, ldw, width, rows, (X *)(ws + p.w), p.wide, &a, s)));
+            const Slope<X, I> e{dz, p.most, lse, dloss, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
+            bool made = false;
+            if constexpr (std::is_same_v<X, T>) {
+                made = few_tokens(dt, tokens, vocab, width);
+                if (made) KT_GO(few(a.p, a.ld, rows, (const T *)copy, p.wide, tokens, width, e, s));
+            }
+            if (!made) KT_GO((product<X, true, true>(cut_of(dt, p.three, rows, tokens, width, 1), a, rows, b, tokens, width, live, e, s)));
         }
         if (dx && tokens) {
-            const Operand<T> wide{a.p, a.ld, (int)cols}, slope{dz, p.most, (int)tokens};
+            const Operand<X> wide{a.p, a.ld, (int)cols}, slope{dz, p.most, (int)tokens};
             const bool first = v == 0, last = v + rows == vocab;
             const Cut k{p.kx.side, p.kx.pieces, (int)up(over(rows, p.kx.pieces), 64)};
             if (!last) {
                 const Carry e{acc, first};
-                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
+                KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else if (k.pieces == 1) {
                 const Result<T> e{dx, lddx, 0, first ? nullptr : acc, map, live, (int)tokens, (int)width};
-                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
+                KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else {
                 const int64_t apart = tokens * p.ldp;
                 const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, nullptr, live, (int)tokens, (int)p.ldp};
-                KT_GO((product<T, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
+                KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
                 KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, map, live, s));
             }
         }
         if (dw) {
-            const Operand<T> wide{b.p, b.ld, (int)cols}, slope{dz, p.most, (int)up(rows, VE<T>)};
-            const Cut k = cut_of(dt, width, rows, tokens, MOST_PIECES);
+            const Operand<X> wide{b.p, b.ld, (int)cols}, slope{dz, p.most, (int)up(rows, UNIT)};
+            const Cut k = cut_of(dt, p.three, width, rows, tokens, MOST_PIECES);
             if (k.pieces == 1) {
                 const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, nullptr, (int)rows, (int)width};
-                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
+                KT_GO((product<X, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
             } else {
                 const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, nullptr, (int)rows, (int)p.ldp};
-                KT_GO((product<T, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
+                KT_GO((product<X, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
                 KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, nullptr, nullptr, s));
             }
         }
@@ -950,7 +1166,12 @@ int kt_launch_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t 
 {
     return by_types(dt, it, [&](auto t, auto i) {
         typedef decltype(t) T;
-        return fwd(dt, tokens, vocab, width, (const T *)x, ldx, (const T *)w, ldw, (const decltype(i) *)targets, loss, lse, (char *)ws, (hipStream_t)stream);
+        typedef decltype(i) I;
+        const Plan p = plan_of(dt, tokens, vocab, width, false);
+        if constexpr (sizeof(T) == 4) {
+            if (p.three) return fwd<Three, T, I>(p, dt, tokens, vocab, width, (const T *)x, ldx, (const T *)w, ldw, (const I *)targets, loss, lse, (char *)ws, (hipStream_t)stream);
+        }
+        return fwd<T, T, I>(p, dt, tokens, vocab, width, (const T *)x, ldx, (const T *)w, ldw, (const I *)targets, loss, lse, (char *)ws, (hipStream_t)stream);
     });
 }
 
@@ -960,6 +1181,12 @@ int kt_launch_linear_xent_bwd(kt_dtype dt, kt_index it, int64_t tokens, int64_t 
 {
     return by_types(dt, it, [&](auto t, auto i) {
         typedef decltype(t) T;
-        return bwd(dt, tokens, vocab, width, dloss, (const T *)x, ldx, (const T *)w, ldw, (const decltype(i) *)targets, lse, (T *)dx, lddx, (T *)dw, lddw, (char *)ws, (hipStream_t)stream);
+        typedef decltype(i) I;
+        const Plan p = plan_of(dt, tokens, vocab, width, true);
+        if constexpr (sizeof(T) == 4) {
+            if (p.three)
+                return bwd<Three, T, I>(p, dt, tokens, vocab, width, dloss, (const T *)x, ldx, (const T *)w, ldw, (const I *)targets, lse, (T *)dx, lddx, (T *)dw, lddw, (char *)ws, (hipStream_t)stream);
+        }
+        return bwd<T, T, I>(p, dt, tokens, vocab, width, dloss, (const T *)x, ldx, (const T *)w, ldw, (const I *)targets, lse, (T *)dx, lddx, (T *)dw, lddw, (char *)ws, (hipStream_t)stream);
     });
 }

@@ -113,6 +113,27 @@ def test_tiles_and_pieces(dtype, tokens, vocab, width):
     c.check_forward()
 
 
+# f32 numbers in three parts: widths that fill no group of 32 and tiles that fill no 256 x 128, rows at odd places, pieces of the tokens and of the vocabulary
+@pytest.mark.parametrize("tokens,vocab,width,gap,off", [(512, 12288, 128, 0, 0), (700, 12301, 132, 0, 0), (513, 12289, 129, 3, 1), (6200, 1100, 257, 8, 8),
+                                                        (20000, 4099, 136, 1, 3), (1100, 5003, 1001, 0, 0)])
+def test_numbers_in_three_parts(tokens, vocab, width, gap, off):
+    c = Case(tokens, vocab, width, torch.float32, gap, off).forward()
+    c.check_forward()
+    c.backward().check_backward()
+
+
+def test_numbers_in_three_parts_of_every_size():
+    """From 2^-100 to 2^100, and the type's largest, whose nearest number of 8 bits is infinity: 100 columns that both sides have, products of 1 about."""
+    g = gen(3)
+    c = Case(600, 12301, 200, torch.float32, gaps=False)
+    power = torch.exp2(torch.randint(-100, 101, (200,), generator=g, device=DEV).float())
+    c.x.put(c.x.t * power)
+    c.w.put(c.w.t / power)
+    c.x.t[:, 0], c.w.t[:, 0] = torch.finfo(torch.float32).max, 2.0 ** -126
+    c.forward().check_forward()
+    c.backward().check_backward()
+
+
 # more vocabulary than a piece of dz takes; more of a weight at odd addresses than is copied at a time
 @pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 20000, 7003, 72), ("f32", 20000, 6657, 40), ("f32", 70, 9500, 8191), ("bf16", 5, 9001, 16383)])
 def test_pieces_of_the_vocabulary(dtype, tokens, vocab, width):
@@ -122,7 +143,7 @@ def test_pieces_of_the_vocabulary(dtype, tokens, vocab, width):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("tokens,vocab,width", [(700, 300, 100), (130, 90, 64), (3000, 4200, 136)])
+@pytest.mark.parametrize("tokens,vocab,width", [(700, 300, 100), (130, 90, 64), (3000, 4200, 136), (1500, 6200, 130)])
 def test_tokens_that_take_no_part(dtype, tokens, vocab, width):
     """Whole tiles and steps of them, at the start, in between and at the end; what their rows hold reaches nothing."""
     c = Case(tokens, vocab, width, DT[dtype])
@@ -184,15 +205,16 @@ def test_large_logits(dtype):
     assert bool(c.dx.t.isfinite().all()) and bool(c.dw.t.isfinite().all())
 
 
-def test_logits_that_are_not_finite():
-    c = Case(100, 200, 64, torch.float32, gaps=False)
+@pytest.mark.parametrize("tokens,vocab,width", [(100, 200, 64), (1500, 6200, 130)])
+def test_logits_that_are_not_finite(tokens, vocab, width):
+    c = Case(tokens, vocab, width, torch.float32, gaps=False)
     c.forward()
     want = c.loss.clone()
     c.x.t[7] = float("nan")
     c.x.t[9] = float("inf")
     c.forward()
     assert not bool(c.loss[7].isfinite()) and not bool(c.loss[9].isfinite())
-    keep = torch.ones(100, dtype=torch.bool, device=DEV)
+    keep = torch.ones(tokens, dtype=torch.bool, device=DEV)
     keep[[7, 9]] = False
     assert torch.equal(c.loss[keep], want[keep])
 
@@ -238,7 +260,7 @@ def test_the_same_bits_every_time_and_with_a_workspace_of_the_callers():
         assert all(torch.equal(a, b) for a, b in zip(first, (c.loss, c.lse, c.dx.t, c.dw.t)))
 
 
-@pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 300, 700, 136), ("f32", 300, 700, 129), ("bf16", 3000, 4200, 136)])
+@pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 300, 700, 136), ("f32", 300, 700, 129), ("bf16", 3000, 4200, 136), ("f32", 1500, 6200, 130)])
 def test_in_graphs_and_on_another_stream(dtype, tokens, vocab, width):
     """Two recorded calls share a workspace; their replays follow each other."""
     c = Case(tokens, vocab, width, DT[dtype]).forward().backward()
