@@ -261,7 +261,10 @@ KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
  *   dt       type of x, w, dx and dw.  dx or dw may be NULL: not wanted.
  *   ws       kt_linear_xent_bwd_workspace(...) bytes: up to 2^27 elements of dz, a row of
  *            binary32 sums for each token, and copies as in the forward pass.
- * Rounding in bf16: dz is rounded to bf16 as an operand of both products.  f32 has no
+ * lse has to be that of these logits, but its roundings may be others: the element of a
+ * target that is likely is, in f32, minus the sum of the others' (where dz is one piece).
+ * Rounding in bf16: dz, in units of the largest dloss, is rounded to bf16 as an operand of
+ * both products.  f32 has no
  * rounding but that of its own arithmetic, and the parts of large products as above.
  */
 KT_API int64_t kt_linear_xent_bwd_workspace(kt_dtype dt, int64_t tokens,

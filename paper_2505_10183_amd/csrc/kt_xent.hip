@@ -53,24 +53,38 @@ struct Three {
 constexpr int PLANES = 3, GROUP = 32;
 static_assert(sizeof(Three) * GROUP == 64 * PLANES, "pointers to Three count elements, a group at a time");
 
-// 8 numbers of a group, from column c % 32 = 0, 8, 16 or 24 on.  A number that is not finite is its first part, and one that would round to infinity is
-// cut off instead.
+// A number that is not finite is its first part, and one that would round to infinity is cut off instead.
+__device__ __forceinline__ void in_parts(float f, bf16 *part)
+{
+    const uint32_t bits = as_u(f);
+    const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+    float first = (float)(bf16)f;
+    if (finite && (as_u(first) & 0x7f800000u) == 0x7f800000u) first = as_f(bits & 0xffff0000u);
+    const float left = finite ? f - first : 0.0f, second = (float)(bf16)left;
+    part[0] = (bf16)first;
+    part[1] = (bf16)second;
+    part[2] = (bf16)(left - second);
+}
+// 8 numbers of a group, from column c % 32 = 0, 8, 16 or 24 on; one.
 __device__ __forceinline__ void put_three(Three *group, int c, const float *f)
 {
     bf16x8 part[PLANES];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const uint32_t bits = as_u(f[j]);
-        const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
-        float first = (float)(bf16)f[j];
-        if (finite && (as_u(first) & 0x7f800000u) == 0x7f800000u) first = as_f(bits & 0xffff0000u);
-        const float left = finite ? f[j] - first : 0.0f, second = (float)(bf16)left;
-        part[0][j] = (bf16)first;
-        part[1][j] = (bf16)second;
-        part[2][j] = (bf16)(left - second);
+        bf16 of[PLANES];
+        in_parts(f[j], of);
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) part[p][j] = of[p];
     }
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) *(u32x4 *)((char *)group + p * 64 + c * 2) = __builtin_bit_cast(u32x4, part[p]);
+}
+__device__ __forceinline__ void put_one(Three *group, int c, float f)
+{
+    bf16 of[PLANES];
+    in_parts(f, of);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) *(bf16 *)((char *)group + p * 64 + c * 2) = of[p];
 }
 
 // A number that a kernel before has written, the same for all.
@@ -517,16 +531,18 @@ template <typename I> struct Stats {
 
 // Backward: dz of a piece of the vocabulary, rows of tokens `ld` apart; columns past the vocabulary are zeros.
 template <typename T, typename I> struct Slope {
-    static constexpr bool ROWS = true;
+    static constexpr bool ROWS = true, HALVES = std::is_same_v<T, bf16>;
     T *dz;
     int64_t ld;
-    const float *lse, *dloss;
+    const float *lse, *dloss, *unit;
+    float *others;                  // [row][part of `parts`]: what the exponentials of other rows than the target's add up to, or null
     const I *targets;
     const int *map, *live;          // the token of each row, and their number
-    int tokens, vocab, first, end_;
+    int tokens, vocab, first, end_, parts;
     __device__ __forceinline__ bool skip(int, int) const { return false; }
     template <typename A> __device__ __forceinline__ void begin(A &, int64_t) const {}
-    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int64_t, int, char *scratch) const
+    __device__ __forceinline__ float share(int at) const { return HALVES ? dloss[at] / *unit : dloss[at]; }
+    template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int64_t, int part, char *scratch) const
     {
         const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
 #pragma unroll
@@ -534,13 +550,15 @@ template <typename T, typename I> struct Slope {
             const int row = n + 32 * j, first_row = row - l, rows = scalar(live);
             if (first_row >= rows) continue;
             const int at = map[min(row, rows - 1)], target = (int)targets[at] - first, room = end_ - first;
-            const float up = dloss[at], base = lse[at];
+            const float up = share(at), base = lse[at];
+            float sum = 0;
             auto values = [&](int i, float *f) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int v = m + 32 * i + r;
-                    const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E) - (v == target ? 1.0f : 0.0f);
+                    const float e = __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E), p = e - (v == target ? 1.0f : 0.0f);
                     f[r] = v < room ? p * up : 0.0f;
+                    if constexpr (!HALVES) sum += v < room && v != target ? e : 0.0f;
                 }
             };
             if constexpr (std::is_same_v<T, Three>) {
@@ -556,24 +574,57 @@ template <typename T, typename I> struct Slope {
             } else {
                 store_rows<FM>(scratch, dz + m0, ld, first_row, rows - first_row, (int)ld - m0, nullptr, values);
             }
+            if constexpr (!HALVES) {
+                sum += __shfl_xor(sum, 32);
+                if (others && h == 0 && row < rows) others[(int64_t)row * parts + part] = sum;
+            }
         }
     }
-    __device__ __forceinline__ void few(f32x4 z, int v, int t, int) const
+    __device__ __forceinline__ void few(f32x4 z, int v, int t, int part) const
     {
-        if (t >= scalar(live) || v >= ld) return;
+        if (t >= scalar(live)) return;
         const int at = map[t], want = (int)targets[at] - first - v, room = end_ - first - v;
-        const float up = dloss[at], base = lse[at];
+        const float up = share(at), base = lse[at];
         T f[4];
+        float sum = 0;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float p = __builtin_amdgcn_exp2f((z[r] - base) * LOG2E) - (r == want ? 1.0f : 0.0f);
+            const float e = __builtin_amdgcn_exp2f((z[r] - base) * LOG2E), p = e - (r == want ? 1.0f : 0.0f);
             f[r] = (T)(r < room ? p * up : 0.0f);
+            sum += r < room && r != want ? e : 0.0f;
         }
+        if constexpr (!HALVES) {
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (others && (threadIdx.x & 63) < 16) others[(int64_t)t * parts + part] = sum;
+        }
+        if (v >= ld) return;
         T *row = dz + t * ld + v;
-        if constexpr (sizeof(T) == 2) *(u32x2 *)row = __builtin_bit_cast(u32x2, f);
+        if constexpr (HALVES) *(u32x2 *)row = __builtin_bit_cast(u32x2, f);
         else *(u32x4 *)row = __builtin_bit_cast(u32x4, f);
     }
 };
+
+// f32, where a piece is the whole vocabulary: exp(z - lse) - 1 of a target that is likely is a difference of near numbers, off by what z and lse are, and is
+// taken from the others' exponentials, which add up to what it lacks of 1.  (Below 1/2 the difference is the nearer one.)  With logits of 4096 products and an
+// lse whose roundings are not this layer's the gradients of 4 tokens of 1000 were off by 2.1e-5 of their norm.  A wavefront a token: 3 us at a few.
+template <typename X, typename I>
+__global__ __launch_bounds__(256) void kt_xent_target_kernel(X *dz, int64_t ld, const float *others, int parts, const float *dloss, const I *targets, const int *map,
+                                                             const int *live)
+{
+    const int row = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
+    if (row >= *live) return;
+    const float *of = others + (int64_t)row * parts;
+    float sum = 0;
+    for (int k = lane; k < parts; k += 64) sum += of[k];
+#pragma unroll
+    for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+    if (lane || !(sum < 0.5f)) return;
+    const int at = map[row], v = (int)targets[at];
+    const float f = -sum * dloss[at];
+    if constexpr (std::is_same_v<X, Three>) put_one(dz + row * ld + v / GROUP * GROUP, v % GROUP, f);
+    else dz[row * ld + v] = f;
+}
 
 // Sums that the next piece of the vocabulary goes on with, as the lanes hold them: nobody else reads them.  `holder`: the wavefront's number.
 template <int FM, int FN> __device__ __forceinline__ void resume(const float *sums, int64_t holder, f32x16 (&acc)[FM][FN])
@@ -623,6 +674,7 @@ template <typename G> struct Result {
     int64_t ld, apart;              // rows; matrices of the pieces of k
     const float *sums;              // what Carry left, or null
     const int *map, *live;          // where a row goes, and how many there are, or null
+    const float *unit;              // what the sums are in, or null: 1
     int rows, cols;
     __device__ __forceinline__ bool skip(int, int) const { return false; }
     template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int64_t holder) const
@@ -632,13 +684,14 @@ template <typename G> struct Result {
     template <int FM, int FN> __device__ __forceinline__ void end(f32x16 (&acc)[FM][FN], int m, int n, int64_t, int, char *scratch) const
     {
         const int h = threadIdx.x >> 5 & 1, l = threadIdx.x & 31, m0 = m - 16 * h;
+        const float of = unit ? *unit : 1.0f;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const int first = n + 32 * j - l, end = live ? scalar(live) : rows;
             if (first >= end || m0 >= cols) continue;
             store_rows<FM>(scratch, out + blockIdx.y * apart + m0, ld, first, end - first, cols - m0, map, [&](int i, float *f) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) f[r] = acc[i][j][r];
+                for (int r = 0; r < 16; ++r) f[r] = acc[i][j][r] * of;
             });
         }
     }
@@ -685,12 +738,18 @@ __global__ __launch_bounds__(64) void kt_xent_few_kernel(const T *w, int64_t ldw
             for (int t = 0; t < GROUPS; ++t) rb[set][u][t] = ld16(b[t] + k + u * STEP_);
         }
     };
+    // a set's sums first, then theirs: 4096 f32 products one after another are off three times as far, at no less time
     auto use = [&](auto set0) __attribute__((always_inline)) {
         constexpr int set = set0;
+        f32x4 of[GROUPS];
+#pragma unroll
+        for (int t = 0; t < GROUPS; ++t) of[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int u = 0; u < FEW_AHEAD; ++u)
 #pragma unroll
-            for (int t = 0; t < GROUPS; ++t) multiply16(z[t], ra[set][u], rb[set][u][t], T());
+            for (int t = 0; t < GROUPS; ++t) multiply16(of[t], ra[set][u], rb[set][u][t], T());
+#pragma unroll
+        for (int t = 0; t < GROUPS; ++t) z[t] += of[t];
     };
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
@@ -780,22 +839,37 @@ __global__ __launch_bounds__(256) void kt_xent_join_kernel(const f32x2 *parts, i
     if (lse) lse[t] = on ? all : 0.0f;
 }
 
-// The tokens that take part, in their order, and their number.  A workgroup counts those before its own by itself, which takes one launch.
+// The tokens that take part, in their order, and their number; the largest finite dloss of one.  A workgroup counts those before its own by itself, which takes one launch.
 template <typename I>
-__global__ __launch_bounds__(1024) void kt_xent_list_kernel(const I *targets, const float *dloss, int tokens, int vocab, int *map, int *live)
+__global__ __launch_bounds__(1024) void kt_xent_list_kernel(const I *targets, const float *dloss, int tokens, int vocab, int *map, int *live, float *unit)
 {
     __shared__ int before[16], mine[16];
+    __shared__ float most[16];
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, first = blockIdx.x * 1024, t = first + threadIdx.x;
     auto takes_part = [&](int t) { return target_of(targets, t, tokens, vocab) >= 0 && (!dloss || dloss[t] != 0.0f); };
     int n = 0;
+    float top = 0;
+    auto see = [&](int t) {
+        const float up = fabsf(dloss[t]);
+        if (up < INFINITY) top = fmaxf(top, up);
+    };
 #pragma unroll 4
-    for (int at = threadIdx.x; at < first; at += 1024) n += takes_part(at);
-    for (int d = 32; d; d /= 2) n += __shfl_xor(n, d);
+    for (int at = threadIdx.x; at < first; at += 1024) {
+        const bool on = takes_part(at);
+        n += on;
+        if (unit && on) see(at);
+    }
     const bool on = takes_part(t);
+    if (unit && on) see(t);
+    for (int d = 32; d; d /= 2) {
+        n += __shfl_xor(n, d);
+        top = fmaxf(top, __shfl_xor(top, d));
+    }
     const uint64_t word = __ballot(on);
     if (lane == 0) {
         before[wave] = n;
         mine[wave] = __popcll(word);
+        most[wave] = top;
     }
     __syncthreads();
     int at = 0, all = 0;
@@ -804,7 +878,11 @@ __global__ __launch_bounds__(1024) void kt_xent_list_kernel(const I *targets, co
         all += before[w] + mine[w];
     }
     if (on) map[at + __popcll(word & ((1ull << lane) - 1))] = t;
-    if (threadIdx.x == 0 && blockIdx.x == gridDim.x - 1) *live = all;
+    if (threadIdx.x || blockIdx.x != gridDim.x - 1) return;
+    *live = all;
+    if (!unit) return;
+    for (int w = 0; w < 16; ++w) top = fmaxf(top, most[w]);
+    *unit = top > 0 ? top : 1.0f;
 }
 
 // Their rows of x one after another, zeros up to `ld`; where dx is given, zeros into its rows of the other tokens.
@@ -825,13 +903,14 @@ __global__ __launch_bounds__(256) void kt_xent_gather_kernel(const T *x, int64_t
     }
 }
 
-// The sum of pieces of k, in their order; rows of the pieces `ldp` apart.  map, live: as Result has them.
+// The sum of pieces of k, in their order; rows of the pieces `ldp` apart.  map, live, unit: as Result has them.
 template <typename G>
 __global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, int pieces, int64_t apart, int ldp, int rows, int cols, G *out, int64_t ld, const int *map,
-                                                           const int *live)
+                                                           const int *live, const float *unit)
 {
     const int across = (cols + 3) / 4;
     if (live) rows = *live;
+    const float of = unit ? *unit : 1.0f;
     for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < (int64_t)rows * across; n += (int64_t)gridDim.x * 256) {
         const int64_t row = n / across;
         const int c = (int)(n % across) * 4;
@@ -841,7 +920,7 @@ __global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, in
         for (int k = 1; k < pieces; ++k) s += *(const f32x4 *)(p + k * apart);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (c + j < cols) out[to + c + j] = (G)s[j];
+            if (c + j < cols) out[to + c + j] = (G)(s[j] * of);
     }
 }
 
@@ -897,12 +976,13 @@ bool few_tokens(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
     return tokens <= 16 || (tokens <= 32 && (width * (dt == KT_F32 ? 4 : 2) % 16 || vocab * width < 1 << 25));
 }
 
-// Whether f32 products are made of numbers in three parts: where the copies into parts cost little beside them and tiles of 256 x 128 keep the chip busy.
-// us, f32 instructions and parts: forward 8192 tokens of 50304 x 768 4810 and 3020, 1024 of 5003 x 1001 118 and 90, but 512 of 5003 x 1024 65 and 87;
-// backward 4096 of 50304 x 768 7520 and 5160, 512 of 5003 x 1024 204 and 171, but 100 of 50304 x 768 343 and 375, 1024 of 1000 x 768 92 and 116.
-bool in_three(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd)
+// Whether f32 products are made of numbers in three parts: where the copies into parts cost little beside them and tiles of 256 x 128 keep the chip busy.  The
+// same in both passes, so that their logits have the same bits.  us, f32 instructions and parts: 8192 tokens of 50304 x 768 4810 and 3020 forward and
+// 14870 and 10100 backward, 1024 of 5003 x 1001 118 and 90, 365 and 231, 512 of 5003 x 1024 65 and 87, 204 and 171; but 2048 of 1000 x 4096 172 and 247, 468
+// and 436, 1024 of 1000 x 768 26 and 64, 93 and 117, 100 of 50304 x 768 114 and 182, 343 and 375.
+bool in_three(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
 {
-    return dt == KT_F32 && width >= 128 && tokens >= (bwd ? 256 : 512) && over(vocab, Split::BM) * over(tokens, Split::BN) >= (bwd ? 64 : 144);
+    return dt == KT_F32 && width >= 128 && tokens >= 256 && over(vocab, Split::BM) * over(tokens, Split::BN) >= 80;
 }
 
 // What a call needs of the workspace, and its cut.  Matrices that loads of 16 bytes cannot take as they are are copied to rows of a multiple of 16 bytes first
@@ -912,11 +992,12 @@ struct Plan {
     int64_t es, wide;               // bytes of an operand's element; elements to a row of a copy
     int64_t copy;                   // rows of the weight copied at a time
     int64_t most, piece;            // rows of the vocabulary in a piece: with the weight as it is; with copies
-    Cut z;                          // of the forward pass
+    Cut z;                          // of the logits of the whole vocabulary
+    int64_t slopes;                 // wavefronts that share a token's logits then
     int64_t ldp;                    // backward: elements to a row of sums
     Cut kx;                         // of dx over a piece of the vocabulary
     bool list;                      // whether the tokens that take part are listed
-    int64_t x, w, parts, hit, dz, map, live, acc, sums, bytes;  // where in the workspace
+    int64_t x, w, parts, hit, others, dz, map, live, acc, sums, bytes;  // where in the workspace
 };
 int64_t at_most(int64_t a, int64_t b) { return a < b ? a : b; }
 // Rows of a multiple of 256 that keep rows * of below `most`.
@@ -929,7 +1010,7 @@ int64_t rows_in(int64_t most, int64_t of, int64_t vocab)
 Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd)
 {
     Plan p{};
-    p.three = in_three(dt, tokens, vocab, width, bwd);
+    p.three = in_three(dt, tokens, vocab, width);
     p.es = p.three ? sizeof(Three) : dt == KT_F32 ? 4 : 2;
     p.wide = up(width, 64);
     p.copy = rows_in(128 << 20, p.wide * p.es, vocab);
@@ -950,12 +1031,14 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
     // a list and a copy of x cost some 6 us and its bytes twice: worth while for the forward pass from some 100 us on
     p.list = bwd || p.three || (double)tokens * vocab * width * (dt == KT_F32 ? 8 : 1) > 5e10;
     p.map = take(p.list ? tokens * 4 : 0);
-    p.live = take(p.list ? 4 : 0);
+    p.live = take(p.list ? 8 : 0);
+    p.slopes = few ? over(vocab, 16) : over(vocab, p.z.m()) * (p.z.m() / p.z.part());
     if (!bwd) {
-        p.parts = take((few ? over(vocab, 16) : over(vocab, p.z.m()) * (p.z.m() / p.z.part())) * tokens * 8);
+        p.parts = take(p.slopes * tokens * 8);
         p.hit = take(tokens * 4);
         return p;
     }
+    p.others = take(dt == KT_F32 && p.most >= vocab ? p.slopes * tokens * 4 : 0);
     p.dz = take(tokens * p.most * p.es);
     p.kx = cut_of(dt, p.three, width, tokens, at_most(p.most, vocab), MOST_PIECES);
     if (p.piece < vocab) p.acc = take(p.kx.pieces * over(width, p.kx.m()) * over(tokens, p.kx.n()) * p.kx.m() * p.kx.n() * 4);
@@ -1041,9 +1124,9 @@ int aligned_rows(bool as_is, const T *x, int64_t ldx, int64_t width, int64_t row
 // The list of the tokens that take part and their rows of x; zeros in dx's rows of the others.
 template <typename X, typename T, typename I>
 int list(const T *x, int64_t ldx, int64_t width, const I *targets, const float *dloss, int64_t tokens, int64_t vocab, X *copy, int64_t wide, int *map,
-         int *live, T *dx, int64_t lddx, hipStream_t s)
+         int *live, float *unit, T *dx, int64_t lddx, hipStream_t s)
 {
-    kt_xent_list_kernel<I><<<(unsigned)over(tokens, 1024), 1024, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, map, live);
+    kt_xent_list_kernel<I><<<(unsigned)over(tokens, 1024), 1024, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, map, live, unit);
     KT_GO((int)hipGetLastError());
     const int64_t blocks = over(tokens * over(wide, 64 * EACH<X>), 4);
     kt_xent_gather_kernel<X, T, I><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, map, live, targets, dloss, (int)tokens, (int)vocab, dx, lddx);
@@ -1061,13 +1144,12 @@ int fwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
     const bool w_as_is = std::is_same_v<X, T> && plain(w, ldw, width), by_few = few_tokens(dt, tokens, vocab, width);
     X *const copy = (X *)(ws + p.x);
     Operand<X> a, b;
-    int count = (int)(over(vocab, p.z.m()) * (p.z.m() / p.z.part()));
+    const int count = (int)p.slopes;
     if (by_few) {
         const Stats<I> e{parts, hit, targets, nullptr, nullptr, (int)tokens, (int)vocab, 0, (int)vocab, 0};
         KT_GO(few(w, ldw, vocab, x, ldx, tokens, width, e, s));
-        count = (int)over(vocab, 16);
     } else if (p.list) {
-        KT_GO((list<X, T, I>(x, ldx, width, targets, nullptr, tokens, vocab, copy, p.wide, map, live, nullptr, 0, s)));
+        KT_GO((list<X, T, I>(x, ldx, width, targets, nullptr, tokens, vocab, copy, p.wide, map, live, nullptr, nullptr, 0, s)));
         b = Operand<X>{copy, p.wide, (int)tokens};
     } else {
         KT_GO((aligned_rows<X, T>(plain(x, ldx, width), x, ldx, width, tokens, copy, p.wide, &b, s)));
@@ -1084,10 +1166,10 @@ int fwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
 }
 
 template <typename G> int sum(const float *parts, const Cut &k, int64_t apart, int64_t ldp, int64_t rows, int64_t cols, G *out, int64_t ld, const int *map, const int *live,
-                              hipStream_t s)
+                              const float *unit, hipStream_t s)
 {
     const int64_t blocks = over(rows * over(cols, 4), 256);
-    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.pieces, apart, (int)ldp, (int)rows, (int)cols, out, ld, map, live);
+    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.pieces, apart, (int)ldp, (int)rows, (int)cols, out, ld, map, live, unit);
     return (int)hipGetLastError();
 }
 
@@ -1100,23 +1182,30 @@ int bwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
     float *acc = (float *)(ws + p.acc), *sums = (float *)(ws + p.sums);
     const bool w_as_is = std::is_same_v<X, T> && plain(w, ldw, width);
     constexpr int UNIT = std::is_same_v<X, Three> ? GROUP : VE<T>;
+    // bf16: dz in units of the largest dloss, so that a mean's 1 / tokens, the same share of every token, is not rounded with it
+    float *const unit = tokens && sizeof(T) == 2 ? (float *)live + 1 : nullptr;
     const int64_t cols = up(width, UNIT);               // of an operand: what a copy has past the width is zeros
     const int64_t piece = w_as_is ? p.most : p.piece;
+    float *const others = sizeof(T) == 4 && piece >= vocab ? (float *)(ws + p.others) : nullptr;
     X *const copy = (X *)(ws + p.x);
     Operand<X> a;
     const Operand<X> b{copy, p.wide, (int)tokens};
-    if (tokens) KT_GO((list<X, T, I>(x, ldx, width, targets, dloss, tokens, vocab, copy, p.wide, map, live, dx, lddx, s)));
+    if (tokens) KT_GO((list<X, T, I>(x, ldx, width, targets, dloss, tokens, vocab, copy, p.wide, map, live, unit, dx, lddx, s)));
     for (int64_t v = 0, rows; v < vocab; v += rows) {
         rows = at_most(piece, vocab - v);
         if (tokens) {
             KT_GO((aligned_rows<X, T>(w_as_is, w + v * ldw, ldw, width, rows, (X *)(ws + p.w), p.wide, &a, s)));
-            const Slope<X, I> e{dz, p.most, lse, dloss, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows)};
+            const Slope<X, I> e{dz, p.most, lse, dloss, unit, others, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows), (int)p.slopes};
             bool made = false;
             if constexpr (std::is_same_v<X, T>) {
                 made = few_tokens(dt, tokens, vocab, width);
                 if (made) KT_GO(few(a.p, a.ld, rows, (const T *)copy, p.wide, tokens, width, e, s));
             }
             if (!made) KT_GO((product<X, true, true>(cut_of(dt, p.three, rows, tokens, width, 1), a, rows, b, tokens, width, live, e, s)));
+            if (others) {
+                kt_xent_target_kernel<X, I><<<(unsigned)over(tokens, 4), 256, 0, s>>>(dz, p.most, others, (int)p.slopes, dloss, targets, map, live);
+                KT_GO((int)hipGetLastError());
+            }
         }
         if (dx && tokens) {
             const Operand<X> wide{a.p, a.ld, (int)cols}, slope{dz, p.most, (int)tokens};
@@ -1126,25 +1215,25 @@ int bwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
                 const Carry e{acc, first};
                 KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else if (k.pieces == 1) {
-                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, map, live, (int)tokens, (int)width};
+                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, map, live, unit, (int)tokens, (int)width};
                 KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else {
                 const int64_t apart = tokens * p.ldp;
-                const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, nullptr, live, (int)tokens, (int)p.ldp};
+                const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, nullptr, live, nullptr, (int)tokens, (int)p.ldp};
                 KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
-                KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, map, live, s));
+                KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, map, live, unit, s));
             }
         }
         if (dw) {
             const Operand<X> wide{b.p, b.ld, (int)cols}, slope{dz, p.most, (int)up(rows, UNIT)};
             const Cut k = cut_of(dt, p.three, width, rows, tokens, MOST_PIECES);
             if (k.pieces == 1) {
-                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, nullptr, (int)rows, (int)width};
+                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, nullptr, unit, (int)rows, (int)width};
                 KT_GO((product<X, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
             } else {
-                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, nullptr, (int)rows, (int)p.ldp};
+                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, nullptr, nullptr, (int)rows, (int)p.ldp};
                 KT_GO((product<X, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
-                KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, nullptr, nullptr, s));
+                KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, nullptr, nullptr, unit, s));
             }
         }
     }

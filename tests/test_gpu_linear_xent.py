@@ -219,6 +219,61 @@ def test_logits_that_are_not_finite(tokens, vocab, width):
     assert torch.equal(c.loss[keep], want[keep])
 
 
+@pytest.mark.parametrize("tokens,vocab,width", [(4, 1000, 4096), (30, 900, 520), (300, 700, 136), (700, 12301, 132)])
+def test_targets_that_are_likely(tokens, vocab, width):
+    """With an lse that has none of the kernels' roundings a target of probability p lacks as much of 1 as the others have: off by a share of 1 - p, not of p."""
+    c = Case(tokens, vocab, width, torch.float32, gaps=False, lean=16.0)
+    x, w = c.x.t.double(), c.w.t.double()
+    z = x @ w.t().contiguous()
+    ez = (width + 2) * U * (x.abs() @ w.abs().t().contiguous())
+    lse = torch.logsumexp(z, 1)
+    c.lse.copy_(lse)
+    c.dloss.abs_()
+    c.backward()
+    n = torch.arange(tokens, device=DEV)
+    p, share = torch.exp(z - lse[:, None]), ez + 5 * U * lse[:, None] + 4 * U * (z.abs() + 1)
+    dz, wrong = p.clone(), p * share
+    dz[n, c.at] = 0
+    others, off = dz.sum(1), wrong.sum(1) - wrong[n, c.at]
+    dz[n, c.at] = -others
+    wrong[n, c.at] = torch.where(others < 0.49, off + (300 + vocab / 16) * U * others, wrong[n, c.at] + off)
+    assert bool((others < 0.49).any())
+    up = c.dloss.double()[:, None]
+    dz, wrong = dz * up, wrong * up + 3 * U * dz.abs() * up
+    want, size = dz @ w, dz.abs() @ w.abs()
+    within(c.dx.t, want, wrong @ w.abs() * (1 + U) + (vocab + 40) * U * size + U * want.abs(), "dx")
+    dzt, wt = dz.t().contiguous(), wrong.t().contiguous()
+    want, size = dzt @ x, dzt.abs() @ x.abs()
+    within(c.dw.t, want, wt @ x.abs() * (1 + U) + (tokens + 40) * U * size + U * want.abs(), "dw")
+
+
+@pytest.mark.parametrize("tokens,vocab,width", [(3, 500, 264), (200, 300, 72), (3000, 300, 72)])
+def test_a_common_dloss_is_not_rounded_to_bf16(tokens, vocab, width):
+    """dz is rounded in units of the largest dloss: gradients of equal ones are in proportion but for their own two roundings."""
+    c = Case(tokens, vocab, width, torch.bfloat16).forward()
+    c.dloss.fill_(1.0)
+    c.backward()
+    dx, dw = c.dx.t.double(), c.dw.t.double()
+    for up in (1 / 3, 0.7, 1e-20, 3e4):
+        c.dloss.fill_(up)
+        c.backward()
+        up = float(c.dloss[0])
+        for got, one in ((c.dx.t, dx), (c.dw.t, dw)):
+            within(got, up * one, 2.01 * HALF[torch.bfloat16] * (up * one).abs(), up)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_dloss_that_is_not_finite(dtype):
+    c = Case(200, 300, 72, DT[dtype], gaps=False).forward().backward()
+    dx, largest = c.dx.t.clone(), int(c.dloss.abs().argmax())
+    t = (largest + 1) % 200
+    for bad in (float("inf"), float("nan")):
+        c.dloss[t] = bad
+        c.backward()
+        others = torch.arange(200, device=DEV) != t
+        assert torch.equal(c.dx.t[others], dx[others]) and not bool(c.dx.t[t].isfinite().all()) and not bool(c.dw.t.isfinite().all())
+
+
 def test_gradient_against_differences():
     """Of the sum of dloss * loss: central differences with steps of h are off by h^2 of the third derivative (below 1 for logits' steps of h) and
     by twice the losses' own error over 2 h."""
@@ -260,7 +315,7 @@ def test_the_same_bits_every_time_and_with_a_workspace_of_the_callers():
         assert all(torch.equal(a, b) for a, b in zip(first, (c.loss, c.lse, c.dx.t, c.dw.t)))
 
 
-@pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 300, 700, 136), ("f32", 300, 700, 129), ("bf16", 3000, 4200, 136), ("f32", 1500, 6200, 130)])
+@pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 300, 700, 136), ("f32", 300, 700, 129), ("bf16", 3000, 4200, 136), ("f32", 1500, 6200, 130), ("f32", 20, 700, 136)])
 def test_in_graphs_and_on_another_stream(dtype, tokens, vocab, width):
     """Two recorded calls share a workspace; their replays follow each other."""
     c = Case(tokens, vocab, width, DT[dtype]).forward().backward()
