@@ -264,8 +264,8 @@ KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
  * lse has to be that of these logits, but its roundings may be others: the element of a
  * target that is likely is, in f32, minus the sum of the others' (where dz is one piece).
  * Rounding in bf16: dz, in units of the largest dloss, is rounded to bf16 as an operand of
- * both products.  f32 has no
- * rounding but that of its own arithmetic, and the parts of large products as above.
+ * both products.  f32 has no rounding but that of its own arithmetic, and the parts of
+ * large products as above.
  */
 KT_API int64_t kt_linear_xent_bwd_workspace(kt_dtype dt, int64_t tokens,
                                             int64_t vocab, int64_t width);

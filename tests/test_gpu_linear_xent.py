@@ -113,6 +113,15 @@ def test_tiles_and_pieces(dtype, tokens, vocab, width):
     c.check_forward()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [8192, 8193, 300001])
+def test_many_tokens(tokens, dtype):
+    """Listed by workgroups that count for themselves, and in two launches."""
+    c = Case(tokens, 33, 24, DT[dtype], it=32).forward()
+    c.check_forward()
+    c.backward().check_backward()
+
+
 # f32 numbers in three parts: widths that fill no group of 32 and tiles that fill no 256 x 128, rows at odd places, pieces of the tokens and of the vocabulary
 @pytest.mark.parametrize("tokens,vocab,width,gap,off", [(512, 12288, 128, 0, 0), (700, 12301, 132, 0, 0), (513, 12289, 129, 3, 1), (6200, 1100, 257, 8, 8),
                                                         (20000, 4099, 136, 1, 3), (1100, 5003, 1001, 0, 0)])
