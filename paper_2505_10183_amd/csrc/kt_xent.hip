@@ -840,8 +840,9 @@ __global__ __launch_bounds__(256) void kt_xent_join_kernel(const f32x2 *parts, i
     __syncthreads();
     if (w || t >= tokens) return;
     for (int k = 1; k < LEFT; ++k) add(of[k][i]);
-    const float all = top + __builtin_amdgcn_logf(sum) * LN2;
-    loss[t] = on ? all - hit[t] : 0.0f;
+    // the loss not by way of lse, whose rounding a likely target's loss would be small beside
+    const float rest = __builtin_amdgcn_logf(sum) * LN2, all = top + rest;
+    loss[t] = on ? (top - hit[t]) + rest : 0.0f;
     if (lse) lse[t] = on ? all : 0.0f;
 }
 
