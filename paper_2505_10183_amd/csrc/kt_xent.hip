@@ -622,6 +622,7 @@ __global__ __launch_bounds__(256) void kt_xent_target_kernel(X *dz, int64_t ld, 
     if (row >= *live) return;
     const float *of = others + (int64_t)row * parts;
     float sum = 0;
+#pragma unroll 8
     for (int k = lane; k < parts; k += 64) sum += of[k];
 #pragma unroll
     for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
@@ -981,6 +982,8 @@ struct Cut {
 // to 555 us, of 128 600 to 650, of 64 850 to 1060; f32 4096 x 32768 x 768: 128 1578 to 1684, 64 1639 to 1829; in
 // three parts 8192 x 50304 x 768 3000).  Both sides of a choice, us: f32
 // 768 x 4096 over 32768 in 2 pieces (384 workgroups) 2024, in 4 (768) 1578; bf16 2048 x 1152 over 16384 in tiles of 64 206, of 128 in 3 pieces 122.
+// A workgroup of 4 wavefronts that has a CU to itself waits for its loads with nothing beside it, `alone` times the rate.  Without that and with it, gradients: 1024 tokens of
+// 50304 x 768 bf16 382 and 352 (dx in twice the pieces), 4000 of 300 x 768 46.6 and 42.9, f32 92 of 50304 x 1024 422 and 383, 1000 of 1000 x 768 91.7 and 83.9.
 Cut cut_of(kt_dtype dt, bool three, int64_t m, int64_t n, int64_t k, int64_t most)
 {
     Cut best{three ? 0 : 64, 1, (int)up(k < 1 ? 1 : k, 64)};
@@ -988,12 +991,13 @@ Cut cut_of(kt_dtype dt, bool three, int64_t m, int64_t n, int64_t k, int64_t mos
     for (int side : {0, 256, 128, 64}) {
         if (three != (side == 0) || (side == 256 && dt == KT_F32)) continue;
         const double rate = three ? 4.0e5 : dt == KT_F32 ? (side == 128 ? 2.5e5 : 2.3e5) : side == 256 ? 2.0e6 : side == 128 ? 1.75e6 : 1.15e6;
+        const double alone = side == 64 ? 0.6 : side == 128 ? 0.7 : 1;
         const Cut c{side, 1, 0};
         const int64_t tiles = over(m, c.m()) * over(n, c.n());
         for (int64_t p = 1; p <= most && (p == 1 || p * 128 <= k); ++p) {
             const int64_t piece = up(over(k < 1 ? 1 : k, p), 64), count = over(k < 1 ? 1 : k, piece);
             if (count != p) continue;
-            const double t = (double)over(tiles * p, 256) * c.m() * c.n() * (double)(piece + 128) / rate + (p > 1 ? 4 + (double)m * n * 8 * p / 5.5e6 : 0);
+            const double t = (double)over(tiles * p, 256) * c.m() * c.n() * (double)(piece + 128) / (tiles * p <= 256 ? alone * rate : rate) + (p > 1 ? 4 + (double)m * n * 8 * p / 5.5e6 : 0);
             if (t < least) {
                 least = t;
                 best = Cut{side, (int)p, (int)piece};
