@@ -699,7 +699,7 @@ int bwd(int64_t tokens, int vocab, int width, const I *ids, const T *dy, int64_t
     if (tokens <= HANDFUL) {
         const int span = 64 * EACH<T, W>, spans = (width + span - 1) / span;
         const int64_t zeros = add ? 0 : vocab * ((width * (int64_t)sizeof(W) + 4095) / 4096);
-        const int64_t waves = tokens * spans + (zeros < 16384 ? zeros : 16384);
+        const int64_t waves = tokens * spans + (zeros < 65536 ? zeros : 65536);
         if (waves == 0) return 0;
         // (a wavefront of zeros at least, whatever the last workgroup leaves of them)
         const unsigned blocks = (unsigned)((waves + 3) / 4);

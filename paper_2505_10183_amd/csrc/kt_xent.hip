@@ -1031,7 +1031,8 @@ bool in_three(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
 }
 
 // What a call needs of the workspace, and its cut.  Matrices that loads of 16 bytes cannot take as they are are copied to rows of a multiple of 16 bytes first
-// (the weight up to 128 MiB of it at a time), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
+// (the weight up to 128 MiB of it at a time; 512 in three parts, whose tiles of 256 rows would else be few: gradients of 300 tokens of
+// 50304 x 4096 4509 and 2985 us), which costs their bytes twice more: 4099 tokens of 5003 x 1001 8 of 137 us.
 struct Plan {
     bool three;                     // operands in three parts
     int64_t es, wide;               // bytes of an operand's element; elements to a row of a copy
@@ -1058,7 +1059,7 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
     p.three = in_three(dt, tokens, vocab, width);
     p.es = p.three ? sizeof(Three) : dt == KT_F32 ? 4 : 2;
     p.wide = up(width, 64);
-    p.copy = rows_in(128 << 20, p.wide * p.es, vocab);
+    p.copy = rows_in((p.three ? 512 : 128) << 20, p.wide * p.es, vocab);
     // backward: dz of up to 2^27 elements, 256 MiB of bf16, what the last-level cache holds; forward: a launch of up to 2^20 tiles of 256
     p.most = rows_in(bwd ? 1ll << (p.three ? 26 : 27) : 1ll << 36, tokens, vocab);
     if (bwd) p.most = at_most(p.most, 1 << 18);
