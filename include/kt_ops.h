@@ -262,7 +262,8 @@ KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
  *   ws       kt_linear_xent_bwd_workspace(...) bytes: up to 2^27 elements of dz, a row of
  *            binary32 sums for each token, and copies as in the forward pass.
  * lse has to be that of these logits, but its roundings may be others: the element of a
- * target that is likely is, in f32, minus the sum of the others' (where dz is one piece).
+ * target that is likely is, in f32, minus the sum of the others'.  In bf16 it is a
+ * difference, off by what z and lse are: some 2^-24 of their magnitude, not of its own.
  * Rounding in bf16: dz, in units of the largest dloss, is rounded to bf16 as an operand of
  * both products.  f32 has no rounding but that of its own arithmetic, and the parts of
  * large products as above.
