@@ -235,11 +235,12 @@ KT_API kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it,
  *   dt       type of x [tokens, width] and w [vocab, width];  it: of targets [tokens].
  *   lse      for the backward pass; NULL: not wanted.
  *   ws       kt_linear_xent_fwd_workspace(...) bytes.
- * Logits are products of dt pairs summed in binary32, and not rounded.  Where one is not
- * finite the token's loss is not either.  Large f32 products are made of three bf16 parts
+ * Logits are products of dt pairs summed in binary32, and not rounded.  One of -inf counts
+ * as exp(-inf) = 0 (a target's: the loss is +inf); where one is +inf or NaN, or all are
+ * -inf, the token's loss is infinite or NaN.  Large f32 products are made of three bf16 parts
  * of each number, copied into the workspace, as near as those of the numbers themselves;
- * bits of a number that lie under 2^-133 are lost then, and a sum that an infinite one
- * takes part in is NaN.  x and w may have any stride and start; rows that are
+ * bits of a number that lie under 2^-133 are lost then.  Logits that do not come out finite
+ * that way are made again from the numbers.  x and w may have any stride and start; rows that are
  * not multiples of 16 bytes, or do not begin at one, are copied into the workspace first.
  * KT_EUNSUPPORTED: more than 2^24 tokens or rows of w, 2^20 columns, 2^36 elements of x or w.
  */
@@ -266,7 +267,7 @@ KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
  * difference, off by what z and lse are: some 2^-24 of their magnitude, not of its own.
  * Rounding in bf16: dz, in units of the largest dloss, is rounded to bf16 as an operand of
  * both products.  f32 has no rounding but that of its own arithmetic, and the parts of
- * large products as above.
+ * large products as above.  An infinite weight times a dz of 0 is NaN, as ever.
  */
 KT_API int64_t kt_linear_xent_bwd_workspace(kt_dtype dt, int64_t tokens,
                                             int64_t vocab, int64_t width);

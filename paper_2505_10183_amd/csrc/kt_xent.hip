@@ -49,8 +49,9 @@ template <typename T> struct Operand {
 // A binary32 number as three bf16 that add up to it: 8 bits of its significand each, nearest first.  A product of two such numbers is six products of bf16 pairs,
 // exact and summed in binary32, and what is left out (of the 2nd and the 3rd part, and of the 3rd ones) is below 2^-24 of it, half a step of binary32: for the
 // matrix cores six bf16 products cost six sixteenths of an f32 one.  As the sums have fewer steps, they are nearer: the log-sum-exp of 5003 logits of 4096
-// products each is off by 2.3e-6 on the average, with f32 instructions by 3.0e-6.  Of a number below 2^-110 bits under 2^-133 are lost; an infinite one times
-// a part that is 0 is NaN, so its sums are.  Rows of such numbers are groups of 32, a group the 64 bytes of each part one after another.
+// products each is off by 2.3e-6 on the average, with f32 instructions by 3.0e-6.  Of a number below 2^-110 bits under 2^-133 are lost.  An infinite one times
+// a part that is 0 is NaN, and products of large ones overflow part by part, to infinities of both signs: logits that are not finite are made again from the numbers
+// themselves.  (Not so the gradients' products: dz is finite there, and times an infinite weight nothing is.)  Rows of such numbers are groups of 32, a group the 64 bytes of each part one after another.
 struct Three {
     uint16_t part[3];
 };
@@ -351,6 +352,14 @@ template <int SIDE, int BLOCK, bool ALONG, bool SPREAD> struct BringThree {
         if constexpr (ALONG) return *(const bf16x8 *)(t + along(first + (threadIdx.x & 31), 2 * c + (threadIdx.x >> 5 & 1)));
         else return fragment<bf16, SIDE, false, SPREAD>(t, first, c);
     }
+    // the same of the numbers themselves
+    static __device__ __forceinline__ f32x8 numbers(const char *tile, int first, int c)
+    {
+        f32x8 v = __builtin_convertvector(read(tile, PLANES - 1, first, c), f32x8);
+#pragma unroll
+        for (int p = PLANES - 2; p >= 0; --p) v += __builtin_convertvector(read(tile, p, first, c), f32x8);
+        return v;
+    }
 };
 
 struct Split {
@@ -427,6 +436,60 @@ __global__ __launch_bounds__(Split::BLOCK) void kt_xent_three_kernel(Operand<Thr
         if (more) k += K;
         else --ahead;
     }
+    if constexpr (E::LOGITS) {
+        // Sums times 0 are 0 if they are finite; those of rows past the list, which hold anything, do not count.  4096 tokens of 50304 x 768 forward: 1.95 ms with this look
+        // and without; with a token of NaN, whose tiles all fall to a few CUs, 5.2, with nothing else 5.0.
+        const int rows = live ? scalar(live) : b.count;
+        bool not_finite = false;
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            float zero[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) zero[r % 2] = __builtin_fmaf(acc[i][j][r], 0.0f, zero[r % 2]);
+            not_finite |= !(zero[0] + zero[1] == 0.0f) && n0 + wn + 32 * j + (lane & 31) < rows;
+        }
+        const bool mine = __ballot(not_finite) != 0;
+        int *const odd = (int *)lds;
+        __syncthreads();                                    // LDS is read
+        if (lane == 0) odd[wave] = mine;
+        __syncthreads();
+        int any = 0;
+        for (int w = 0; w < S::WM * S::WN; ++w) any |= odd[w];
+        if (__builtin_amdgcn_readfirstlane(any)) {
+            __syncthreads();                                // all have read what the others say
+            f32x16 sum[S::FM][S::FN];
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j) sum[i][j] = f32x16{0};
+#pragma unroll 1
+            for (k = k0; k < k1; k += K) {
+                bring(lds, k);
+                meet<0>();
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    f32x8 na[S::FM], nb[S::FN];
+#pragma unroll
+                    for (int i = 0; i < S::FM; ++i) na[i] = BringA::numbers(lds, wm + 32 * i, c);
+#pragma unroll
+                    for (int j = 0; j < S::FN; ++j) nb[j] = BringB::numbers(lds + ABYTES, wn + 32 * j, c);
+#pragma unroll
+                    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                        for (int j = 0; j < S::FN; ++j) mma(sum[i][j], na[i], nb[j]);
+                }
+                meet<0>();
+            }
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = fabsf(acc[i][j][r]) < INFINITY ? acc[i][j][r] : sum[i][j][r];
+        }
+    }
     if constexpr (E::ROWS) __syncthreads();                 // LDS is read: the epilogue takes it
     e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), holder, wave / S::WN + S::WM * at.m, lds + wave * (S::FM * 4096));
 }
@@ -472,7 +535,7 @@ template <int FM, typename G, typename F> __device__ __forceinline__ void store_
 // Forward: for a wavefront's vocabulary rows the largest logit of each token and the sum of the exponentials over it; the
 // target's logit.
 template <typename I> struct Stats {
-    static constexpr bool ROWS = false;
+    static constexpr bool ROWS = false, LOGITS = true;
     f32x2 *parts;                   // [part][tokens]
     float *hit;                     // [tokens]
     const I *targets;
@@ -544,7 +607,7 @@ template <typename I> struct Stats {
 
 // Backward: dz of a piece of the vocabulary, rows of tokens `ld` apart; columns past the vocabulary are zeros.
 template <typename T, typename I> struct Slope {
-    static constexpr bool ROWS = true, HALVES = std::is_same_v<T, bf16>;
+    static constexpr bool ROWS = true, LOGITS = true, HALVES = std::is_same_v<T, bf16>;
     T *dz;
     int64_t ld;
     const float *lse, *dloss, *unit;
@@ -715,7 +778,7 @@ template <int FM, int FN> __device__ __forceinline__ void resume(const float *su
             }
 }
 struct Carry {
-    static constexpr bool ROWS = false;
+    static constexpr bool ROWS = false, LOGITS = false;
     float *sums;
     bool first;
     __device__ __forceinline__ bool skip(int, int) const { return false; }
@@ -742,7 +805,7 @@ struct Carry {
 
 // The result, or (G = float, pieces of k) the sums of a piece.
 template <typename G> struct Result {
-    static constexpr bool ROWS = true;
+    static constexpr bool ROWS = true, LOGITS = false;
     G *out;
     int64_t ld, apart;              // rows; matrices of the pieces of k
     const float *sums;              // what Carry left, or null
