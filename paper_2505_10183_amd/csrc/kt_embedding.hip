@@ -346,6 +346,7 @@ template <typename W, int E, bool ADD> __device__ __forceinline__ void put(W *ro
         float o[E];
         load_e<W, E>(row, c, width, old);
         widen_e<W, E>(old, o);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // a neighbour may write what this lane reads (Columns): no load sinks below the first store
 #pragma unroll
         for (int j = 0; j < E; ++j) f[j] += o[j];
     }
