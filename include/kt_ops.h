@@ -207,8 +207,10 @@ KT_API kt_status kt_embedding_fwd(kt_dtype dt, kt_dtype wdt, kt_index it,
 
 /*
  * The gradient of the table: dw[v] = scale * sum over the tokens t with
- * ids[t] = v of dy[t], in the order of t in pieces that depend on the number of
- * tokens alone.  Rows of dy without a token (an id outside [0, vocab)) are not read.
+ * ids[t] = v of dy[t], in the order of t.  The tokens sorted by id are cut into pieces,
+ * as many as the number of tokens and the width say, and a row whose tokens lie in several is
+ * the sum of their sums: its bits depend on the other ids and on the width too.
+ * Rows of dy without a token (an id outside [0, vocab)) are not read.
  *   dt          type of dy [tokens, width];  wdt: type of dw [vocab, width].
  *   accumulate  0: every row of dw is written, those without a token as 0.
  *               Otherwise the sums are added to dw (and rounded once more), and
