@@ -236,7 +236,9 @@ KT_API kt_status kt_embedding_bwd(kt_dtype dt, kt_dtype wdt, kt_index it,
  * loss and lse are 0 there, whatever the token's row of x holds.
  *   dt       type of x [tokens, width] and w [vocab, width];  it: of targets [tokens].
  *   lse      for the backward pass; NULL: not wanted.
- *   ws       kt_linear_xent_fwd_workspace(...) bytes.
+ *   ws       kt_linear_xent_fwd_workspace(...) bytes.  In it: for each token 8 bytes for
+ *            every 16 to 128 rows of w and, beyond a few tokens, its row of x; up to 128 MiB
+ *            of w (512 in three parts; 256 rows at least), whether it has to be copied or not.
  * Logits are products of dt pairs summed in binary32, and not rounded.  One of -inf counts
  * as exp(-inf) = 0 (a target's: the loss is +inf); where one is +inf or NaN, or all are
  * -inf, the token's loss is infinite or NaN.  Large f32 products are made of three bf16 parts
@@ -262,8 +264,13 @@ KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
  * Every element of dx and dw is written.  A token without a target, or with dloss 0,
  * takes no part whatever its row of x holds; its row of dx is 0.
  *   dt       type of x, w, dx and dw.  dx or dw may be NULL: not wanted.
- *   ws       kt_linear_xent_bwd_workspace(...) bytes: up to 2^27 elements of dz, a row of
- *            binary32 sums for each token, and copies as in the forward pass.
+ *   ws       kt_linear_xent_bwd_workspace(...) bytes.  In it: dz of a piece of the
+ *            vocabulary, up to 2^27 elements (2^26 in three parts) or, from 2^19 tokens
+ *            (2^18) on, 256 a token; the tokens' rows of x; copies of w as in the forward
+ *            pass; binary32 sums of the size of dx and of a piece's rows of dw,
+ *            for short products up to 64 sets of them; in f32 the sums of exponentials, up
+ *            to a sixteenth of dz, and kt_embedding_bwd_workspace(...) where there are
+ *            several pieces.
  * lse has to be that of these logits, but its roundings may be others: the element of a
  * target that is likely is, in f32, minus the sum of the others'.  In bf16 it is a
  * difference, off by what z and lse are: some 2^-24 of their magnitude, not of its own.
