@@ -274,8 +274,8 @@ KT_API kt_status kt_linear_xent_fwd(kt_dtype dt, kt_index it, int64_t tokens,
  * lse has to be that of these logits, but its roundings may be others: the element of a
  * target that is likely is, in f32, minus the sum of the others'.  In bf16 it is a
  * difference, off by what z and lse are: some 2^-24 of their magnitude, not of its own.
- * Rounding in bf16: dz, in units of the largest dloss, is rounded to bf16 as an operand of
- * both products.  f32 has no rounding but that of its own arithmetic, and the parts of
+ * Rounding in bf16: dz, in units of the largest finite dloss, is rounded to bf16 as an
+ * operand of both products (and loses more bits where it is under 2^-126 of that).  f32 has no rounding but that of its own arithmetic, and the parts of
  * large products as above.  An infinite weight times a dz of 0 is NaN, as ever.
  */
 KT_API int64_t kt_linear_xent_bwd_workspace(kt_dtype dt, int64_t tokens,

@@ -79,3 +79,11 @@ def test_what_a_workspace_held_before_reaches_nothing(dtype, tokens, vocab, widt
             assert bool((ws[need:] == fill).all())
         assert all(torch.equal(a, b) for a, b in zip(first, outs))
         assert c.dx.intact() and c.dw.intact()
+
+
+@pytest.mark.parametrize("dtype,tokens,vocab,width", [("bf16", 12, 300, 72), ("bf16", 500, 700, 136), ("bf16", 20000, 7003, 72), ("f32", 500, 700, 136), ("f32", 1500, 6200, 130)])
+def test_dloss_of_many_sizes(dtype, tokens, vocab, width):
+    """Each token's row of dx is as near as with equal ones, though dz in bf16 is kept in units of the largest (2^-90 of it times a probability is above 2^-126)."""
+    c = Case(tokens, vocab, width, DT[dtype]).forward()
+    c.dloss.copy_(torch.exp2(torch.randint(-60, 31, (tokens,), generator=gen(4), device=DEV).float()) * torch.where(c.dloss < 0, -1, 1))
+    c.backward().check_backward()
