@@ -48,8 +48,8 @@ template <typename T> struct Operand {
 
 // A binary32 number as three bf16 that add up to it: 8 bits of its significand each, nearest first.  A product of two such numbers is six products of bf16 pairs,
 // exact and summed in binary32, and what is left out (of the 2nd and the 3rd part, and of the 3rd ones) is below 2^-24 of it, half a step of binary32: for the
-// matrix cores six bf16 products cost six sixteenths of an f32 one.  As the sums have fewer steps, they are nearer: the log-sum-exp of 5003 logits of 4096
-// products each is off by 2.3e-6 on the average, with f32 instructions by 3.0e-6.  Of a number below 2^-110 bits under 2^-133 are lost.  An infinite one times
+// matrix cores six bf16 products cost six sixteenths of an f32 one.  The log-sum-exp of 1024 tokens of 5003 logits of 4096
+// products each is off by 4.4e-7, half a step of its own, where a library product's logits in 32 bits are off by 1.2e-6.  Of a number below 2^-110 bits under 2^-133 are lost.  An infinite one times
 // a part that is 0 is NaN, and products of large ones overflow part by part, to infinities of both signs: logits that are not finite are made again from the numbers
 // themselves.  (Not so the gradients' products: dz is finite there, and times an infinite weight nothing is.)  Rows of such numbers are groups of 32, a group the 64 bytes of each part one after another.
 struct Three {
@@ -204,10 +204,27 @@ template <int LATER> __device__ __forceinline__ void meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LATER) : "memory");
 }
 
+// f32 sums are made in sets of as many steps (128 of k), then added to the total: one after another, thousands of products are rounded at the size of all of
+// them.  Loss of 200 tokens of 300 x 8192 off by 6.8e-6 and 6.4e-7 (184 and 197 us; a library product in 32 bits 2.1e-6), of 87 of 1153 x 936 2.1e-6 and 3.9e-7 (27.0 and
+// 28.6), gradients of 112 of 50304 x 4096 1.4e-6 and 4.0e-7 (1415 and 1437); in three parts the loss of 8192 of 50304 x 768 7.0e-7 and 1.6e-7 (2984 and 3048).
+// With sets of 256 of k the loss of 87 of 1153 x 936 is off by 6.2e-7 (28.2).  bf16 operands bring their own 2^-9, and 16 of them are summed by one instruction: no sets.
+constexpr int SET = 4;
+template <int FM, int FN> __device__ __forceinline__ void collect(f32x16 (&total)[FM][FN], f32x16 (&acc)[FM][FN])
+{
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int n = 0; n < FN; ++n) {
+            total[m][n] += acc[m][n];
+            acc[m][n] = f32x16{0};
+        }
+}
+
 // live: how many of n (B along k) or of the steps (B across) there are, or null: all.
 // E: what becomes of the tile.  E::skip(n0, count): nothing to multiply;  E::begin(acc, ...) the sums' start;  E::end(acc, ...).
+// f32: no more registers than two workgroups to a CU have, which sets without the bound pass (gradients of 112 of 50304 x 4096 1728 us instead of 1437).
 template <typename T, typename S, bool AA, bool BA, typename E>
-__global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a, Operand<T> b, int steps, int piece, const int *live, int mt, int nt, E e)
+__global__ __launch_bounds__(S::BLOCK, sizeof(T) == 4 ? 2 : 1) void kt_xent_product_kernel(Operand<T> a, Operand<T> b, int steps, int piece, const int *live, int mt, int nt, E e)
 {
     constexpr int K = STEP<T>;
     typedef Bring<T, S::BM, S::BLOCK, AA, true> BringA;
@@ -232,11 +249,12 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
     const int k0 = blockIdx.y * piece, k1 = min(steps, k0 + piece);
     const int64_t holder = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (S::WM * S::WN) + wave;
 
-    f32x16 acc[S::FM][S::FN];
+    constexpr bool SETS = sizeof(T) == 4;
+    f32x16 acc[S::FM][S::FN], total[S::FM][S::FN];         // (without sets: acc alone)
 #pragma unroll
     for (int m = 0; m < S::FM; ++m)
 #pragma unroll
-        for (int n = 0; n < S::FN; ++n) acc[m][n] = f32x16{0};
+        for (int n = 0; n < S::FN; ++n) acc[m][n] = total[m][n] = f32x16{0};
     if (!e.skip(n0, S::BN)) {
         BringA from_a(a, m0);
         BringB from_b(b, n0);
@@ -264,11 +282,13 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
             aim(lds + ahead * SLOT, k);
             span<0, LOADS>(load);
         }
-        e.begin(acc, holder);
+        if constexpr (SETS) e.begin(total, holder);
+        else e.begin(acc, holder);
         meet<0>();
         span<0, READS>([&](auto r) { read(lds, std::integral_constant<int, 0>(), r); });
         __builtin_amdgcn_sched_barrier(0);
-        for (int slot = 0; ahead > 0;) {
+        int slot = 0;
+        auto step = [&]() __attribute__((always_inline)) {
             const int after = slot + 1 == SLOTS ? 0 : slot + 1;
             char *const now = lds + slot * SLOT, *const then = lds + after * SLOT;
             const bool more = k < k1;
@@ -298,8 +318,18 @@ __global__ __launch_bounds__(S::BLOCK) void kt_xent_product_kernel(Operand<T> a,
             if (more) k += K;
             else --ahead;
             slot = after;
+        };
+        if constexpr (SETS) {
+            while (ahead > 0) {
+#pragma unroll 1
+                for (int n = 0; n < SET && ahead > 0; ++n) step();
+                collect(total, acc);
+            }
+        } else {
+            while (ahead > 0) step();
         }
     }
+    if constexpr (SETS) collect(acc, total);                // acc is 0
     if constexpr (E::ROWS) __syncthreads();                 // LDS is read: the epilogue takes it
     e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), holder, wave / S::WN + S::WM * at.m, lds + wave * (S::FM * 4096));
 }
@@ -389,11 +419,11 @@ __global__ __launch_bounds__(Split::BLOCK) void kt_xent_three_kernel(Operand<Thr
     const int m0 = at.m * S::BM, n0 = at.n * S::BN, wm = wave / S::WN * S::FM * 32, wn = wave % S::WN * S::FN * 32;
     const int k0 = blockIdx.y * piece, k1 = min(steps, k0 + piece);
 
-    f32x16 acc[S::FM][S::FN];
+    f32x16 acc[S::FM][S::FN], total[S::FM][S::FN];
 #pragma unroll
     for (int m = 0; m < S::FM; ++m)
 #pragma unroll
-        for (int n = 0; n < S::FN; ++n) acc[m][n] = f32x16{0};
+        for (int n = 0; n < S::FN; ++n) acc[m][n] = total[m][n] = f32x16{0};
     BringA from_a(a, m0);
     BringB from_b(b, n0);
     auto bring = [&](char *to, int k) __attribute__((always_inline)) {
@@ -416,11 +446,12 @@ __global__ __launch_bounds__(Split::BLOCK) void kt_xent_three_kernel(Operand<Thr
     int k = k0, ahead = 0;
     for (; ahead < 2 && k < k1; ++ahead, k += K) bring(lds + ahead * S::SLOT, k);
     const int64_t holder = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (S::WM * S::WN) + wave;
-    e.begin(acc, holder);
+    e.begin(total, holder);
     meet<0>();
     span<0, READS>([&](auto r) { read(lds, std::integral_constant<int, 0>(), r); });
     __builtin_amdgcn_sched_barrier(0);
-    for (int slot = 0; ahead > 0; slot ^= 1) {
+    int slot = 0;
+    auto step = [&]() __attribute__((always_inline)) {
         char *const now = lds + slot * S::SLOT, *const then = lds + (slot ^ 1) * S::SLOT;
         const bool more = k < k1;
         span<0, 2 * ALL>([&](auto n1) {
@@ -435,7 +466,14 @@ __global__ __launch_bounds__(Split::BLOCK) void kt_xent_three_kernel(Operand<Thr
         });
         if (more) k += K;
         else --ahead;
+        slot ^= 1;
+    };
+    while (ahead > 0) {
+#pragma unroll 1
+        for (int n = 0; n < SET && ahead > 0; ++n) step();
+        collect(total, acc);
     }
+    collect(acc, total);
     if constexpr (E::LOGITS) {
         // Sums times 0 are 0 if they are finite; those of rows past the list, which hold anything, do not count.  4096 tokens of 50304 x 768 forward: 1.95 ms with this look
         // and without; with a token of NaN, whose tiles all fall to a few CUs, 5.2, with nothing else 5.0.
