@@ -22,7 +22,7 @@ namespace {
 // first products are read beside the last products of this one: the matrix cores wait for nothing but the barrier itself.
 // A fragment is 16 bytes a lane for both types: lane l holds V of k (V c + ... : chunk c of a step, half h = l / 32, k = V (2 c + h) + j) of its row.  The 32 rows of a fragment of A are taken in an order that
 // gives a lane of D 16 neighbouring m: register r of half h is row 16 h + r.
-// Measured: 16384 tokens of 50304 x 2048 bf16 forward 2.79 to 2.86 ms, 1.18 to 1.21 PFLOP/s (a library product of these sizes that stores z takes 2.85), matrix cores busy
+// Measured: 16384 tokens of 50304 x 2048 bf16 forward 2.74 to 2.96 ms, 1.14 to 1.23 PFLOP/s (a library product of these sizes that stores z takes 2.82 to 2.96), matrix cores busy
 // 62 % of the cycles at a clock that their load brings down; products of 16384 x 8192 x 2048, dz 495 to 535 us, dx 505 to 545, dw 460 to 510.  f32, 4096 of
 // 50304 x 768: 126 TFLOP/s.
 
@@ -1189,9 +1189,9 @@ bool few_tokens(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
 }
 
 // Whether f32 products are made of numbers in three parts: where the copies into parts cost little beside them and tiles of 256 x 128 keep the chip busy.  The
-// same in both passes, so that their logits have the same bits.  us, f32 instructions and parts: 8192 tokens of 50304 x 768 4810 and 3020 forward and
-// 14870 and 10100 backward, 1024 of 5003 x 1001 118 and 90, 365 and 231, 512 of 5003 x 1024 65 and 87, 204 and 171; but 2048 of 1000 x 4096 172 and 247, 468
-// and 436, 1024 of 1000 x 768 26 and 64, 93 and 117, 100 of 50304 x 768 114 and 182, 343 and 375.
+// same in both passes, so that their logits have the same bits.  us, f32 instructions and parts: 8192 tokens of 50304 x 768 4850 and 3010 forward and
+// 15300 and 10030 backward, 1024 of 5003 x 1001 115 and 90, 328 and 233, 512 of 5003 x 1024 65 and 89, 188 and 176; but 2048 of 1000 x 4096 181 and 263, 471
+// and 451, 1024 of 1000 x 768 28 and 68, 92 and 125, 100 of 50304 x 768 111 and 150, 329 and 334.
 bool in_three(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width)
 {
     return dt == KT_F32 && width >= 128 && tokens >= 256 && over(vocab, Split::BM) * over(tokens, Split::BN) >= 80;
