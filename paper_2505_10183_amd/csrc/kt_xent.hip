@@ -5,8 +5,8 @@
 // token, which a small kernel joins.  The backward pass goes over pieces of the vocabulary: it makes z of a piece again, leaves dz in the
 // workspace in the operands' type, and takes the other two products from there; dx is carried from piece to piece in binary32.
 // dz is rounded to bf16 as an operand of bf16 products, as attention's probabilities are, in units of the largest dloss (a mean's 1 / tokens would be the same
-// error in all): gradients stand 2.0 to 2.4e-3 from the definition in norm, with dz in binary32 and one rounding 1.7e-3; of one token alone, whose
-// target's element is most of both gradients, 2.7e-3.
+// error in all).  A target's element is most of its token's gradients and would carry its rounding into all of them, so what that takes of it (Rests) is added to both
+// products: gradients stand 1.65 to 1.75e-3 from the definition in norm, as far as one rounding of the result leaves them, instead of 2.0 to 2.8e-3.
 //
 // Tokens without a target (or with dloss 0) take no part: the backward pass, and the forward pass where it is long, list the others and copy their rows
 // of x one after another, so that the products are made of those alone, and what the rows of the others hold reaches nothing.
@@ -204,6 +204,14 @@ template <int LATER> __device__ __forceinline__ void meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LATER) : "memory");
 }
 
+// 16 bytes a lane from memory to LDS, the lanes' one after another from `lds` on, which is the same in all of a wavefront's.
+__device__ __forceinline__ void to_lds([[maybe_unused]] const void *p, [[maybe_unused]] char *lds)
+{
+#ifdef __HIP_DEVICE_COMPILE__           // the host pass does not know the builtin
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)p, (KT_LDS void *)lds, 16, 0, 0);
+#endif
+}
+
 // f32 sums are made in sets of as many steps (128 of k), then added to the total: one after another, thousands of products are rounded at the size of all of
 // them.  Loss of 200 tokens of 300 x 8192 off by 6.8e-6 and 6.4e-7 (184 and 197 us; a library product in 32 bits 2.1e-6), of 87 of 1153 x 936 2.1e-6 and 3.9e-7 (27.0 and
 // 28.6), gradients of 112 of 50304 x 4096 1.4e-6 and 4.0e-7 (1415 and 1437); in three parts the loss of 8192 of 50304 x 768 7.0e-7 and 1.6e-7 (2984 and 3048).
@@ -219,6 +227,18 @@ template <int FM, int FN> __device__ __forceinline__ void collect(f32x16 (&total
             acc[m][n] = f32x16{0};
         }
 }
+
+// bf16: what rounding takes from a target's element of dz (in its units), which is most of a token's gradients: 2^-9 of them where nothing makes up for it.  dx adds
+// it times the target's row of the weight to its sums; for the weight's gradient a tile adds it times the rows of x whose target is one of its own.  Without and with it, us:
+// 16384 tokens of 50304 x 2048 9230 and 9360, 4099 of 5003 x 1001 (then the table's gradient) 201 and 211, 810 of 1000 x 1024 38.0 and 44.1, 15329 of 300 x 1024, whose tiles
+// have nearly all tokens each, 91.6 and 114, one of 50304 x 2048 148 and 155.
+struct Rests {
+    const float *rest;              // of each row of the list, or null: none
+    const int *goals;               // its target
+    int first;                      // dw: of the piece of the vocabulary
+    const void *w;                  // dx: the weight, rows ldw apart
+    int64_t ldw;
+};
 
 // live: how many of n (B along k) or of the steps (B across) there are, or null: all.
 // E: what becomes of the tile.  E::skip(n0, count): nothing to multiply;  E::begin(acc, ...) the sums' start;  E::end(acc, ...).
@@ -330,6 +350,82 @@ __global__ __launch_bounds__(S::BLOCK, sizeof(T) == 4 ? 2 : 1) void kt_xent_prod
         }
     }
     if constexpr (SETS) collect(acc, total);                // acc is 0
+    if constexpr (E::TARGETS) {
+        // Rests: products of the rows of x whose target is one of this tile's n with a matrix of their rests and zeros.  The rows, of the tokens that this workgroup has gone
+        // through, are listed up to LIST of them at a time in the other slot; 64 of them are a step.
+        static_assert(!AA && !BA && sizeof(T) == 2, "the weight's gradient in bf16");
+        constexpr int LIST = 4096, WAVES = S::BLOCK / 64, EACH = LIST / S::BLOCK, MOST = 64;
+        static_assert(SLOTS >= 2 && LIST * 4 <= SLOT && K == MOST, "a slot holds the list");
+        struct Own {
+            int n;
+            float rest;
+        };
+        Own *const own = (Own *)(lds + ABYTES);
+        int *const counts = (int *)(own + MOST), *const list = (int *)(lds + SLOT);
+        const int there = min(S::BM, a.count - m0);
+        for (int base = k0; base < k1; base += LIST) {
+            int goal[EACH], n = 0;
+            const int mine = base + wave * (LIST / WAVES) + lane;
+#pragma unroll
+            for (int u = 0; u < EACH; ++u) goal[u] = mine + u * 64 < k1 ? e.rests.goals[mine + u * 64] - e.rests.first - n0 : -1;
+#pragma unroll
+            for (int u = 0; u < EACH; ++u) n += __popcll(__ballot(goal[u] >= 0 && goal[u] < S::BN));
+            meet<0>();                                      // LDS is read
+            if (lane == 0) counts[wave] = n;
+            meet<0>();
+            int before = 0, all = 0;
+            for (int w = 0; w < WAVES; ++w) {
+                before += w < wave ? counts[w] : 0;
+                all += counts[w];
+            }
+            all = __builtin_amdgcn_readfirstlane(all);
+            if (all == 0) continue;
+#pragma unroll
+            for (int u = 0; u < EACH; ++u) {
+                const bool here = goal[u] >= 0 && goal[u] < S::BN;
+                const uint64_t word = __ballot(here);
+                if (here) list[before + __popcll(word & ((1ull << lane) - 1))] = mine + u * 64;
+                before += __popcll(word);
+            }
+            meet<0>();
+            for (int s = 0; s < all; s += MOST) {
+                const int left = all - s;
+#pragma unroll
+                for (int u = 0; u < BringA::N; ++u) {
+                    // rows past the list's end meet zeros only, and columns past the width are nobody's: any of them will do
+                    const int row = list[s + min(BringA::row_of(u), left - 1)], c = BringA::col_of(u);
+                    to_lds(a.p + row * a.ld + m0 + (c < there ? c : 0), lds + wave * 1024 + u * (S::BLOCK * 16));
+                }
+                if (wave == 0) {
+                    Own o{-1, 0.0f};
+                    if (lane < left) {
+                        const int row = list[s + lane];
+                        o = Own{e.rests.goals[row] - e.rests.first - n0, e.rests.rest[row]};
+                    }
+                    own[lane] = o;
+                }
+                meet<0>();
+#pragma unroll
+                for (int c = 0; c < ROW / 32; ++c) {
+                    if (16 * c >= left) break;
+                    F fa[S::FM], fb[S::FN];
+#pragma unroll
+                    for (int i = 0; i < S::FM; ++i) fa[i] = fragment<T, S::BM, AA, true>(lds, wm + 32 * i, c);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const Own o = own[16 * c + 8 * (lane >> 5) + q];
+#pragma unroll
+                        for (int j = 0; j < S::FN; ++j) fb[j][q] = o.n == wn + 32 * j + (lane & 31) ? (T)o.rest : (T)0.0f;
+                    }
+#pragma unroll
+                    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                        for (int j = 0; j < S::FN; ++j) multiply<0>(acc[i][j], fa[i], fb[j]);
+                }
+                meet<0>();
+            }
+        }
+    }
     if constexpr (E::ROWS) __syncthreads();                 // LDS is read: the epilogue takes it
     e.end(acc, m0 + wm + (lane >> 5) * 16, n0 + wn + (lane & 31), holder, wave / S::WN + S::WM * at.m, lds + wave * (S::FM * 4096));
 }
@@ -573,7 +669,7 @@ template <int FM, typename G, typename F> __device__ __forceinline__ void store_
 // Forward: for a wavefront's vocabulary rows the largest logit of each token and the sum of the exponentials over it; the
 // target's logit.
 template <typename I> struct Stats {
-    static constexpr bool ROWS = false, LOGITS = true;
+    static constexpr bool ROWS = false, LOGITS = true, TARGETS = false;
     f32x2 *parts;                   // [part][tokens]
     float *hit;                     // [tokens]
     const I *targets;
@@ -645,7 +741,7 @@ template <typename I> struct Stats {
 
 // Backward: dz of a piece of the vocabulary, rows of tokens `ld` apart; columns past the vocabulary are zeros.
 template <typename T, typename I> struct Slope {
-    static constexpr bool ROWS = true, LOGITS = true, HALVES = std::is_same_v<T, bf16>;
+    static constexpr bool ROWS = true, LOGITS = true, TARGETS = false, HALVES = std::is_same_v<T, bf16>;
     T *dz;
     int64_t ld;
     const float *lse, *dloss, *unit;
@@ -653,6 +749,7 @@ template <typename T, typename I> struct Slope {
     const I *targets;
     const int *map, *live;          // the token of each row, and their number
     int tokens, vocab, first, end_, parts;
+    float *rest;                    // [row], bf16: what rounding takes from the target's element
     __device__ __forceinline__ bool skip(int, int) const { return false; }
     template <typename A> __device__ __forceinline__ void begin(A &, int64_t) const {}
     __device__ __forceinline__ float share(int at) const { return HALVES ? dloss[at] / *unit : dloss[at]; }
@@ -665,7 +762,7 @@ template <typename T, typename I> struct Slope {
             if (first_row >= rows) continue;
             const int at = map[min(row, rows - 1)], target = (int)targets[at] - first, room = end_ - first;
             const float up = share(at), base = lse[at];
-            float sum = 0;
+            float sum = 0, hit = 0;
             auto values = [&](int i, float *f) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -673,6 +770,7 @@ template <typename T, typename I> struct Slope {
                     const float e = __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E), p = e - (v == target ? 1.0f : 0.0f);
                     f[r] = v < room ? p * up : 0.0f;
                     if constexpr (!HALVES) sum += v < room && v != target ? e : 0.0f;
+                    else hit = v == target ? f[r] : hit;
                 }
             };
             if constexpr (std::is_same_v<T, Three>) {
@@ -691,6 +789,10 @@ template <typename T, typename I> struct Slope {
             if constexpr (!HALVES) {
                 sum += __shfl_xor(sum, 32);
                 if (others && h == 0 && row < rows) others[(int64_t)row * parts + part] = sum;
+            } else {
+                // 16 of each 32 columns are this lane's
+                const int in = target - m;
+                if (in >= 0 && in < FM * 32 && in % 32 < 16 && row < rows) rest[row] = hit - (float)(bf16)hit;
             }
         }
     }
@@ -706,6 +808,9 @@ template <typename T, typename I> struct Slope {
             const float e = __builtin_amdgcn_exp2f((z[r] - base) * LOG2E), p = e - (r == want ? 1.0f : 0.0f);
             f[r] = (T)(r < room ? p * up : 0.0f);
             sum += r < room && r != want ? e : 0.0f;
+            if constexpr (HALVES) {
+                if (r == want) rest[t] = p * up - (float)f[r];
+            }
         }
         if constexpr (!HALVES) {
             sum += __shfl_xor(sum, 16);
@@ -816,7 +921,7 @@ template <int FM, int FN> __device__ __forceinline__ void resume(const float *su
             }
 }
 struct Carry {
-    static constexpr bool ROWS = false, LOGITS = false;
+    static constexpr bool ROWS = false, LOGITS = false, TARGETS = false;
     float *sums;
     bool first;
     __device__ __forceinline__ bool skip(int, int) const { return false; }
@@ -842,14 +947,15 @@ struct Carry {
 };
 
 // The result, or (G = float, pieces of k) the sums of a piece.
-template <typename G> struct Result {
-    static constexpr bool ROWS = true, LOGITS = false;
+template <typename G, bool TARGETS_ = false> struct Result {
+    static constexpr bool ROWS = true, LOGITS = false, TARGETS = TARGETS_;
     G *out;
     int64_t ld, apart;              // rows; matrices of the pieces of k
     const float *sums;              // what Carry left, or null
     const int *map, *live;          // where a row goes, and how many there are, or null
     const float *unit;              // what the sums are in, or null: 1
     int rows, cols;
+    Rests rests;                    // bf16
     __device__ __forceinline__ bool skip(int, int) const { return false; }
     template <int FM, int FN> __device__ __forceinline__ void begin(f32x16 (&acc)[FM][FN], int64_t holder) const
     {
@@ -863,9 +969,25 @@ template <typename G> struct Result {
         for (int j = 0; j < FN; ++j) {
             const int first = n + 32 * j - l, end = live ? scalar(live) : rows;
             if (first >= end || m0 >= cols) continue;
+            const G *w = nullptr;
+            float more = 0;
+            if constexpr (sizeof(G) == 2 && !TARGETS) {
+                if (rests.rest && n + 32 * j < end) {
+                    more = rests.rest[n + 32 * j];
+                    w = static_cast<const G *>(rests.w) + rests.goals[n + 32 * j] * rests.ldw;
+                }
+            }
             store_rows<FM>(scratch, out + blockIdx.y * apart + m0, ld, first, end - first, cols - m0, map, [&](int i, float *f) {
+                if constexpr (sizeof(G) == 2 && !TARGETS) {
+                    float g[16];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) f[r] = acc[i][j][r] * of;
+                    for (int r = 0; r < 16; r += 8) widen<G>(w ? ld_chunk(w, m + 32 * i + r, cols) : u32x4{0, 0, 0, 0}, g + r);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) f[r] = (acc[i][j][r] + more * g[r]) * of;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) f[r] = acc[i][j][r] * of;
+                }
             });
         }
     }
@@ -1052,7 +1174,7 @@ __global__ __launch_bounds__(1024) void kt_xent_count_kernel(const I *targets, c
 // one launch, or (`counts`, of 8193 tokens on) adds what others have counted: 16384 tokens take 20 us by themselves and 10 in two launches.
 template <typename I>
 __global__ __launch_bounds__(1024) void kt_xent_list_kernel(const I *targets, const float *dloss, int tokens, int vocab, const int *counts, const float *tops, int *map,
-                                                            int *live, float *unit)
+                                                            int *live, float *unit, int *goals)
 {
     __shared__ int before[16], mine[16];
     __shared__ float most[16];
@@ -1085,7 +1207,11 @@ __global__ __launch_bounds__(1024) void kt_xent_list_kernel(const I *targets, co
         at += before[w] + (w < wave ? mine[w] : 0);
         all += before[w] + mine[w];
     }
-    if (on) map[at + __popcll(word & ((1ull << lane) - 1))] = t;
+    if (on) {
+        const int row = at + __popcll(word & ((1ull << lane) - 1));
+        map[row] = t;
+        if (goals) goals[row] = (int)targets[t];
+    }
     if (threadIdx.x || blockIdx.x != gridDim.x - 1) return;
     *live = all;
     if (!unit) return;
@@ -1111,10 +1237,10 @@ __global__ __launch_bounds__(256) void kt_xent_gather_kernel(const T *x, int64_t
     }
 }
 
-// The sum of pieces of k, in their order; rows of the pieces `ldp` apart.  map, live, unit: as Result has them.
+// The sum of pieces of k, in their order; rows of the pieces `ldp` apart.  map, live, unit, rests: as Result has them.
 template <typename G>
 __global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, int pieces, int64_t apart, int ldp, int rows, int cols, G *out, int64_t ld, const int *map,
-                                                           const int *live, const float *unit)
+                                                           const int *live, const float *unit, Rests rests)
 {
     const int across = (cols + 3) / 4;
     if (live) rows = *live;
@@ -1126,6 +1252,13 @@ __global__ __launch_bounds__(256) void kt_xent_sum_kernel(const float *parts, in
         const int64_t to = (map ? map[row] : row) * ld;
         f32x4 s = *(const f32x4 *)p;
         for (int k = 1; k < pieces; ++k) s += *(const f32x4 *)(p + k * apart);
+        if constexpr (sizeof(G) == 2) {
+            if (rests.rest) {
+                const G *w = static_cast<const G *>(rests.w) + rests.goals[row] * rests.ldw;
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < cols) s[j] += rests.rest[row] * (float)w[c + j];
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (c + j < cols) out[to + c + j] = (G)(s[j] * of);
@@ -1211,6 +1344,7 @@ struct Plan {
     int64_t ldp;                    // backward: elements to a row of sums
     Cut kx;                         // of dx over a piece of the vocabulary
     bool list;                      // whether the tokens that take part are listed
+    int64_t goals, rest;            // bf16, backward
     int64_t x, w, parts, hit, others, likely, ids, table, dz, map, live, acc, sums, bytes;      // where in the workspace
 };
 // Wavefronts that share a token's logits of `rows` rows of the vocabulary.
@@ -1268,6 +1402,10 @@ Plan plan_of(kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width, bool bwd
             p.ids = take(tokens * 4);
             p.table = take(kt_embedding_bwd_ws(tokens, vocab, width));
         }
+    }
+    if (dt == KT_BF16) {
+        p.goals = take(tokens * 4);
+        p.rest = take(tokens * 4);
     }
     p.dz = take(tokens * p.most * p.es);
     p.kx = cut_of(dt, p.three, width, tokens, at_most(p.most, vocab), MOST_PIECES);
@@ -1354,14 +1492,14 @@ int aligned_rows(bool as_is, const T *x, int64_t ldx, int64_t width, int64_t row
 // The list of the tokens that take part and their rows of x; zeros in dx's rows of the others.
 template <typename X, typename T, typename I>
 int list(const T *x, int64_t ldx, int64_t width, const I *targets, const float *dloss, int64_t tokens, int64_t vocab, X *copy, int64_t wide, int *map,
-         int *live, float *unit, T *dx, int64_t lddx, hipStream_t s)
+         int *live, float *unit, T *dx, int64_t lddx, int *goals, hipStream_t s)
 {
     const unsigned groups = (unsigned)over(tokens, 1024);
     int *const counts = groups > 8 ? live + 2 : nullptr;
     float *const tops = (float *)(live + 2 + groups);
     if (counts) kt_xent_count_kernel<I><<<groups, 1024, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, counts, tops);
     KT_GO((int)hipGetLastError());
-    kt_xent_list_kernel<I><<<groups, 1024, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, counts, tops, map, live, unit);
+    kt_xent_list_kernel<I><<<groups, 1024, 0, s>>>(targets, dloss, (int)tokens, (int)vocab, counts, tops, map, live, unit, goals);
     KT_GO((int)hipGetLastError());
     const int64_t blocks = over(tokens * over(wide, 64 * EACH<X>), 4);
     kt_xent_gather_kernel<X, T, I><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(x, ldx, (int)width, copy, wide, map, live, targets, dloss, (int)tokens, (int)vocab, dx, lddx);
@@ -1384,7 +1522,7 @@ int fwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
         const Stats<I> e{parts, hit, targets, nullptr, nullptr, (int)tokens, (int)vocab, 0, (int)vocab, 0};
         KT_GO(few(w, ldw, vocab, x, ldx, tokens, width, e, s));
     } else if (p.list) {
-        KT_GO((list<X, T, I>(x, ldx, width, targets, nullptr, tokens, vocab, copy, p.wide, map, live, nullptr, nullptr, 0, s)));
+        KT_GO((list<X, T, I>(x, ldx, width, targets, nullptr, tokens, vocab, copy, p.wide, map, live, nullptr, nullptr, 0, nullptr, s)));
         b = Operand<X>{copy, p.wide, (int)tokens};
     } else {
         KT_GO((aligned_rows<X, T>(plain(x, ldx, width), x, ldx, width, tokens, copy, p.wide, &b, s)));
@@ -1401,10 +1539,10 @@ int fwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
 }
 
 template <typename G> int sum(const float *parts, const Cut &k, int64_t apart, int64_t ldp, int64_t rows, int64_t cols, G *out, int64_t ld, const int *map, const int *live,
-                              const float *unit, hipStream_t s)
+                              const float *unit, const Rests &rests, hipStream_t s)
 {
     const int64_t blocks = over(rows * over(cols, 4), 256);
-    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.pieces, apart, (int)ldp, (int)rows, (int)cols, out, ld, map, live, unit);
+    kt_xent_sum_kernel<G><<<(unsigned)at_most(blocks, 1 << 20), 256, 0, s>>>(parts, k.pieces, apart, (int)ldp, (int)rows, (int)cols, out, ld, map, live, unit, rests);
     return (int)hipGetLastError();
 }
 
@@ -1424,16 +1562,20 @@ int bwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
     const bool several = piece < vocab;
     float *const others = sizeof(T) == 4 ? (float *)(ws + p.others) : nullptr, *const likely = (float *)(ws + p.likely);
     X *const copy = (X *)(ws + p.x);
+    constexpr bool HALVES = sizeof(T) == 2;
+    int *const goals = HALVES ? (int *)(ws + p.goals) : nullptr;
+    float *const rest = HALVES ? (float *)(ws + p.rest) : nullptr;
+    const Rests none{}, of_dx{rest, goals, 0, w, ldw};
     Operand<X> a;
     const Operand<X> b{copy, p.wide, (int)tokens};
-    if (tokens) KT_GO((list<X, T, I>(x, ldx, width, targets, dloss, tokens, vocab, copy, p.wide, map, live, unit, dx, lddx, s)));
+    if (tokens) KT_GO((list<X, T, I>(x, ldx, width, targets, dloss, tokens, vocab, copy, p.wide, map, live, unit, dx, lddx, goals, s)));
     for (int64_t v = 0, rows; v < vocab; v += rows) {
         rows = at_most(piece, vocab - v);
         if (tokens) {
             KT_GO((aligned_rows<X, T>(w_as_is, w + v * ldw, ldw, width, rows, (X *)(ws + p.w), p.wide, &a, s)));
             const Cut z = cut_of(dt, p.three, rows, tokens, width, 1);
             const int parts = (int)sharing(p.few, z, rows);
-            const Slope<X, I> e{dz, p.most, lse, dloss, unit, others, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows), parts};
+            const Slope<X, I> e{dz, p.most, lse, dloss, unit, others, targets, map, live, (int)tokens, (int)vocab, (int)v, (int)(v + rows), parts, rest};
             bool made = false;
             if constexpr (std::is_same_v<X, T>) {
                 made = p.few;
@@ -1455,25 +1597,26 @@ int bwd(const Plan &p, kt_dtype dt, int64_t tokens, int64_t vocab, int64_t width
                 const Carry e{acc, first};
                 KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else if (k.pieces == 1) {
-                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, map, live, unit, (int)tokens, (int)width};
+                const Result<T> e{dx, lddx, 0, first ? nullptr : acc, map, live, unit, (int)tokens, (int)width, of_dx};
                 KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
             } else {
                 const int64_t apart = tokens * p.ldp;
-                const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, nullptr, live, nullptr, (int)tokens, (int)p.ldp};
+                const Result<float> e{sums, p.ldp, apart, first ? nullptr : acc, nullptr, live, nullptr, (int)tokens, (int)p.ldp, none};
                 KT_GO((product<X, false, true>(k, wide, width, slope, tokens, rows, live, e, s)));
-                KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, map, live, unit, s));
+                KT_GO(sum(sums, k, apart, p.ldp, tokens, width, dx, lddx, map, live, unit, of_dx, s));
             }
         }
         if (dw) {
             const Operand<X> wide{b.p, b.ld, (int)cols}, slope{dz, p.most, (int)up(rows, UNIT)};
             const Cut k = cut_of(dt, p.three, width, rows, tokens, MOST_PIECES);
+            const Rests of_dw{rest, goals, (int)v, nullptr, 0};
             if (k.pieces == 1) {
-                const Result<T> e{dw + v * lddw, lddw, 0, nullptr, nullptr, nullptr, unit, (int)rows, (int)width};
+                const Result<T, HALVES> e{dw + v * lddw, lddw, 0, nullptr, nullptr, nullptr, unit, (int)rows, (int)width, of_dw};
                 KT_GO((product<X, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
             } else {
-                const Result<float> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, nullptr, nullptr, (int)rows, (int)p.ldp};
+                const Result<float, HALVES> e{sums, p.ldp, rows * p.ldp, nullptr, nullptr, nullptr, nullptr, (int)rows, (int)p.ldp, of_dw};
                 KT_GO((product<X, false, false>(k, wide, width, slope, rows, tokens, tokens ? live : nullptr, e, s)));
-                KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, nullptr, nullptr, unit, s));
+                KT_GO(sum(sums, k, rows * p.ldp, p.ldp, rows, width, dw + v * lddw, lddw, nullptr, nullptr, unit, none, s));
             }
         }
     }
